@@ -71,7 +71,9 @@ typedef enum {
   ZO_ERR_WORKSPACE = 6
 } zo_status;
 
-typedef enum { ZO_F32 = 0, ZO_BF16 = 1, ZO_F16 = 2 } zo_dtype;
+/* ZO_E4M3 (8-bit floats of 4 exponent and 3 mantissa bits, no infinities, largest 448) is the type
+ * of a zo_kv_cache only. */
+typedef enum { ZO_F32 = 0, ZO_BF16 = 1, ZO_F16 = 2, ZO_E4M3 = 3 } zo_dtype;
 /* Epilogues fused into the perturbed linear's output (zo_perturbed_linear_apply_ex). */
 typedef enum { ZO_EPI_NONE = 0, ZO_EPI_RELU = 1, ZO_EPI_RESIDUAL = 2, ZO_EPI_SILU_MUL = 3 } zo_epilogue;
 
@@ -617,6 +619,106 @@ int zo_llama_lora_layer_forward(int T, int seq_len, int d, int heads,
                                 const void* H, long long h_block_stride,
                                 const zo_llama_lora_layer* layer, void* H_out,
                                 void* workspace, size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
+ * Answering with a tuned model -- one layer's paged key/value cache: single
+ * tokens, drafted tokens or pieces of prompts, each at its own position,
+ * against the keys and values of what came before.
+ *
+ * Cache.  A pool of num_pages pages; a page holds page_size consecutive
+ * positions of one sequence for every key/value head: K and V are
+ * num_pages x kv_heads x page_size x dh.  With dtype ZO_BF16 or ZO_F16 they
+ * hold the keys and values themselves; with ZO_E4M3 a value is its code times
+ * the scale of its page, head and tensor (k_scale, v_scale: device fp32,
+ * num_pages x kv_heads; NULL for the 16-bit types).
+ *
+ * Batch.  Sequence s has the rows q_start[s] .. q_start[s+1] - 1 (n_s of them)
+ * of the call's row-major tensors and, those included, kv_len[s] positions:
+ * row i of s is at position p = kv_len[s] - n_s + i.  Position t lies in slot
+ * t % page_size of page page_table[s * max_pages + t / page_size].
+ *   nseq       sequences; rows: rows of the call's tensors, of which those
+ *              behind the last sequence's are neither read nor written.
+ *   max_q      at least the largest n_s.
+ *   q_start    device int32 [nseq + 1], not decreasing, within [0, rows];
+ *              NULL: row s is the one row of sequence s (rows >= nseq).
+ *   kv_len     device int32 [nseq].  A row with p < 0 is padding: it is not
+ *              stored, and attends to nothing.
+ *   page_table device int32 [nseq x max_pages].  Entries behind a sequence's
+ *              last position are not used and may hold anything.
+ *   bad_flag   device int, nullable: set to 1 (never cleared here) when a
+ *              sequence breaks these rules: a page outside [0, num_pages), a
+ *              position outside the table, more than max_q rows, or a
+ *              q_start that decreases or leaves [0, rows].  No access leaves
+ *              the tensors then: such positions are not stored, rows that
+ *              attend to one are NaN, rows beyond max_q are not written, and
+ *              q_start is taken as clamped to its range.
+ * The contents of q_start, kv_len and page_table may change between replays of
+ * a captured call. */
+typedef struct {
+  int num_pages, page_size, kv_heads, dh;
+  int dtype; /* zo_dtype: ZO_BF16, ZO_F16 or ZO_E4M3 */
+  void* K;
+  void* V;
+  float* k_scale;
+  float* v_scale;
+} zo_kv_cache;
+
+typedef struct {
+  int nseq, rows, max_q, max_pages;
+  const int* q_start;
+  const int* kv_len;
+  const int* page_table;
+  int* bad_flag;
+} zo_kv_batch;
+
+/* Appends the batch's rows to the cache, rotating keys (and queries) to their
+ * positions on the way: q' = R(p) q, k' = R(p) k as zo_rope rotates, at the
+ * row's own position p.
+ *   dtype     of Q, Q_out, K, V: ZO_BF16 or ZO_F16; a 16-bit cache has the same.
+ *   K, V      rows of kv_heads dh elements, ldk and ldv elements apart.
+ *   Q, Q_out  rows of heads dh elements, ldq and ldqo apart: the rotated queries
+ *             in dtype.  Q_out may be Q (with ldqo = ldq).  Both NULL: no
+ *             queries (heads is not read).  Padding rows are copied.
+ *   rope_base > 1; or 0: no rotation, and then Q and Q_out are NULL.
+ * The angle is formed and reduced in fp64; its sine and cosine and the rotation
+ * are taken in fp32 and rounded once, to the cache's or Q_out's type.
+ * ZO_E4M3: per page, head and tensor, let a be the largest finite magnitude
+ * among the call's values there and need the smallest power of two with
+ * a <= 448 need (within [2^-126, 2^120]).  If the call stores the page's first
+ * slot, the scale becomes need; else max(scale, need), and where that is
+ * larger than before, the page's earlier slots are rounded again to the new
+ * scale (exact but for values under 2^-6 of it).  Then code = e4m3(x / scale),
+ * to nearest even.  Values that are not finite are stored as NaN.
+ * One call must not store into one page of one head from two sequences, and no
+ * tensor of the call may overlap another but Q_out = Q.
+ * Limits: dh = 64 or 128; page_size 16, 32, 64, 128 or 256; ld* % 8 == 0;
+ * 16-byte aligned tensors. */
+int zo_kv_append(const zo_kv_cache* cache, const zo_kv_batch* batch, int heads,
+                 int dtype, const void* Q, long long ldq, void* Q_out,
+                 long long ldqo, const void* K, long long ldk, const void* V,
+                 long long ldv, float rope_base, void* stream);
+
+/* Causal attention of the batch's rows over the cache, which holds their own
+ * keys and values already: row i of sequence s attends to the positions
+ * t <= p with weights softmax(q . k_t / sqrt(dh)); query head h reads key/value
+ * head h / (heads / kv_heads).  A padding row's output is 0.
+ *   Q, O      rows of heads dh elements of dtype (ZO_BF16 or ZO_F16; a 16-bit
+ *             cache has the same), ldq and ldo apart.  O may be Q (ldo = ldq).
+ * Slots behind a sequence's last position may hold anything, NaN included.
+ * Arithmetic: fp32 softmax; the products run on the MFMA (8-bit codes are
+ * exact in 16 bits; their scales are applied in fp32) with P as a hi + lo
+ * 16-bit pair, as for zo_causal_attention.
+ * The workspace holds partial results where a sequence's keys are split over
+ * workgroups; its size depends on the host arguments only (0 where nothing is
+ * split), and calls that may run at the same time need one each.
+ * Limits: those of zo_kv_append; heads % kv_heads == 0. */
+size_t zo_paged_attention_workspace(const zo_kv_cache* cache,
+                                    const zo_kv_batch* batch, int heads,
+                                    int dtype);
+int zo_paged_attention(const zo_kv_cache* cache, const zo_kv_batch* batch,
+                       int heads, int dtype, const void* Q, long long ldq,
+                       void* O, long long ldo, void* workspace,
+                       size_t ws_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -19,20 +19,24 @@ of include/zo.h); this package only binds it.  Entry points:
                            positions, SwiGLU MLP) with all seven matrices perturbed
     LlamaLoraLayer         the LoRA scheme's layer (grouped key/value heads, frozen
                            base, perturbed adapters on q and v)
+    kv_append, paged_attention
+                           answering with a tuned model: a layer's paged key/value cache
+                           (16-bit, or e4m3 with a scale per page and head), appended to with
+                           the rotation on the way, and the causal attention that reads it
     subspace_adam_update   subspace Adam and W <- W - lr U S V^T (Eqs. 6-10)
     subspace_sgd_update    plain subspace SGD, W <- W - lr U Zbar V^T
     sq_loss, combine_central, combine_forward   loss and estimate helpers (central
                            difference, or forward difference against a baseline block)
 """
-from ._lib import (ZO_BF16, ZO_EPI_NONE, ZO_EPI_RELU, ZO_EPI_RESIDUAL, ZO_EPI_SILU_MUL, ZO_F16, ZO_F32, ZO_MAX_BLOCKS,
+from ._lib import (ZO_BF16, ZO_E4M3, ZO_EPI_NONE, ZO_EPI_RELU, ZO_EPI_RESIDUAL, ZO_EPI_SILU_MUL, ZO_F16, ZO_F32, ZO_MAX_BLOCKS,
                    ZO_MAX_QR_RANK, ZO_MAX_RANK, ZO_NOALLOC_SCRATCH_BYTES, ABI_SYMBOLS, LIB_PATH, DecoderLayer, LlamaLayer,
                    LlamaLoraLayer, LoraPerturbedLinear, PerturbedLinear, Workspace, ZoError, abi_version, causal_attention, combine_central,
-                   combine_forward, layernorm, lib, lora_perturbed_linear, perturbed_linear, prepare_group, rmsnorm, rope,
+                   combine_forward, kv_append, layernorm, lib, lora_perturbed_linear, paged_attention, perturbed_linear, prepare_group, rmsnorm, rope,
                    sq_loss, subspace_adam_update, subspace_refresh, subspace_refresh_noalloc,
                    subspace_sgd_update)
 
-__all__ = ["ZO_BF16", "ZO_EPI_NONE", "ZO_EPI_RELU", "ZO_EPI_RESIDUAL", "ZO_EPI_SILU_MUL", "ZO_F16", "ZO_F32", "ZO_MAX_BLOCKS",
+__all__ = ["ZO_BF16", "ZO_E4M3", "ZO_EPI_NONE", "ZO_EPI_RELU", "ZO_EPI_RESIDUAL", "ZO_EPI_SILU_MUL", "ZO_F16", "ZO_F32", "ZO_MAX_BLOCKS",
            "ZO_MAX_QR_RANK", "ZO_MAX_RANK", "ZO_NOALLOC_SCRATCH_BYTES", "ABI_SYMBOLS", "LIB_PATH", "DecoderLayer", "LlamaLayer", "LlamaLoraLayer", "LoraPerturbedLinear",
            "PerturbedLinear", "Workspace", "ZoError", "abi_version", "causal_attention", "combine_central",
-           "combine_forward", "layernorm", "lib", "lora_perturbed_linear", "perturbed_linear", "prepare_group", "rmsnorm", "rope", "sq_loss",
+           "combine_forward", "kv_append", "layernorm", "lib", "lora_perturbed_linear", "paged_attention", "perturbed_linear", "prepare_group", "rmsnorm", "rope", "sq_loss",
            "subspace_adam_update", "subspace_refresh", "subspace_refresh_noalloc", "subspace_sgd_update"]

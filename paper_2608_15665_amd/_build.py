@@ -35,6 +35,7 @@ HIPCC_FLAGS = [
 # rescale (and leaves room for a third wave per SIMD).  The GEMMs elsewhere need the AGPRs.
 FILE_FLAGS = {
     "zo_decoder.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
+    "zo_paged.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
 }
 
 

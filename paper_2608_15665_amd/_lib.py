@@ -18,7 +18,7 @@ import torch
 _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "libzo.so")
 
-ZO_F32, ZO_BF16, ZO_F16 = 0, 1, 2
+ZO_F32, ZO_BF16, ZO_F16, ZO_E4M3 = 0, 1, 2, 3
 ZO_MAX_RANK = 128
 ZO_MAX_QR_RANK = 128
 ZO_MAX_BLOCKS = 256
@@ -41,6 +41,7 @@ ABI_SYMBOLS = (
     "zo_causal_attention_gqa", "zo_llama_lora_layer_workspace", "zo_llama_lora_layer_forward",
     "zo_perturbed_linear_group_workspace", "zo_perturbed_linear_prepare_group",
     "zo_subspace_refresh_noalloc",
+    "zo_kv_append", "zo_paged_attention_workspace", "zo_paged_attention",
 )
 ZO_NOALLOC_SCRATCH_BYTES = 64 << 20
 ZO_EPI_NONE, ZO_EPI_RELU, ZO_EPI_RESIDUAL, ZO_EPI_SILU_MUL = 0, 1, 2, 3
@@ -72,6 +73,18 @@ class LlamaLoraLayerDesc(ctypes.Structure):
     """zo_llama_lora_layer: adapted q and v, the frozen k, o, gate, up, down, the RMS gammas."""
     _fields_ = [("q", LoraMatrix), ("v", LoraMatrix)] + [
         (nm, ctypes.c_void_p) for nm in ("k", "o", "gate", "up", "down", "rms1_gamma", "rms2_gamma")]
+
+
+class KvCacheDesc(ctypes.Structure):
+    """zo_kv_cache: a layer's pool of key/value pages."""
+    _fields_ = [(nm, ctypes.c_int) for nm in ("num_pages", "page_size", "kv_heads", "dh", "dtype")] + [
+        (nm, ctypes.c_void_p) for nm in ("K", "V", "k_scale", "v_scale")]
+
+
+class KvBatchDesc(ctypes.Structure):
+    """zo_kv_batch: the sequences of a call."""
+    _fields_ = [(nm, ctypes.c_int) for nm in ("nseq", "rows", "max_q", "max_pages")] + [
+        (nm, ctypes.c_void_p) for nm in ("q_start", "kv_len", "page_table", "bad_flag")]
 
 
 class ZoError(RuntimeError):
@@ -204,6 +217,14 @@ def lib() -> ctypes.CDLL:
                                                                       c_f, c_int, c_vp, c_ll,
                                                                       ctypes.POINTER(LlamaLoraLayerDesc), c_vp, c_vp,
                                                                       c_sz, c_vp])
+            cache_p, batch_p = ctypes.POINTER(KvCacheDesc), ctypes.POINTER(KvBatchDesc)
+            L.zo_kv_append.restype = c_int
+            L.zo_kv_append.argtypes = [cache_p, batch_p, c_int, c_int, c_vp, c_ll, c_vp, c_ll, c_vp, c_ll, c_vp, c_ll,
+                                       c_f, c_vp]
+            L.zo_paged_attention_workspace.restype = c_sz
+            L.zo_paged_attention_workspace.argtypes = [cache_p, batch_p, c_int, c_int]
+            L.zo_paged_attention.restype = c_int
+            L.zo_paged_attention.argtypes = [cache_p, batch_p, c_int, c_int, c_vp, c_ll, c_vp, c_ll, c_vp, c_sz, c_vp]
             _lib = L
     return _lib
 
@@ -496,6 +517,126 @@ def causal_attention(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, nblk: in
     else:
         _check(lib().zo_causal_attention_gqa(nblk, T, seq_len, d, heads, kv_heads, _DT[Q.dtype], Q.data_ptr(),
                                              K.data_ptr(), V.data_ptr(), out.data_ptr(), _stream_handle()))
+    return out
+
+
+def _kv_args(name: str, rows: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, page_table: torch.Tensor,
+             kv_len: torch.Tensor, q_start: Optional[torch.Tensor], max_q: int, k_scale: Optional[torch.Tensor],
+             v_scale: Optional[torch.Tensor], bad_flag: Optional[torch.Tensor]):
+    """The checked cache and batch descriptors of a call whose row tensors are like `rows`."""
+    if k_cache.dim() != 4 or v_cache.shape != k_cache.shape:
+        raise ValueError("k_cache and v_cache must both be num_pages x kv_heads x page_size x dh")
+    pages, kv_heads, page_size, dh = k_cache.shape
+    dt = k_cache.dtype
+    e8 = dt == torch.float8_e4m3fn
+    if not e8 and dt != rows.dtype:
+        raise TypeError(f"{name}: a cache of {dt} with rows of {rows.dtype} (the same, or torch.float8_e4m3fn)")
+    here = torch.cuda.current_device()
+    for nm, t, want, numel in (("k_cache", k_cache, dt, None), ("v_cache", v_cache, dt, None),
+                               ("page_table", page_table, torch.int32, None), ("kv_len", kv_len, torch.int32, None),
+                               ("q_start", q_start, torch.int32, None), ("bad_flag", bad_flag, torch.int32, 1),
+                               ("k_scale", k_scale, torch.float32, pages * kv_heads),
+                               ("v_scale", v_scale, torch.float32, pages * kv_heads)):
+        if t is not None:
+            _need(t, nm, want, numel)
+            if t.device.index != here:
+                raise ValueError(f"{nm} must live on the current device cuda:{here} (got {t.device})")
+    if e8 != (k_scale is not None) or e8 != (v_scale is not None):
+        raise ValueError("k_scale and v_scale belong to an e4m3 cache, and only to one")
+    nseq = kv_len.numel()
+    if page_table.dim() != 2 or page_table.shape[0] != nseq:
+        raise ValueError(f"page_table must be nseq x max_pages, with nseq = {nseq} of kv_len")
+    if q_start is not None and q_start.numel() != nseq + 1:
+        raise ValueError(f"q_start must hold nseq + 1 = {nseq + 1} elements (got {q_start.numel()})")
+    return (KvCacheDesc(pages, page_size, kv_heads, dh, ZO_E4M3 if e8 else _DT.get(dt, -1), k_cache.data_ptr(),
+                        v_cache.data_ptr(), _ptr(k_scale), _ptr(v_scale)),
+            KvBatchDesc(nseq, rows.shape[0], int(max_q), page_table.shape[1], _ptr(q_start), kv_len.data_ptr(),
+                        page_table.data_ptr(), _ptr(bad_flag)))
+
+
+def _row_tensor(t: torch.Tensor, name: str, dtype, rows: int, cols: int) -> int:
+    """Checks a rows x cols tensor whose rows are dense (they may lie apart, as a column range of a wider
+    tensor's do) and returns the distance of its rows in elements."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if t.device.type != "cuda" or t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} must live on the current GPU (got {t.device})")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype} (got {t.dtype})")
+    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
+        raise ValueError(f"{name} must be {rows} x {cols} (got {tuple(t.shape)})")
+    if t.stride(1) != 1 and cols > 1:
+        raise ValueError(f"{name}'s rows must be dense")
+    return t.stride(0) if rows > 1 else max(t.stride(0), cols)
+
+
+def kv_append(K: torch.Tensor, V: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor,
+              page_table: torch.Tensor, kv_len: torch.Tensor, q_start: Optional[torch.Tensor] = None, max_q: int = 1,
+              Q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
+              rope_base: Optional[float] = None, k_scale: Optional[torch.Tensor] = None,
+              v_scale: Optional[torch.Tensor] = None, bad_flag: Optional[torch.Tensor] = None):
+    """Appends the rows of K and V (rows x kv_heads dh) to the paged cache (num_pages x kv_heads x page_size
+    x dh; the rows' type, or torch.float8_e4m3fn with k_scale and v_scale, num_pages x kv_heads), keys rotated
+    to their positions where rope_base is given.  kv_len counts the new rows.  With Q (rows x heads dh) also
+    returns the rotated queries (in q_out, or a new tensor).  See zo_kv_append."""
+    cache, batch = _kv_args("kv_append", K, k_cache, v_cache, page_table, kv_len, q_start, max_q, k_scale, v_scale,
+                            bad_flag)
+    rows, dt, dkv = K.shape[0], K.dtype, k_cache.shape[1] * k_cache.shape[3]
+    if dt not in _DT:
+        raise TypeError(f"unsupported dtype {dt}")
+    ldk, ldv = _row_tensor(K, "K", dt, rows, dkv), _row_tensor(V, "V", dt, rows, dkv)
+    ldq = ldqo = heads = 0
+    if Q is not None:
+        dq, dh = Q.shape[-1], k_cache.shape[3]
+        heads = dq // dh
+        if heads * dh != dq:
+            raise ValueError(f"Q must have a multiple of dh = {dh} columns (got {dq})")
+        ldq = _row_tensor(Q, "Q", dt, rows, dq)
+        if q_out is None:
+            q_out = torch.empty((rows, dq), dtype=dt, device=Q.device)
+        ldqo = _row_tensor(q_out, "q_out", dt, rows, dq)
+    elif q_out is not None:
+        raise ValueError("q_out without Q")
+    _check(lib().zo_kv_append(cache, batch, heads, _DT[dt], _ptr(Q), ldq, _ptr(q_out), ldqo, K.data_ptr(), ldk,
+                              V.data_ptr(), ldv, 0.0 if rope_base is None else float(rope_base), _stream_handle()))
+    return q_out
+
+
+def paged_attention(Q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, page_table: torch.Tensor,
+                    kv_len: torch.Tensor, q_start: Optional[torch.Tensor] = None, max_q: int = 1,
+                    k_scale: Optional[torch.Tensor] = None, v_scale: Optional[torch.Tensor] = None,
+                    out: Optional[torch.Tensor] = None, bad_flag: Optional[torch.Tensor] = None,
+                    workspace: Optional[torch.Tensor] = None):
+    """Causal attention of the new rows' queries Q (rows x heads dh) over the paged cache that kv_append fills
+    (which holds their own keys and values already).  Rows of `out` behind the last sequence are left as they
+    are.  The workspace is the stream's own, or under graph capture one of the graph's.  See
+    zo_paged_attention."""
+    cache, batch = _kv_args("paged_attention", Q, k_cache, v_cache, page_table, kv_len, q_start, max_q, k_scale,
+                            v_scale, bad_flag)
+    dt, dh = Q.dtype, k_cache.shape[3]
+    if dt not in _DT:
+        raise TypeError(f"unsupported dtype {dt}")
+    rows, dq = Q.shape[0], Q.shape[-1]
+    heads = dq // max(dh, 1)
+    if heads * dh != dq:
+        raise ValueError(f"Q must have a multiple of dh = {dh} columns (got {dq})")
+    ldq = _row_tensor(Q, "Q", dt, rows, dq)
+    if out is None:
+        out = torch.empty((rows, dq), dtype=dt, device=Q.device)
+    ldo = _row_tensor(out, "out", dt, rows, dq)
+    L = lib()
+    need = L.zo_paged_attention_workspace(cache, batch, heads, _DT[dt])
+    ws, ws_n = None, 0
+    if workspace is not None:
+        ws, ws_n = _need(workspace, "workspace", torch.uint8).data_ptr(), workspace.numel()
+    elif need:
+        # A graph that is replayed on another stream, or after the stream's buffer has grown, needs memory
+        # of its own.
+        buf = (torch.empty(need, dtype=torch.uint8, device=Q.device) if torch.cuda.is_current_stream_capturing()
+               else Workspace.get(need))
+        ws, ws_n = buf.data_ptr(), buf.numel()
+    _check(L.zo_paged_attention(cache, batch, heads, _DT[dt], Q.data_ptr(), ldq, out.data_ptr(), ldo, ws, ws_n,
+                                _stream_handle()))
     return out
 
 

@@ -989,4 +989,136 @@ int zo_combine_forward(int q, const double* L, float eps, float* g, void* stream
   return zo_combine_forward_launch(q, L, eps, g, (hipStream_t)stream);
 }
 
+// ------------------------------------------------------------------ paged key/value cache
+static int kv_args(const char* what, const zo_kv_cache* c, const zo_kv_batch* b, int heads, int dtype, KvArgs* a) {
+  ZO_CHECK(c && b, "%s: cache or batch is NULL", what);
+  ZO_CHECK(b->nseq >= 0 && b->rows >= 0 && b->max_q >= 0, "%s: nseq = %d, rows = %d, max_q = %d must be >= 0", what,
+           b->nseq, b->rows, b->max_q);
+  ZO_CHECK(b->rows <= (1 << 30), "%s: rows = %d too many", what, b->rows);
+  ZO_CHECK(b->max_pages >= 1 && c->num_pages >= 1 && c->kv_heads >= 1,
+           "%s: max_pages = %d, num_pages = %d, kv_heads = %d must be >= 1", what, b->max_pages, c->num_pages, c->kv_heads);
+  ZO_CHECK(heads >= 0 && heads <= (1 << 16) && c->kv_heads <= (1 << 16), "%s: heads = %d, kv_heads = %d out of range",
+           what, heads, c->kv_heads);
+  if (dtype != ZO_BF16 && dtype != ZO_F16) {
+    zo_set_error("%s: dtype %d unsupported (bf16 or fp16)", what, dtype);
+    return ZO_ERR_UNSUPPORTED;
+  }
+  if (c->dtype != dtype && c->dtype != ZO_E4M3) {
+    zo_set_error("%s: a cache of dtype %d with rows of dtype %d unsupported (the same, or e4m3)", what, c->dtype, dtype);
+    return ZO_ERR_UNSUPPORTED;
+  }
+  if (c->dh != 64 && c->dh != 128) {
+    zo_set_error("%s: head dim %d unsupported (64 or 128)", what, c->dh);
+    return ZO_ERR_UNSUPPORTED;
+  }
+  int log2ps = 4;
+  while (log2ps < 8 && (1 << log2ps) < c->page_size) ++log2ps;
+  if ((1 << log2ps) != c->page_size) {
+    zo_set_error("%s: page_size %d unsupported (16, 32, 64, 128 or 256)", what, c->page_size);
+    return ZO_ERR_UNSUPPORTED;
+  }
+  ZO_CHECK((long long)b->max_pages << log2ps <= 0x7fffffffLL - 4096, "%s: max_pages = %d of %d positions exceed 2^31", what,
+           b->max_pages, c->page_size);
+  ZO_CHECK(b->q_start || (b->rows >= b->nseq && (b->nseq == 0 || b->max_q >= 1)),
+           "%s: rows = %d, max_q = %d without q_start (need one row of each of the %d sequences)", what, b->rows, b->max_q,
+           b->nseq);
+  if (b->nseq > 0) {
+    ZO_CHECK(b->kv_len && b->page_table, "%s: kv_len or page_table is NULL", what);
+    ZO_CHECK(aligned(b->kv_len, 4) && aligned(b->page_table, 4) && aligned(b->q_start, 4) && aligned(b->bad_flag, 4),
+             "%s: kv_len, page_table, q_start, bad_flag must be 4-byte aligned", what);
+    ZO_CHECK(c->K && c->V && aligned(c->K, 16) && aligned(c->V, 16), "%s: the cache's K or V is NULL or not 16-byte aligned",
+             what);
+    ZO_CHECK(c->dtype != ZO_E4M3 || (c->k_scale && c->v_scale && aligned(c->k_scale, 4) && aligned(c->v_scale, 4)),
+             "%s: an e4m3 cache needs k_scale and v_scale, 4-byte aligned", what);
+  }
+  a->K = c->K;
+  a->V = c->V;
+  a->e8 = c->dtype == ZO_E4M3;
+  a->ks = a->e8 ? c->k_scale : nullptr;
+  a->vs = a->e8 ? c->v_scale : nullptr;
+  a->q_start = b->q_start;
+  a->kv_len = b->kv_len;
+  a->table = b->page_table;
+  a->bad_flag = b->bad_flag;
+  a->nseq = b->nseq;
+  a->rows = b->rows;
+  a->max_q = b->max_q < b->rows ? b->max_q : b->rows;
+  if (!b->q_start && a->max_q > 1) a->max_q = 1;
+  a->max_pages = b->max_pages;
+  a->num_pages = c->num_pages;
+  a->kv_heads = c->kv_heads;
+  a->dh = c->dh;
+  a->log2ps = log2ps;
+  a->heads = heads;
+  a->dtype = dtype;
+  return ZO_OK;
+}
+
+// A row tensor of `cols` columns: dense within a row, rows ld elements apart.
+static int check_rows(const char* what, const char* name, const void* p, long long ld, long long cols) {
+  ZO_CHECK(p && aligned(p, 16), "%s: %s is NULL or not 16-byte aligned", what, name);
+  ZO_CHECK(ld >= cols && ld % 8 == 0 && ld < (1LL << 31), "%s: rows of %s are %lld elements apart (need a multiple of 8, >= %lld)",
+           what, name, ld, cols);
+  return ZO_OK;
+}
+
+int zo_kv_append(const zo_kv_cache* cache, const zo_kv_batch* batch, int heads, int dtype, const void* Q, long long ldq,
+                 void* Q_out, long long ldqo, const void* K, long long ldk, const void* V, long long ldv,
+                 float rope_base, void* stream) {
+  const char* what = "kv_append";
+  KvArgs a;
+  int st = kv_args(what, cache, batch, Q ? heads : 0, dtype, &a);
+  if (st != ZO_OK) return st;
+  ZO_CHECK(rope_base == 0.f || (isfinite(rope_base) && rope_base > 1.f), "%s: rope_base must be 0 or finite and > 1", what);
+  ZO_CHECK(!Q == !Q_out, "%s: Q and Q_out go together", what);
+  ZO_CHECK(!Q || rope_base != 0.f, "%s: Q without a rotation", what);
+  ZO_CHECK(!Q || heads >= 1, "%s: heads = %d must be >= 1", what, heads);
+  if (a.nseq == 0 || a.max_q == 0) return ZO_OK;
+  const long long dkv = (long long)a.kv_heads * a.dh;
+  if ((st = check_rows(what, "K", K, ldk, dkv)) != ZO_OK || (st = check_rows(what, "V", V, ldv, dkv)) != ZO_OK) return st;
+  if (Q) {
+    const long long dq = (long long)heads * a.dh;
+    if ((st = check_rows(what, "Q", Q, ldq, dq)) != ZO_OK || (st = check_rows(what, "Q_out", Q_out, ldqo, dq)) != ZO_OK)
+      return st;
+    ZO_CHECK(Q != Q_out || ldq == ldqo, "%s: Q_out is Q, with another row distance", what);
+  }
+  return zo_kv_append_launch(a, Q, ldq, Q_out, ldqo, K, ldk, V, ldv, rope_base, (hipStream_t)stream);
+}
+
+static int check_paged(const zo_kv_cache* cache, const zo_kv_batch* batch, int heads, int dtype, KvArgs* a) {
+  int st = kv_args("paged_attention", cache, batch, heads, dtype, a);
+  if (st != ZO_OK) return st;
+  ZO_CHECK(heads >= 1 && heads % a->kv_heads == 0, "paged_attention: heads = %d not a multiple of kv_heads = %d", heads,
+           a->kv_heads);
+  return ZO_OK;
+}
+
+size_t zo_paged_attention_workspace(const zo_kv_cache* cache, const zo_kv_batch* batch, int heads, int dtype) {
+  KvArgs a;
+  if (check_paged(cache, batch, heads, dtype, &a) != ZO_OK || a.nseq == 0 || a.max_q == 0) return 0;
+  size_t need = 0;
+  zo_paged_attention_launch(a, nullptr, 0, nullptr, 0, nullptr, nullptr, &need);
+  return need;
+}
+
+int zo_paged_attention(const zo_kv_cache* cache, const zo_kv_batch* batch, int heads, int dtype, const void* Q,
+                       long long ldq, void* O, long long ldo, void* workspace, size_t ws_bytes, void* stream) {
+  const char* what = "paged_attention";
+  KvArgs a;
+  int st = check_paged(cache, batch, heads, dtype, &a);
+  if (st != ZO_OK) return st;
+  if (a.nseq == 0 || a.max_q == 0) return ZO_OK;
+  const long long dq = (long long)heads * a.dh;
+  if ((st = check_rows(what, "Q", Q, ldq, dq)) != ZO_OK || (st = check_rows(what, "O", O, ldo, dq)) != ZO_OK) return st;
+  ZO_CHECK(Q != O || ldq == ldo, "%s: O is Q, with another row distance", what);
+  size_t need = 0;
+  if ((st = zo_paged_attention_launch(a, nullptr, 0, nullptr, 0, nullptr, nullptr, &need)) != ZO_OK) return st;
+  if (need && (ws_bytes < need || !workspace)) {
+    zo_set_error("%s: workspace %zu bytes < required %zu", what, ws_bytes, need);
+    return ZO_ERR_WORKSPACE;
+  }
+  ZO_CHECK(!need || aligned(workspace, 256), "%s: workspace not 256-byte aligned", what);
+  return zo_paged_attention_launch(a, Q, ldq, O, ldo, workspace, (hipStream_t)stream, nullptr);
+}
+
 }  // extern "C"

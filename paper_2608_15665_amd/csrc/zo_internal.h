@@ -188,6 +188,22 @@ int zo_rope_launch(long long rows, int seq_len, int d, int heads, int dtype, voi
                    hipStream_t stream);
 int zo_attention_launch(int nblk, int T, int seq_len, int d, int heads, int kv_heads, int dtype,
                         const void* Q, const void* K, const void* V, void* O, hipStream_t stream);
+// Paged key/value cache (zo_kv.hip, zo_paged.hip): a checked call's cache and batch.
+struct KvArgs {
+  void *K, *V;        // num_pages x kv_heads x 2^log2ps x dh
+  float *ks, *vs;     // num_pages x kv_heads (8-bit caches), else nullptr
+  const int *q_start, *kv_len, *table;
+  int* bad_flag;
+  int nseq, rows, max_q, max_pages, num_pages, kv_heads, dh, log2ps;
+  int heads;
+  int dtype, e8;      // of the rows; whether the cache holds e4m3 codes
+};
+int zo_kv_append_launch(const KvArgs& a, const void* Q, long long ldq, void* Q_out, long long ldqo,
+                        const void* K, long long ldk, const void* V, long long ldv, float rope_base,
+                        hipStream_t stream);
+// ws_needed: only the workspace size is computed.
+int zo_paged_attention_launch(const KvArgs& a, const void* Q, long long ldq, void* O, long long ldo,
+                              void* ws, hipStream_t stream, size_t* ws_needed);
 int zo_plinear_apply(const PlinearPlan& p, const void* X, const void* W, void* Y, void* ws,
                      hipStream_t stream, int epi = ZO_EPI_NONE, const void* R = nullptr,
                      long long r_block_stride = 0);
