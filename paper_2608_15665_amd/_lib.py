@@ -235,7 +235,8 @@ def _check(status: int) -> None:
 
 
 def _stream_handle() -> int:
-    return torch.cuda.current_stream().cuda_stream
+    # The current stream's handle without the torch.cuda.Stream object around it (8 us of a 20 us call).
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
 
 
 def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
@@ -520,54 +521,75 @@ def causal_attention(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, nblk: in
     return out
 
 
-def _kv_args(name: str, rows: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, page_table: torch.Tensor,
+def _kv_tensor(t: torch.Tensor, name: str, dtype, here: int) -> int:
+    """The address of a dense tensor of the type on the current device `here` (a token's call takes some ten
+    such checks, next to a kernel of a few microseconds)."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if t.get_device() != here:
+        raise ValueError(f"{name} must live on the current device cuda:{here} (got {t.device})")
+    if t.dtype is not dtype:
+        raise TypeError(f"{name} must be {dtype} (got {t.dtype})")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t.data_ptr()
+
+
+def _kv_args(dt, rows: int, here: int, k_cache: torch.Tensor, v_cache: torch.Tensor, page_table: torch.Tensor,
              kv_len: torch.Tensor, q_start: Optional[torch.Tensor], max_q: int, k_scale: Optional[torch.Tensor],
              v_scale: Optional[torch.Tensor], bad_flag: Optional[torch.Tensor]):
-    """The checked cache and batch descriptors of a call whose row tensors are like `rows`."""
-    if k_cache.dim() != 4 or v_cache.shape != k_cache.shape:
+    """The checked cache and batch descriptors of a call with `rows` rows of type dt."""
+    shape = k_cache.shape
+    if len(shape) != 4 or v_cache.shape != shape:
         raise ValueError("k_cache and v_cache must both be num_pages x kv_heads x page_size x dh")
-    pages, kv_heads, page_size, dh = k_cache.shape
-    dt = k_cache.dtype
-    e8 = dt == torch.float8_e4m3fn
-    if not e8 and dt != rows.dtype:
-        raise TypeError(f"{name}: a cache of {dt} with rows of {rows.dtype} (the same, or torch.float8_e4m3fn)")
-    here = torch.cuda.current_device()
-    for nm, t, want, numel in (("k_cache", k_cache, dt, None), ("v_cache", v_cache, dt, None),
-                               ("page_table", page_table, torch.int32, None), ("kv_len", kv_len, torch.int32, None),
-                               ("q_start", q_start, torch.int32, None), ("bad_flag", bad_flag, torch.int32, 1),
-                               ("k_scale", k_scale, torch.float32, pages * kv_heads),
-                               ("v_scale", v_scale, torch.float32, pages * kv_heads)):
-        if t is not None:
-            _need(t, nm, want, numel)
-            if t.device.index != here:
-                raise ValueError(f"{nm} must live on the current device cuda:{here} (got {t.device})")
-    if e8 != (k_scale is not None) or e8 != (v_scale is not None):
-        raise ValueError("k_scale and v_scale belong to an e4m3 cache, and only to one")
+    pages, kv_heads, page_size, dh = shape
+    ct = k_cache.dtype
+    ks = vs = qs = flag = None
+    if ct is torch.float8_e4m3fn:
+        if k_scale is None or v_scale is None:
+            raise ValueError("an e4m3 cache needs k_scale and v_scale")
+        ks, vs = _kv_tensor(k_scale, "k_scale", torch.float32, here), _kv_tensor(v_scale, "v_scale", torch.float32, here)
+        if k_scale.numel() != pages * kv_heads or v_scale.numel() != pages * kv_heads:
+            raise ValueError(f"k_scale and v_scale must hold num_pages x kv_heads = {pages * kv_heads} elements")
+        code = ZO_E4M3
+    elif ct is not dt:
+        raise TypeError(f"a cache of {ct} with rows of {dt} (the same, or torch.float8_e4m3fn)")
+    elif k_scale is not None or v_scale is not None:
+        raise ValueError("k_scale and v_scale belong to an e4m3 cache")
+    else:
+        code = _DT[dt]
     nseq = kv_len.numel()
     if page_table.dim() != 2 or page_table.shape[0] != nseq:
         raise ValueError(f"page_table must be nseq x max_pages, with nseq = {nseq} of kv_len")
-    if q_start is not None and q_start.numel() != nseq + 1:
-        raise ValueError(f"q_start must hold nseq + 1 = {nseq + 1} elements (got {q_start.numel()})")
-    return (KvCacheDesc(pages, page_size, kv_heads, dh, ZO_E4M3 if e8 else _DT.get(dt, -1), k_cache.data_ptr(),
-                        v_cache.data_ptr(), _ptr(k_scale), _ptr(v_scale)),
-            KvBatchDesc(nseq, rows.shape[0], int(max_q), page_table.shape[1], _ptr(q_start), kv_len.data_ptr(),
-                        page_table.data_ptr(), _ptr(bad_flag)))
+    if q_start is not None:
+        qs = _kv_tensor(q_start, "q_start", torch.int32, here)
+        if q_start.numel() != nseq + 1:
+            raise ValueError(f"q_start must hold nseq + 1 = {nseq + 1} elements (got {q_start.numel()})")
+    if bad_flag is not None:
+        flag = _kv_tensor(bad_flag, "bad_flag", torch.int32, here)
+        if bad_flag.numel() != 1:
+            raise ValueError(f"bad_flag must hold one element (got {bad_flag.numel()})")
+    return (KvCacheDesc(pages, page_size, kv_heads, dh, code, _kv_tensor(k_cache, "k_cache", ct, here),
+                        _kv_tensor(v_cache, "v_cache", ct, here), ks, vs),
+            KvBatchDesc(nseq, rows, max_q, page_table.shape[1], qs, _kv_tensor(kv_len, "kv_len", torch.int32, here),
+                        _kv_tensor(page_table, "page_table", torch.int32, here), flag))
 
 
-def _row_tensor(t: torch.Tensor, name: str, dtype, rows: int, cols: int) -> int:
+def _row_tensor(t: torch.Tensor, name: str, dtype, rows: int, cols: int, here: int) -> int:
     """Checks a rows x cols tensor whose rows are dense (they may lie apart, as a column range of a wider
     tensor's do) and returns the distance of its rows in elements."""
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
-    if t.device.type != "cuda" or t.device.index != torch.cuda.current_device():
-        raise ValueError(f"{name} must live on the current GPU (got {t.device})")
-    if t.dtype != dtype:
+    if t.get_device() != here:
+        raise ValueError(f"{name} must live on the current device cuda:{here} (got {t.device})")
+    if t.dtype is not dtype:
         raise TypeError(f"{name} must be {dtype} (got {t.dtype})")
-    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
+    if t.shape != (rows, cols):
         raise ValueError(f"{name} must be {rows} x {cols} (got {tuple(t.shape)})")
-    if t.stride(1) != 1 and cols > 1:
+    ld, one = t.stride()
+    if one != 1 and cols > 1:
         raise ValueError(f"{name}'s rows must be dense")
-    return t.stride(0) if rows > 1 else max(t.stride(0), cols)
+    return ld if rows > 1 else max(ld, cols)  # one row has no distance
 
 
 def kv_append(K: torch.Tensor, V: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor,
@@ -579,22 +601,25 @@ def kv_append(K: torch.Tensor, V: torch.Tensor, k_cache: torch.Tensor, v_cache: 
     x dh; the rows' type, or torch.float8_e4m3fn with k_scale and v_scale, num_pages x kv_heads), keys rotated
     to their positions where rope_base is given.  kv_len counts the new rows.  With Q (rows x heads dh) also
     returns the rotated queries (in q_out, or a new tensor).  See zo_kv_append."""
-    cache, batch = _kv_args("kv_append", K, k_cache, v_cache, page_table, kv_len, q_start, max_q, k_scale, v_scale,
-                            bad_flag)
-    rows, dt, dkv = K.shape[0], K.dtype, k_cache.shape[1] * k_cache.shape[3]
+    dt, here = K.dtype, torch._C._cuda_getDevice()
     if dt not in _DT:
         raise TypeError(f"unsupported dtype {dt}")
-    ldk, ldv = _row_tensor(K, "K", dt, rows, dkv), _row_tensor(V, "V", dt, rows, dkv)
+    rows = K.shape[0]
+    cache, batch = _kv_args(dt, rows, here, k_cache, v_cache, page_table, kv_len, q_start, max_q, k_scale, v_scale,
+                            bad_flag)
+    dh = cache.dh
+    dkv = cache.kv_heads * dh
+    ldk, ldv = _row_tensor(K, "K", dt, rows, dkv, here), _row_tensor(V, "V", dt, rows, dkv, here)
     ldq = ldqo = heads = 0
     if Q is not None:
-        dq, dh = Q.shape[-1], k_cache.shape[3]
+        dq = Q.shape[-1]
         heads = dq // dh
         if heads * dh != dq:
             raise ValueError(f"Q must have a multiple of dh = {dh} columns (got {dq})")
-        ldq = _row_tensor(Q, "Q", dt, rows, dq)
+        ldq = _row_tensor(Q, "Q", dt, rows, dq, here)
         if q_out is None:
             q_out = torch.empty((rows, dq), dtype=dt, device=Q.device)
-        ldqo = _row_tensor(q_out, "q_out", dt, rows, dq)
+        ldqo = _row_tensor(q_out, "q_out", dt, rows, dq, here)
     elif q_out is not None:
         raise ValueError("q_out without Q")
     _check(lib().zo_kv_append(cache, batch, heads, _DT[dt], _ptr(Q), ldq, _ptr(q_out), ldqo, K.data_ptr(), ldk,
@@ -611,19 +636,20 @@ def paged_attention(Q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tenso
     (which holds their own keys and values already).  Rows of `out` behind the last sequence are left as they
     are.  The workspace is the stream's own, or under graph capture one of the graph's.  See
     zo_paged_attention."""
-    cache, batch = _kv_args("paged_attention", Q, k_cache, v_cache, page_table, kv_len, q_start, max_q, k_scale,
-                            v_scale, bad_flag)
-    dt, dh = Q.dtype, k_cache.shape[3]
+    dt, here = Q.dtype, torch._C._cuda_getDevice()
     if dt not in _DT:
         raise TypeError(f"unsupported dtype {dt}")
-    rows, dq = Q.shape[0], Q.shape[-1]
+    rows, dq = Q.shape
+    cache, batch = _kv_args(dt, rows, here, k_cache, v_cache, page_table, kv_len, q_start, max_q, k_scale, v_scale,
+                            bad_flag)
+    dh = cache.dh
     heads = dq // max(dh, 1)
     if heads * dh != dq:
         raise ValueError(f"Q must have a multiple of dh = {dh} columns (got {dq})")
-    ldq = _row_tensor(Q, "Q", dt, rows, dq)
+    ldq = _row_tensor(Q, "Q", dt, rows, dq, here)
     if out is None:
         out = torch.empty((rows, dq), dtype=dt, device=Q.device)
-    ldo = _row_tensor(out, "out", dt, rows, dq)
+    ldo = _row_tensor(out, "out", dt, rows, dq, here)
     L = lib()
     need = L.zo_paged_attention_workspace(cache, batch, heads, _DT[dt])
     ws, ws_n = None, 0
