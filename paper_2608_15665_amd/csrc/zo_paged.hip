@@ -45,6 +45,20 @@ __device__ __forceinline__ int splits_of(const PagedArgs& a, int keys) {
   return min(a.nsplit, max(1, (keys + a.min_keys - 1) / a.min_keys));
 }
 
+// The sequence that is i-th when every 64 consecutive ones are ordered by their lengths, the longest first:
+// workgroups start in that order, so that the long ones are not the last to end.
+__device__ __forceinline__ int by_length(const KvArgs& a, int i, int lane) {
+  const int s0 = i & ~63, n = min(64, a.nseq - s0);
+  const int len = lane < n ? a.kv_len[s0 + lane] : -0x7fffffff - 1;
+  int rank = 0;
+  for (int j = 0; j < n; ++j) {
+    const int other = __builtin_amdgcn_readlane(len, j);
+    rank += other > len || (other == len && j < lane);
+  }
+  const uint64_t hit = __ballot(lane < n && rank == (i & 63));
+  return s0 + __builtin_ctzll(hit);
+}
+
 // What a row tile covers: rows [row0, row0 + nrows) of its (sequence, K/V head), keys [0, kend).
 struct RowTile {
   KvSpan sp;
@@ -65,24 +79,38 @@ __device__ __forceinline__ RowTile row_tile(const PagedArgs& a, int s, int rt) {
   return t;
 }
 
-// The pages of 64 runs of 16 keys, one per lane, from run r0 on; -1 for runs from `rend` on and for bad
-// pages, which are not read: their keys and values (and scales) are 0.  `bad`: the first position of a
-// bad page.
+// Where 64 runs of 16 keys lie in K (and, in the same place, in V), one per lane, from run r0 on: bytes from
+// the cache's start.  Runs from `rend` on, and those of bad pages, lie in page 0, which exists: their keys are
+// masked (or their rows NaN) and their values cleared or, in a tile that is masked anyway, harmless; their
+// scales are 0.  Without a branch at the load, the loads of a tile stay in flight together.
+// `bad`: the first position of a bad page.
 template <bool E8>
-struct Pages {
-  int page;
+struct Runs {
+  uint32_t lo, hi;
   float ks, vs;
-  __device__ __forceinline__ void load(const PagedArgs& a, int s, int kvh, int r0, int rend, int lane, int& bad) {
-    const int r = r0 + lane;
-    page = -1;
-    if (r < rend) {
-      page = kv_page(a.kv, s, r >> (a.kv.log2ps - 4));
-      if (page < 0) bad = min(bad, r * 16);
+  __device__ __forceinline__ void load(const PagedArgs& a, int s, int kvh, int r0, int rend, int run_bytes, int lane, int& bad) {
+    const int r = r0 + lane, lr = a.kv.log2ps - 4;
+    int page = 0;
+    bool used = r < rend;
+    if (used) {
+      page = kv_page(a.kv, s, r >> lr);
+      if (page < 0) {
+        bad = min(bad, r * 16);
+        page = 0;
+        used = false;
+      }
     }
+    const size_t head = (size_t)page * a.kv.kv_heads + kvh;
+    const size_t at = ((head << lr) + (r & ((1 << lr) - 1))) * run_bytes;
+    lo = (uint32_t)at;
+    hi = (uint32_t)(at >> 32);
     if constexpr (E8) {
-      ks = page < 0 ? 0.f : a.kv.ks[(size_t)page * a.kv.kv_heads + kvh];
-      vs = page < 0 ? 0.f : a.kv.vs[(size_t)page * a.kv.kv_heads + kvh];
+      ks = used ? a.kv.ks[head] : 0.f;
+      vs = used ? a.kv.vs[head] : 0.f;
     }
+  }
+  __device__ __forceinline__ size_t at(int l) const {
+    return (size_t)(uint32_t)__builtin_amdgcn_readlane(lo, l) | ((size_t)(uint32_t)__builtin_amdgcn_readlane(hi, l) << 32);
   }
 };
 
@@ -115,6 +143,48 @@ __device__ __forceinline__ uint32_t odd_bits(u32x4 v) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) any |= (v[i] & M) + ONE;
   return any & (E8 ? 0x80808080u : 0x80008000u);
+}
+
+// A pair of 16-bit values with infinities and NaN as 0.
+template <bool F16>
+__device__ __forceinline__ uint32_t finite_pair(uint32_t x) {
+  const uint32_t t = ((x & (F16 ? 0x7c007c00u : 0x7f807f80u)) + (F16 ? 0x04000400u : 0x00800080u)) & 0x80008000u;
+  return x & ~((t - (t >> 15)) | t);
+}
+
+// V of a staged tile of `keys` keys is not finite somewhere.  0 times such a value is NaN, so a product with
+// P = 0 would take it to rows that do not see the key (and a hi + lo pair may meet an infinity with opposite
+// signs).  P V then runs on V without such values, and here they are added to the rows that do see them.
+// at(key, d): where values d .. d + 3 of a key lie.
+template <bool F16, bool E8, int DT, int NG, class At>
+__device__ __forceinline__ void add_odd_values(At at, int k0, int keys, int g, const int* pos, f32x4 (*o)[DT]) {
+#pragma unroll 1
+  for (int key = 0; key < keys; ++key)
+#pragma unroll
+    for (int d = 0; d < DT; ++d) {
+      u32x2 v;
+      if constexpr (E8) {
+        const u32x4 x = widen8<F16>(*(const uint32_t*)at(key, 16 * d + 4 * g), 0);
+        v = (u32x2){x[0], x[1]};
+      } else {
+        v = *(const u32x2*)at(key, 16 * d + 4 * g);
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float x = unpk<F16>(v[e >> 1], e & 1);
+#pragma unroll
+        for (int gq = 0; gq < NG; ++gq)
+          if (k0 + key <= pos[gq] && !(fabsf(x) < INFINITY)) o[gq][d][e] += x;
+      }
+    }
+}
+
+typedef int i32x2_t __attribute__((ext_vector_type(2)));
+// ds_read_b64_tr_b8: within each 16-lane group, lane i reads 8 bytes D[i][0..7] at its own address, and lane j
+// receives D[2 e + j / 8][j % 8] for e = 0..7.  With lanes 2 e and 2 e + 1 addressing the two halves of 16 columns
+// of row r_e, lane j thus receives column j of rows r_0 .. r_7.
+__device__ __forceinline__ u32x2 ds_read_tr8(const char* p) {
+  return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) i32x2_t*)p));
 }
 
 // A result o / l of a row at position p, from unnormalised sums: 0 where it has no keys, NaN where it
@@ -188,46 +258,57 @@ __global__ __launch_bounds__(64 * PG_W, 2) void k_paged_rows(PagedArgs a) {
   int bad = kv_cap(a.kv);
   uint16_t* const vs = (uint16_t*)lds + wave * PG_K * VROW;
   const int rend = (rtile.kend + 15) >> 4;
-  const size_t head_bytes = (size_t)DH * EB << a.kv.log2ps;
 
-  // The bytes of 16 keys (run r) of K or V.
-  auto run_at = [&](const void* base, int page, int r) {
-    return (const char*)base + ((size_t)page * a.kv.kv_heads + kvh) * head_bytes +
-           (size_t)(r & ((1 << (a.kv.log2ps - 4)) - 1)) * (16 * DH * EB);
-  };
-  Pages<E8> pg;
+  // The run window at hand (64 runs, the tiles from `have` on) and the one after it, on its way.
+  constexpr int WT = 64 / NT, RUN = 16 * DH * EB;
+  Runs<E8> pg, pgn;
   u32x4 kreg[NT][KV4], vreg[NT][KV4];
-  auto load_k = [&](int tile, int lane0) {
+  auto load_k = [&](int lane0) {
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-      const int page = __builtin_amdgcn_readlane(pg.page, lane0 + t);
-      const char* p = run_at(a.kv.K, page, NT * tile + t);
+      const char* p = (const char*)a.kv.K + pg.at(lane0 + t);
 #pragma unroll
-      for (int c = 0; c < KV4; ++c)
-        kreg[t][c] = page < 0 ? (u32x4){0, 0, 0, 0} : *(const u32x4*)(p + l16 * DH * EB + 16 * g + 64 * c);
+      for (int c = 0; c < KV4; ++c) kreg[t][c] = *(const u32x4*)(p + l16 * DH * EB + 16 * g + 64 * c);
     }
   };
-  auto load_v = [&](int tile, int lane0) {
+  auto load_v = [&](int lane0) {
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-      const int page = __builtin_amdgcn_readlane(pg.page, lane0 + t);
-      const char* p = run_at(a.kv.V, page, NT * tile + t);
+      const char* p = (const char*)a.kv.V + pg.at(lane0 + t);
 #pragma unroll
-      for (int c = 0; c < KV4; ++c)
-        vreg[t][c] = page < 0 ? (u32x4){0, 0, 0, 0} : *(const u32x4*)(p + 16 * lane + 1024 * c);
+      for (int c = 0; c < KV4; ++c) vreg[t][c] = *(const u32x4*)(p + 16 * lane + 1024 * c);
     }
   };
 
-  int have = t0;  // pg holds the runs of tiles have .. have + 64 / NT - 1
-  if (t0 + wave < t1) pg.load(a, s, kvh, NT * have, rend, lane, bad);
-  for (int tile = t0 + wave; tile < t1; tile += PG_W) {
-    if (tile >= have + 64 / NT) {
-      have += 64 / NT;
-      pg.load(a, s, kvh, NT * have, rend, lane, bad);
+  int have = t0;
+  float ksc[NT], vsc[NT];  // 8-bit: the scales of the tile at hand
+  auto scales = [&](int lane0) {
+    if constexpr (E8) {
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        ksc[t] = lane_f(pg.ks, lane0 + t);
+        vsc[t] = lane_f(pg.vs, lane0 + t);
+      }
     }
-    const int lane0 = NT * (tile - have);
-    load_k(tile, lane0);
-    load_v(tile, lane0);
+  };
+  if (t0 + wave < t1) {
+    pg.load(a, s, kvh, NT * have, rend, RUN, lane, bad);
+    pgn.load(a, s, kvh, NT * (have + WT), rend, RUN, lane, bad);
+    load_k(NT * wave);
+    load_v(NT * wave);
+  }
+  for (int tile = t0 + wave; tile < t1; tile += PG_W) {
+    scales(NT * (tile - have));
+    // The wave's next tile: its K is on its way from the end of this one's S on, its V from the store of this
+    // one's.
+    const int next = tile + PG_W;
+    const bool more = next < t1;
+    if (more && next >= have + WT) {
+      have += WT;
+      pg = pgn;
+      pgn.load(a, s, kvh, NT * (have + WT), rend, RUN, lane, bad);
+    }
+    const int lane0 = NT * (next - have);
     const int k0 = tile * PG_K;
     f32x4 st[NG][NT];
 #pragma unroll
@@ -247,11 +328,11 @@ __global__ __launch_bounds__(64 * PG_W, 2) void k_paged_rows(PagedArgs a) {
         for (int gq = 0; gq < NG; ++gq) st[gq][t] = mfma16<F16>(kf, qf[gq][kk], st[gq][t]);
       }
       if constexpr (E8) {
-        const float ks = lane_f(pg.ks, lane0 + t);
 #pragma unroll
-        for (int gq = 0; gq < NG; ++gq) st[gq][t] *= ks;
+        for (int gq = 0; gq < NG; ++gq) st[gq][t] *= ksc[t];
       }
     }
+    if (more) load_k(lane0);
     // Keys that a row does not see; those behind the sequence are also cleared from V, where they may be
     // NaN.
     const bool mask = k0 + PG_K > pfirst + 1;
@@ -282,6 +363,7 @@ __global__ __launch_bounds__(64 * PG_W, 2) void k_paged_rows(PagedArgs a) {
           *(u32x4*)dst = v;
         }
       }
+    if (more) load_v(lane0);
     // Online softmax: P = 2^((s - m) scale + SHIFT), the difference of the raw logits first, so that it
     // is exact near the maximum at any magnitude; m moves when a logit is more than 2^3 above it.
     bf16x8 bh[NT / 2][NG], bl[NT / 2][NG];
@@ -312,9 +394,8 @@ __global__ __launch_bounds__(64 * PG_W, 2) void k_paged_rows(PagedArgs a) {
           float q1 = __builtin_amdgcn_exp2f(fmaf(st[gq][t][i + 1] - mrow[gq], a.scale_log2, SHIFT));
           lsum[gq] += q0 + q1;
           if constexpr (E8) {
-            const float vsc = lane_f(pg.vs, lane0 + t);
-            q0 *= vsc;
-            q1 *= vsc;
+            q0 *= vsc[t];
+            q1 *= vsc[t];
           }
           const uint32_t h = cvt_pk<PF16>(q0, q1);
           hp[x] = h;
@@ -324,33 +405,8 @@ __global__ __launch_bounds__(64 * PG_W, 2) void k_paged_rows(PagedArgs a) {
         bl[c][gq] = __builtin_bit_cast(bf16x8, lp);
       }
     }
-    if (__builtin_expect(__ballot(odd != 0) != 0, 0)) {
-      // 0 times such a value is NaN, and hi and lo parts of P may have opposite signs: a row must not meet the
-      // keys that it does not see, not even with P = 0, nor an infinity twice.  The tile's keys one by one,
-      // in fp32.
-#pragma unroll
-      for (int gq = 0; gq < NG; ++gq)
-#pragma unroll
-        for (int x = 0; x < 4 * NT; ++x) {
-          const int t = x >> 2, i = x & 3;
-          const uint32_t hw = __builtin_bit_cast(u32x4, bh[t >> 1][gq])[2 * (t & 1) + (i >> 1)];
-          const uint32_t lw = __builtin_bit_cast(u32x4, bl[t >> 1][gq])[2 * (t & 1) + (i >> 1)];
-          const float pk = unpk<PF16>(hw, i & 1) + unpk<PF16>(lw, i & 1);
-          for (int gg = 0; gg < 4; ++gg) {
-            const float q = __shfl(pk, l16 + 16 * gg, 64);
-            const int key = 16 * t + 4 * gg + i;
-            if (k0 + key <= pos[gq]) {
-#pragma unroll
-              for (int d = 0; d < DT; ++d) {
-                const u32x2 v = *(const u32x2*)&vs[key * VROW + 16 * d + 4 * g];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) o[gq][d][e] = fmaf(q, unpk<PF16>(v[e >> 1], e & 1), o[gq][d][e]);
-              }
-            }
-          }
-        }
-      continue;
-    }
+    const bool clean = __builtin_expect(__ballot(odd != 0) != 0, 0);
+    if (clean) add_odd_values<PF16, false, DT, NG>([&](int key, int d) { return &vs[key * VROW + d]; }, k0, PG_K, g, pos, o);
     // Lane group g's k slots are keys 32 c + 4 g + (0..3) and 32 c + 16 + 4 g + (0..3).
 #pragma unroll
     for (int c = 0; c < NT / 2; ++c) {
@@ -358,7 +414,9 @@ __global__ __launch_bounds__(64 * PG_W, 2) void k_paged_rows(PagedArgs a) {
 #pragma unroll
       for (int t = 0; t < DT; ++t) {
         const u32x2 v0 = ds_read_tr(vb + 16 * t), v1 = ds_read_tr(vb + 16 * VROW + 16 * t);
-        const bf16x8 af = __builtin_bit_cast(bf16x8, (u32x4){v0[0], v0[1], v1[0], v1[1]});
+        u32x4 av = {v0[0], v0[1], v1[0], v1[1]};
+        if (clean) av = (u32x4){finite_pair<PF16>(av[0]), finite_pair<PF16>(av[1]), finite_pair<PF16>(av[2]), finite_pair<PF16>(av[3])};
+        const bf16x8 af = __builtin_bit_cast(bf16x8, av);
 #pragma unroll
         for (int gq = 0; gq < NG; ++gq) {
           o[gq][t] = mfma16<PF16>(af, bh[c][gq], o[gq][t]);
@@ -416,28 +474,430 @@ __global__ __launch_bounds__(64 * PG_W, 2) void k_paged_rows(PagedArgs a) {
   }
 }
 
-// Joins the splits of a row: O = sum 2^(m_i - m) O_i / sum 2^(m_i - m) l_i.  One workgroup per row; its
-// 256 / (DH / 4) teams take the splits in turn.
-template <bool F16, int DH>
+// ---------------------------------------------------------------- many rows
+constexpr int PT_NG = 2;                  // 16-row groups per wave
+constexpr int PT_Q = 16 * PT_NG * PG_W;   // rows per workgroup
+constexpr int PT_K = 64;                  // keys per tile
+constexpr int PT_AHEAD = 3;               // LDS reads of a phase that go out before its first MFMA
+constexpr int PT_VALU = 24;               // vector instructions per 16 rows and 16 keys, for the scheduler
+
+// A workgroup of 4 waves takes PT_Q rows and a range of the keys.  Tiles of K and V come as stored (8-bit
+// codes too) by direct global -> LDS loads, two of each: while tile n is worked on, V of tile n + 1 and K of
+// tile n + 2 land, K of n + 1 has landed, and one barrier a tile is enough.  Tile n + 1's S runs under tile
+// n's exponentials.  A row of RB bytes keeps its 16-byte chunk c at c ^ f(row): f_k spreads the 16 rows of a K
+// fragment over all banks, f_v those of a transposed read of V.
+// P enters its product rounded once to 16 bits: each weight is off by at most 2^-8 (bf16) or 2^-11 (fp16) of
+// itself, as the output is by its own rounding, and the errors of many weights average out; the low parts
+// would cost half as many MFMAs again.
+template <int RB, bool E8>
+__device__ __forceinline__ int f_k(int r) {
+  return RB == 256 ? r & 15 : RB == 128 ? (r >> 1) & 7 : (r >> 2) & 3;
+}
+template <int RB, bool E8>
+__device__ __forceinline__ int f_v(int r) {
+  if (E8) return RB == 128 ? ((r >> 1) & 3) | ((r >> 2) & 4) : ((r >> 2) & 1) | ((r >> 3) & 2);
+  return RB == 256 ? 2 * (r & 7) : 2 * ((r >> 1) & 3);
+}
+
+template <bool F16, bool E8, int DH>
+__global__ __launch_bounds__(64 * PG_W, 2) void k_paged_tile(PagedArgs a) {
+  constexpr int NTH = 64 * PG_W;
+  constexpr int KS = DH / 32, DT = DH / 16;
+  constexpr int EB = E8 ? 1 : 2, RB = DH * EB;  // bytes of a cached value, of a row
+  constexpr int CPR = RB / 16;                  // chunks of a row
+  constexpr int KCH = PT_K * CPR / NTH;         // loads per thread and tile
+  constexpr int TILE = PT_K * RB, RUN = 16 * RB;
+  constexpr bool PF16 = F16 && !E8;
+  constexpr float SHIFT = PF16 ? 12.f : 0.f;
+  constexpr int OROW = DH + 8;  // LDS row of the finished rows (16-bit elements)
+  static_assert(16 * OROW * 2 <= TILE, "16 finished rows of a wave fit a buffer");
+  // Four arrays, and steps that know at compile time which they use: the compiler then sees that a tile's reads
+  // do not meet the loads under way, and does not wait for those.
+  __shared__ __attribute__((aligned(1024))) char Kb0[TILE], Kb1[TILE], Vb0[TILE], Vb1[TILE];
+  __shared__ int bads[PG_W];
+
+  // Workgroups are dealt to the 8 XCDs in turn; each XCD gets a contiguous range, a part of the key heads of
+  // every sequence: the row tiles that read one sequence's keys share its L2, and sequences of different lengths
+  // load the XCDs alike.
+  int w = (int)(blockIdx.x & 7) * (int)(gridDim.x >> 3) + min((int)(blockIdx.x & 7), (int)(gridDim.x & 7)) +
+          (int)(blockIdx.x >> 3);
+  const int rt = a.tiles - 1 - w % a.tiles;  // the last rows see the most keys: they begin first
+  w /= a.tiles;
+  const int split = w % a.nsplit;
+  w /= a.nsplit;
+  const int s = by_length(a.kv, w % a.kv.nseq, threadIdx.x & 63), kvh = w / a.kv.nseq;
+  const RowTile rtile = row_tile(a, s, rt);
+  if (rtile.nrows <= 0) return;
+  const int nsp = splits_of(a, rtile.kend);
+  if (split >= nsp) return;
+  const int ntiles = (rtile.kend + PT_K - 1) / PT_K;
+  const int t0 = (int)((long long)ntiles * split / nsp), t1 = (int)((long long)ntiles * (split + 1) / nsp);
+  const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int p0 = rtile.sp.len - rtile.sp.n;
+  const int wr0 = 16 * PT_NG * wave;  // the wave's first row in the tile
+
+  // Rows as B operands of S^T, in the order of K's fragments (see k_paged_rows).
+  int pos[PT_NG];
+  bf16x8 qf[PT_NG][KS];
+#pragma unroll
+  for (int gq = 0; gq < PT_NG; ++gq) {
+    const int r = rtile.row0 + min(wr0 + 16 * gq + l16, rtile.nrows - 1);
+    const int tok = r / a.group;
+    pos[gq] = p0 + tok;
+    const uint16_t* qp = (const uint16_t*)a.Q + (size_t)(rtile.sp.r0 + tok) * a.ldq + (size_t)(kvh * a.group + r % a.group) * DH;
+#pragma unroll
+    for (int kk = 0; kk < KS; ++kk)
+      qf[gq][kk] = __builtin_bit_cast(bf16x8, *(const u32x4*)(qp + (E8 ? 16 * (g + 4 * (kk >> 1)) + 8 * (kk & 1) : 32 * kk + 8 * g)));
+  }
+  // Positions of the wave's first and last row.
+  const int wfirst = p0 + (rtile.row0 + min(wr0, rtile.nrows - 1)) / a.group;
+  const int wlast = wr0 < rtile.nrows ? p0 + (rtile.row0 + min(wr0 + 16 * PT_NG, rtile.nrows) - 1) / a.group : -1;
+
+  f32x4 o[PT_NG][DT];
+  float mrow[PT_NG], lsum[PT_NG];
+#pragma unroll
+  for (int gq = 0; gq < PT_NG; ++gq) {
+#pragma unroll
+    for (int t = 0; t < DT; ++t) o[gq][t] = (f32x4){0.f, 0.f, 0.f, 0.f};
+    mrow[gq] = PG_LOW;
+    lsum[gq] = 0.f;
+  }
+  int bad = kv_cap(a.kv);
+  const int rend = (rtile.kend + 15) >> 4;
+
+  // Load c of this wave fills 64 chunks of LDS, x = NTH c + tid: row x / CPR, place x % CPR; they lie in one run of
+  // 16 keys.  pg: the runs of tiles 16 win .. 16 win + 15, pgn those of the next 16.  K of a tile is loaded one
+  // tile before V, which lies in the same place of its tensor.
+  const int row0 = tid / CPR;  // of load 0; f does not depend on c
+  const unsigned offk = (unsigned)((row0 & 15) * RB + 16 * ((tid % CPR) ^ f_k<RB, E8>(row0)));
+  const unsigned offv = (unsigned)((row0 & 15) * RB + 16 * ((tid % CPR) ^ f_v<RB, E8>(row0)));
+  Runs<E8> pg, pgn;
+  float ksp = 0.f, vsp = 0.f;  // 8-bit: the scales of the window before pg's
+  int win = t0 >> 4;
+  auto dma = [&](const void* base, int tile, unsigned off, char* dst) {
+#pragma unroll
+    for (int c = 0; c < KCH; ++c) {
+      const char* at = (const char*)base + pg.at(4 * (tile & 15) + (NTH * c + 64 * wave) / CPR / 16);
+      const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void*)at, (short)0, RUN, 0x00020000);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_ptr_t)(dst + (NTH * c + 64 * wave) * 16), 16, off, 0, 0, 0);
+    }
+  };
+  auto load_k = [&](int tile, char* dst) {
+    if ((tile >> 4) != win) {
+      win = tile >> 4;
+      if constexpr (E8) {
+        ksp = pg.ks;
+        vsp = pg.vs;
+      }
+      pg = pgn;
+      pgn.load(a, s, kvh, 64 * (win + 1), rend, RUN, lane, bad);
+    }
+    dma(a.kv.K, tile, offk, dst);
+  };
+  // V of the tile whose K was loaded last.
+  auto load_v = [&](int tile, char* dst) { dma(a.kv.V, tile, offv, dst); };
+  // Everything that this wave loads has landed; with the barrier, that of all waves.
+  auto landed = [&]() {
+    __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
+    __syncthreads();
+  };
+
+  // Where this lane reads: fragment kk (8 bits: pair of fragments) of K's row 16 t + l16 at (kat ^ 64 kk) + 16 RB t,
+  // V's column 16 t of rows 32 c + .. at (vat0 ^ 16 EB t) + 32 RB c (f does not depend on t or c, and the chunk
+  // numbers' bits are apart, so that their XOR is one of addresses).
+  const unsigned kat = (unsigned)(l16 * RB + 16 * (g ^ f_k<RB, E8>(l16)));
+  const int vrow = 4 * g + (E8 ? ((l16 >> 1) & 3) + 16 * (l16 >> 3) : l16 >> 2);
+  const unsigned vat0 = (unsigned)(vrow * RB + 16 * ((E8 ? 0 : (l16 >> 1) & 1) ^ f_v<RB, E8>(vrow)) + 8 * (l16 & 1));
+  // S^T of 16 keys (subtile t of the K tile whose reads start at `at`).
+  auto qk = [&](const char* kb, unsigned at, int t, f32x4 (*st)[4]) {
+#pragma unroll
+    for (int gq = 0; gq < PT_NG; ++gq) st[gq][t] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int kk = 0; kk < KS; kk += E8 ? 2 : 1) {
+      const char* p = kb + (at ^ (E8 ? 32 * kk : 64 * kk)) + 16 * RB * t;
+      if constexpr (E8) {
+        const u32x4 x = *(const u32x4*)p;
+        const bf16x8 k0 = __builtin_bit_cast(bf16x8, widen8<F16>(x[0], x[1])), k1 = __builtin_bit_cast(bf16x8, widen8<F16>(x[2], x[3]));
+#pragma unroll
+        for (int gq = 0; gq < PT_NG; ++gq) {
+          st[gq][t] = mfma16<F16>(k0, qf[gq][kk], st[gq][t]);
+          st[gq][t] = mfma16<F16>(k1, qf[gq][kk + 1], st[gq][t]);
+        }
+      } else {
+        const bf16x8 kf = *(const bf16x8*)p;
+#pragma unroll
+        for (int gq = 0; gq < PT_NG; ++gq) st[gq][t] = mfma16<F16>(kf, qf[gq][kk], st[gq][t]);
+      }
+    }
+  };
+  // Opaque, so that the addresses made from it are formed where they are used and not kept in registers
+  // through the loop.
+  auto opaque = [&](unsigned x) {
+    asm volatile("" : "+v"(x));
+    return x;
+  };
+  // One tile: its softmax and P V from V's buffer vt, st being its S.  NEXT: also the next tile's S (into sn,
+  // from K's buffer kb); such a tile lies wholly before the workgroup's rows.
+  auto tile = [&](auto NEXT, int n, const char* vt, const char* kb, f32x4 (*st)[4], f32x4 (*sn)[4]) {
+    constexpr bool next = decltype(NEXT)::value;
+    const unsigned kn = opaque(kat), vn = opaque(vat0);
+    const int k0 = PT_K * n;
+    float vsc[4];
+    if constexpr (E8) {
+      const float kw = (n >> 4) == win ? pg.ks : ksp, vw = (n >> 4) == win ? pg.vs : vsp;
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        const float ksc = lane_f(kw, 4 * (n & 15) + t);
+        vsc[t] = lane_f(vw, 4 * (n & 15) + t);
+#pragma unroll
+        for (int gq = 0; gq < PT_NG; ++gq) st[gq][t] *= ksc;
+      }
+    }
+    bool clean = false;  // V of the tile is not finite, and rows see only a part of it
+    if (!next && k0 + PT_K > wfirst + 1) {
+#pragma unroll
+      for (int gq = 0; gq < PT_NG; ++gq)
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (k0 + 16 * t + 4 * g + i > pos[gq]) st[gq][t][i] = -INFINITY;
+      uint32_t odd = 0;
+#pragma unroll 4
+      for (int x = 0; x < TILE / 1024; ++x) odd |= odd_bits<PF16, E8>(*(const u32x4*)(vt + 1024 * x + 16 * lane));
+      clean = __ballot(odd != 0) != 0;
+    }
+#pragma unroll
+    for (int gq = 0; gq < PT_NG; ++gq) {
+      float tmax = -INFINITY;
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) tmax = fmaxf(tmax, st[gq][t][i]);
+      tmax = max_groups(tmax);
+      const float m = mrow[gq];
+      if (__builtin_expect(__ballot((tmax - m) * a.scale_log2 > 3.f) != 0, 0)) {
+        const float mnew = fmaxf(m, tmax);
+        const float alpha = __builtin_amdgcn_exp2f((m - mnew) * a.scale_log2);
+        mrow[gq] = mnew;
+        lsum[gq] *= alpha;
+#pragma unroll
+        for (int t = 0; t < DT; ++t) o[gq][t] *= alpha;
+      }
+    }
+    bf16x8 bh[2][PT_NG];
+    auto probs = [&](int c) {
+#pragma unroll
+      for (int gq = 0; gq < PT_NG; ++gq) {
+        u32x4 hp;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          const int t = 2 * c + (x >> 1), i = 2 * (x & 1);
+          float q0 = __builtin_amdgcn_exp2f(fmaf(st[gq][t][i] - mrow[gq], a.scale_log2, SHIFT));
+          float q1 = __builtin_amdgcn_exp2f(fmaf(st[gq][t][i + 1] - mrow[gq], a.scale_log2, SHIFT));
+          lsum[gq] += q0 + q1;
+          if constexpr (E8) {
+            q0 *= vsc[t];
+            q1 *= vsc[t];
+          }
+          hp[x] = cvt_pk<PF16>(q0, q1);
+        }
+        bh[c][gq] = __builtin_bit_cast(bf16x8, hp);
+      }
+    };
+    // O^T += V^T P^T over keys 32 c ..: lane group g's k slots are keys 32 c + 4 g + (0..3) and
+    // 32 c + 16 + 4 g + (0..3), transposed reads give V's column 16 t + l16 of those.
+    auto pv = [&](int c, auto CLEAN) {
+#pragma unroll
+      for (int t = 0; t < DT; ++t) {
+        u32x4 av;
+        const char* p = vt + (vn ^ (16 * EB * t)) + 32 * RB * c;
+        if constexpr (E8) {
+          const u32x2 v = ds_read_tr8(p);
+          av = widen8<false>(v[0], v[1]);
+        } else {
+          const u32x2 v0 = ds_read_tr((const uint16_t*)p), v1 = ds_read_tr((const uint16_t*)(p + 16 * RB));
+          av = (u32x4){v0[0], v0[1], v1[0], v1[1]};
+        }
+        if constexpr (decltype(CLEAN)::value)
+          av = (u32x4){finite_pair<PF16>(av[0]), finite_pair<PF16>(av[1]), finite_pair<PF16>(av[2]), finite_pair<PF16>(av[3])};
+        const bf16x8 af = __builtin_bit_cast(bf16x8, av);
+#pragma unroll
+        for (int gq = 0; gq < PT_NG; ++gq) o[gq][t] = mfma16<PF16>(af, bh[c][gq], o[gq][t]);
+      }
+    };
+    // The first reads of a phase go out together; each later one while the MFMAs of an earlier one run.
+    constexpr int KR = E8 ? 2 * KS : 4 * KS, KM = 4 * KS * PT_NG / KR;   // K reads, MFMAs of each
+    constexpr int VR = E8 ? 1 : 2;                                       // V reads of a fragment
+    __builtin_amdgcn_sched_barrier(0);
+    if constexpr (next) {
+#pragma unroll
+      for (int t = 0; t < 4; ++t) qk(kb, kn, t, sn);
+    }
+    probs(0);
+    if constexpr (next) {
+      __builtin_amdgcn_sched_group_barrier(0x100, PT_AHEAD, 0);
+#pragma unroll
+      for (int x = 0; x < KR; ++x) {
+        __builtin_amdgcn_sched_group_barrier(0x002, 4 * PT_VALU / KR, 0);
+        __builtin_amdgcn_sched_group_barrier(0x008, KM, 0);
+        if (x + PT_AHEAD < KR) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    if constexpr (!next) {
+      if (__builtin_expect(clean, 0)) {
+        probs(1);
+        pv(0, std::true_type{});
+        pv(1, std::true_type{});
+        add_odd_values<PF16, E8, DT, PT_NG>([&](int key, int d) { return vt + key * RB + 16 * ((d * EB / 16) ^ f_v<RB, E8>(key)) + (d * EB) % 16; },
+                                            k0, PT_K, g, pos, o);
+        return;
+      }
+    }
+    pv(0, std::false_type{});
+    probs(1);
+    __builtin_amdgcn_sched_group_barrier(0x100, VR * PT_AHEAD, 1);
+#pragma unroll
+    for (int x = 0; x < DT; ++x) {
+      __builtin_amdgcn_sched_group_barrier(0x002, 4 * PT_VALU / DT, 1);
+      __builtin_amdgcn_sched_group_barrier(0x008, PT_NG, 1);
+      if (x + PT_AHEAD < DT) __builtin_amdgcn_sched_group_barrier(0x100, VR, 1);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    pv(1, std::false_type{});
+    __builtin_amdgcn_sched_group_barrier(0x100, VR * PT_AHEAD, 2);
+#pragma unroll
+    for (int x = 0; x < DT; ++x) {
+      __builtin_amdgcn_sched_group_barrier(0x008, PT_NG, 2);
+      if (x + PT_AHEAD < DT) __builtin_amdgcn_sched_group_barrier(0x100, VR, 2);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  };
+
+  // Tiles t0 .. tfull - 1 lie wholly before all rows of the workgroup: they overlap with the next one's S.  The
+  // last few, which are masked, do not.
+  const int tfull = min(t1, (p0 + rtile.row0 / a.group + 1) / PT_K);
+  int n = t0;
+  if (n < t1) {
+    pg.load(a, s, kvh, 64 * win, rend, RUN, lane, bad);
+    pgn.load(a, s, kvh, 64 * (win + 1), rend, RUN, lane, bad);
+    load_k(n, Kb0);
+    load_v(n, Vb0);
+    if (n + 1 < t1) load_k(n + 1, Kb1);
+  }
+  // A whole tile with K and V in buffers k0 / v0, the next in k1 / v1.  At its top K(n + 1) and V(n) have landed,
+  // and every wave is done with K(n) and V(n - 1).
+  auto whole = [&](char* k0, char* v0, char* k1, char* v1, f32x4 (*st)[4], f32x4 (*sn)[4]) {
+    landed();
+    if (n + 1 < t1) load_v(n + 1, v1);
+    if (n + 2 < t1) load_k(n + 2, k0);
+    tile(std::true_type{}, n, v0, k1, st, sn);
+    ++n;
+  };
+  // A tile that is masked, or beyond the rows of some waves: S(n) is formed first, and K(n)'s buffer is not
+  // written until every wave has it.
+  auto part = [&](char* k0, char* v0, char* v1) {
+    landed();
+    if (n + 1 < t1) load_v(n + 1, v1);
+    f32x4 st[PT_NG][4];
+    const bool mine = PT_K * n <= wlast;  // else every key of the tile is after the wave's rows
+    if (mine) {
+#pragma unroll
+      for (int t = 0; t < 4; ++t) qk(k0, kat, t, st);
+    }
+    __syncthreads();
+    if (n + 2 < t1) load_k(n + 2, k0);
+    if (mine) tile(std::false_type{}, n, v0, k0, st, st);
+    ++n;
+  };
+  if (n < tfull) {
+    f32x4 sa[PT_NG][4], sb[PT_NG][4];
+    landed();
+#pragma unroll
+    for (int t = 0; t < 4; ++t) qk(Kb0, kat, t, sa);
+    for (;;) {
+      whole(Kb0, Vb0, Kb1, Vb1, sa, sb);
+      if (n >= tfull) break;
+      whole(Kb1, Vb1, Kb0, Vb0, sb, sa);
+      if (n >= tfull) break;
+    }
+  }
+  if (n < t1 && ((n - t0) & 1)) part(Kb1, Vb1, Vb0);
+  while (n < t1) {
+    part(Kb0, Vb0, Vb1);
+    if (n < t1) part(Kb1, Vb1, Vb0);
+  }
+
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) bad = min(bad, __shfl_xor(bad, off, 64));
+  if (lane == 0) bads[wave] = bad;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < PG_W; ++i) bad = min(bad, bads[i]);
+  if (bad < kv_cap(a.kv) && tid == 0 && a.kv.bad_flag) *a.kv.bad_flag = 1;
+  // The rows: normalised, 16 at a time through a buffer of the wave, so that a store covers whole rows; or a
+  // split's unnormalised sums.
+  uint16_t* const ow = (uint16_t*)(wave == 0 ? Kb0 : wave == 1 ? Kb1 : wave == 2 ? Vb0 : Vb1);
+#pragma unroll
+  for (int gq = 0; gq < PT_NG; ++gq) {
+    float l = lsum[gq] + __shfl_xor(lsum[gq], 16, 64);
+    l += __shfl_xor(l, 32, 64);
+    const int row = wr0 + 16 * gq + l16;
+    if (nsp > 1) {
+      if (row >= rtile.nrows) continue;
+      const size_t at = ((((size_t)s * a.kv.kv_heads + kvh) * a.tiles + rt) * a.nsplit + split) * a.prows + row;
+#pragma unroll
+      for (int t = 0; t < DT; ++t) *(f32x4*)&a.part[at * DH + 16 * t + 4 * g] = o[gq][t];
+      if (g == 0) a.stat[at] = make_float2(mrow[gq], pos[gq] >= bad ? __builtin_nanf("") : l);
+      continue;
+    }
+    const float inv = 1.f / l;
+#pragma unroll
+    for (int t = 0; t < DT; ++t) {
+      float y[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[e] = row_result(o[gq][t][e], inv, pos[gq], bad);
+      store4<F16>(&ow[l16 * OROW + 16 * t + 4 * g], y);
+    }
+    constexpr int C8 = DH / 8;
+#pragma unroll
+    for (int x = lane; x < 16 * C8; x += 64) {
+      const int rr = wr0 + 16 * gq + x / C8, c = x % C8, r = rtile.row0 + rr;
+      const u32x4 v = *(const u32x4*)&ow[(x / C8) * OROW + 8 * c];
+      if (rr < rtile.nrows)
+        *(u32x4*)((uint16_t*)a.O + (size_t)(rtile.sp.r0 + r / a.group) * a.ldo + (size_t)(kvh * a.group + r % a.group) * DH + 8 * c) = v;
+    }
+  }
+}
+
+// ---------------------------------------------------------------- splits
+// Joins the splits of a row: O = sum 2^(m_i - m) O_i / sum 2^(m_i - m) l_i.  TPR teams of DH / 4 lanes share a
+// row and take its splits in turn: one team where a workgroup has rows enough, all of them for many splits
+// of few rows.
+template <bool F16, int DH, int TPR>
 __global__ __launch_bounds__(256) void k_paged_join(PagedArgs a) {
-  constexpr int D4 = DH / 4, TEAMS = 256 / D4;
-  __shared__ f32x4 acc[TEAMS][D4];
-  __shared__ float2 st[TEAMS];
+  constexpr int D4 = DH / 4, TEAMS = 256 / D4, RPW = TEAMS / TPR;
+  __shared__ f32x4 acc[TPR > 1 ? TEAMS : 1][D4];
+  __shared__ float2 st[TPR > 1 ? TEAMS : 1];
+  const int per = (a.prows + RPW - 1) / RPW;  // workgroups of a row tile
+  const int team = threadIdx.x / D4, lane = threadIdx.x % D4, d = 4 * lane;
   int w = blockIdx.x;
-  const int row = w % a.prows;
-  w /= a.prows;
+  const int row = (w % per) * RPW + team / TPR;
+  w /= per;
   const int rt = w % a.tiles;
   w /= a.tiles;
   const int kvh = w % a.kv.kv_heads, s = w / a.kv.kv_heads;
   const RowTile rtile = row_tile(a, s, rt);
-  if (row >= rtile.nrows) return;
   const int nsp = splits_of(a, rtile.kend);
   if (nsp == 1) return;  // written already
-  const int team = threadIdx.x / D4, d = 4 * (threadIdx.x % D4);
+  const bool mine = row < rtile.nrows;
+  if (TPR == 1 && !mine) return;
   const size_t base = (((size_t)s * a.kv.kv_heads + kvh) * a.tiles + rt) * a.nsplit;
   float m = PG_LOW, l = 0.f;
   f32x4 y = {0.f, 0.f, 0.f, 0.f};
-  for (int i = team; i < nsp; i += TEAMS) {
+  for (int i = team % TPR; i < nsp && mine; i += TPR) {
     const size_t at = (base + i) * a.prows + row;
     const float2 ml = a.stat[at];
     const f32x4 v = *(const f32x4*)&a.part[at * DH + d];
@@ -448,26 +908,30 @@ __global__ __launch_bounds__(256) void k_paged_join(PagedArgs a) {
     for (int e = 0; e < 4; ++e) y[e] = y[e] * f + v[e] * h;
     m = mn;
   }
-  acc[team][threadIdx.x % D4] = y;
-  if (d == 0) st[team] = make_float2(m, l);
-  __syncthreads();
-  if (team) return;
-  float mx = PG_LOW;
+  if constexpr (TPR > 1) {
+    acc[team][lane] = y;
+    if (lane == 0) st[team] = make_float2(m, l);
+    __syncthreads();
+    if (team % TPR || !mine) return;
+    m = PG_LOW;
 #pragma unroll
-  for (int i = 0; i < TEAMS; ++i) mx = fmaxf(mx, st[i].x);
-  float o[4] = {0.f, 0.f, 0.f, 0.f};
-  l = 0.f;
+    for (int i = 0; i < TPR; ++i) m = fmaxf(m, st[team + i].x);
+    l = 0.f;
+    y = (f32x4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-  for (int i = 0; i < TEAMS; ++i) {
-    const float f = __builtin_amdgcn_exp2f((st[i].x - mx) * a.scale_log2);
-    l += f * st[i].y;
+    for (int i = 0; i < TPR; ++i) {
+      const float f = __builtin_amdgcn_exp2f((st[team + i].x - m) * a.scale_log2);
+      const f32x4 v = acc[team + i][lane];
+      l += f * st[team + i].y;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) o[e] += f * acc[i][threadIdx.x][e];
+      for (int e = 0; e < 4; ++e) y[e] += f * v[e];
+    }
   }
   const int r = rtile.row0 + row, tok = r / a.group, p = rtile.sp.len - rtile.sp.n + tok;
   const float inv = 1.f / l;
+  float o[4];
 #pragma unroll
-  for (int e = 0; e < 4; ++e) o[e] = row_result(o[e], inv, p, 0x7fffffff);
+  for (int e = 0; e < 4; ++e) o[e] = row_result(y[e], inv, p, 0x7fffffff);
   store4<F16>((uint16_t*)a.O + (size_t)(rtile.sp.r0 + tok) * a.ldo + (size_t)(kvh * a.group + r % a.group) * DH + d, o);
 }
 
@@ -483,16 +947,19 @@ int zo_paged_attention_launch(const KvArgs& kv, const void* Q, long long ldq, vo
   a.ldo = ldo;
   a.group = kv.heads / kv.kv_heads;
   a.scale_log2 = 1.4426950408889634f / sqrtf((float)kv.dh);
-  a.rt_rows = 16;
   const long long all_rows = (long long)kv.max_q * a.group;
+  // Up to 32 rows a sequence and key head read the keys once and little else; more share staged tiles.
+  const bool many = all_rows > 32;
+  const int ng = all_rows > 16 ? 2 : 1;
+  a.rt_rows = many ? PT_Q : 16 * ng;
   a.prows = (int)(all_rows < a.rt_rows ? all_rows : a.rt_rows);
   const long long tiles = (all_rows + a.rt_rows - 1) / a.rt_rows;
   const long long units = (long long)kv.nseq * kv.kv_heads * tiles;
   const long long keys = (long long)kv.max_pages << kv.log2ps;
   a.min_keys = 256;
   const long long most = (keys + a.min_keys - 1) / a.min_keys;
-  long long split = 1024 / units;
-  if (split < (keys + 2047) / 2048) split = (keys + 2047) / 2048;
+  long long split = (many ? 512 : 1024) / units;
+  if (!many && split < (keys + 2047) / 2048) split = (keys + 2047) / 2048;
   if (split > 64) split = 64;
   if (split > most) split = most;
   if (split < 1) split = 1;
@@ -512,10 +979,13 @@ int zo_paged_attention_launch(const KvArgs& kv, const void* Q, long long ldq, vo
   }
   const dim3 grid((unsigned)(units * split)), block(64 * PG_W);
   const bool f16 = kv.dtype == ZO_F16;
-#define ZO_ROWS(F, E, D) hipLaunchKernelGGL((k_paged_rows<F, E, D, 1>), grid, block, 0, stream, a)
+#define ZO_ROWS(F, E, D)                                                                          \
+  if (many) hipLaunchKernelGGL((k_paged_tile<F, E, D>), grid, block, 0, stream, a);              \
+  else if (ng == 2) hipLaunchKernelGGL((k_paged_rows<F, E, D, 2>), grid, block, 0, stream, a);   \
+  else hipLaunchKernelGGL((k_paged_rows<F, E, D, 1>), grid, block, 0, stream, a)
 #define ZO_ROWS_D(F, E) \
-  if (kv.dh == 64) ZO_ROWS(F, E, 64); \
-  else ZO_ROWS(F, E, 128)
+  if (kv.dh == 64) { ZO_ROWS(F, E, 64); } \
+  else { ZO_ROWS(F, E, 128); }
   if (kv.e8) {
     if (f16) { ZO_ROWS_D(true, true); } else { ZO_ROWS_D(false, true); }
   } else {
@@ -523,15 +993,20 @@ int zo_paged_attention_launch(const KvArgs& kv, const void* Q, long long ldq, vo
   }
 #undef ZO_ROWS_D
 #undef ZO_ROWS
-  int st = zo_hip_status(hipGetLastError(), "k_paged_rows");
+  int st = zo_hip_status(hipGetLastError(), many ? "k_paged_tile" : "k_paged_rows");
   if (st != ZO_OK || split == 1) return st;
-  const dim3 jgrid((unsigned)(units * a.prows));
-  if (f16) {
-    if (kv.dh == 64) hipLaunchKernelGGL((k_paged_join<true, 64>), jgrid, dim3(256), 0, stream, a);
-    else hipLaunchKernelGGL((k_paged_join<true, 128>), jgrid, dim3(256), 0, stream, a);
+  // One team of lanes per row, but for many splits of few rows.
+  const int teams = 256 / (kv.dh / 4);
+  const bool wide = split > 4 && units * a.prows <= 4096;
+  const dim3 jgrid((unsigned)(units * (wide ? a.prows : (a.prows + teams - 1) / teams)));
+#define ZO_JOIN(F, D)                                                                                       \
+  if (wide) hipLaunchKernelGGL((k_paged_join<F, D, 256 / (D / 4)>), jgrid, dim3(256), 0, stream, a);       \
+  else hipLaunchKernelGGL((k_paged_join<F, D, 1>), jgrid, dim3(256), 0, stream, a)
+  if (kv.dh == 64) {
+    if (f16) { ZO_JOIN(true, 64); } else { ZO_JOIN(false, 64); }
   } else {
-    if (kv.dh == 64) hipLaunchKernelGGL((k_paged_join<false, 64>), jgrid, dim3(256), 0, stream, a);
-    else hipLaunchKernelGGL((k_paged_join<false, 128>), jgrid, dim3(256), 0, stream, a);
+    if (f16) { ZO_JOIN(true, 128); } else { ZO_JOIN(false, 128); }
   }
+#undef ZO_JOIN
   return zo_hip_status(hipGetLastError(), "k_paged_join");
 }

@@ -6,7 +6,7 @@ import pytest
 import torch
 
 import paper_2608_15665_amd as zo
-from _paged import DT, E4M3, attend, batch, check_attention, dev, host64, rows16
+from _paged import DT, E4M3, attend, batch, check_attention, dev, host64, many, rows16
 
 pytestmark = pytest.mark.gpu
 
@@ -39,7 +39,7 @@ def test_single_tokens(ps, heads, kvh, dh, dt, cache):
 def test_pieces(news, lens, ps, heads, kvh, dh, dt, cache):
     rng = np.random.default_rng(sum(lens) + heads)
     got, ref, mag = attend(rng, dt, lens, news, ps, heads, kvh, dh, cache, pad=8, rows_behind=1)
-    check_attention(got, ref, mag, dt, (news, heads))
+    check_attention(got, ref, mag, dt, (news, heads), many(news, heads, kvh), cache)
 
 
 @pytest.mark.parametrize("cache", ["same", "e4m3"])
@@ -54,7 +54,7 @@ def test_long_contexts(heads, kvh, dh, news, lens, ps, width, cache):
     rng = np.random.default_rng(lens[0])
     for dt in ("bf16", "f16"):
         got, ref, mag = attend(rng, dt, lens, news, ps, heads, kvh, dh, cache, width=width, spread=2.0)
-        check_attention(got, ref, mag, dt, (lens, dt))
+        check_attention(got, ref, mag, dt, (lens, dt), many(news, heads, kvh), cache)
 
 
 @pytest.mark.parametrize("shape", ["rise", "fall", "large"])
@@ -71,7 +71,7 @@ def test_moving_maximum(shape, heads, kvh, dh, news, lens):
             k[s][:, :, 0] = (np.arange(n) if shape == "rise" else n - np.arange(n)) * 0.2 * np.sqrt(dh) / 3.0
     for dt in ("bf16", "f16"):
         got, ref, mag = attend(rng, dt, lens, news, 32, heads, kvh, dh, q=q.reshape(rows, -1), k=k)
-        check_attention(got, ref, mag, dt, (shape, dt))
+        check_attention(got, ref, mag, dt, (shape, dt), many(news, heads, kvh))
 
 
 @pytest.mark.parametrize("dt,c", [("f16", 1000.0), ("f16", 16376.0), ("bf16", 1024.0), ("bf16", 2.0 ** 45)])
@@ -83,7 +83,7 @@ def test_huge_logits(news, dt, c):
     q = np.full((news[0], dh), c)
     v = [rng.standard_normal((1, n, dh))]
     got, ref, mag = attend(rng, dt, [n], news, 64, 1, 1, dh, q=q, k=[np.full((1, n, dh), c)], v=v)
-    check_attention(got, ref, mag, dt, "equal")
+    check_attention(got, ref, mag, dt, "equal", many(news, 1, 1))
     k = [np.full((1, n, dh), c / 4)]
     k[0][0, 77] = c
     got, ref, _ = attend(rng, dt, [n], news, 64, 1, 1, dh, q=q, k=k, v=v)
@@ -120,13 +120,14 @@ def test_values_that_are_not_finite_stay_with_the_rows_that_see_them(news, heads
             from oracle import paged as op
             ref, mag = op.paged_attention(Qv.reshape(news[0], heads, dh), clean, table, q_start, kv_len)
             sees = np.arange(first, n) >= where
-            check_attention(got[~sees], ref[~sees], mag[~sees], "bf16", (tensor, bad, where))
+            check_attention(got[~sees], ref[~sees], mag[~sees], "bf16", (tensor, bad, where), many(news, heads, 1))
             if tensor == "k":
                 assert np.all(np.isnan(got[sees]))
             else:
                 assert np.all(np.isnan(got[sees][..., 5]) if np.isnan(bad) else got[sees][..., 5] == np.inf)
                 rest = np.arange(dh) != 5
-                check_attention(got[sees][..., rest], ref[sees][..., rest], mag[sees][..., rest], "bf16", (tensor, bad, where))
+                check_attention(got[sees][..., rest], ref[sees][..., rest], mag[sees][..., rest], "bf16", (tensor, bad, where),
+                                many(news, heads, 1))
 
 
 def _call(table, kv_len, q_start, max_q, pages=6, ps=16, rows=12, heads=2, dh=64):
