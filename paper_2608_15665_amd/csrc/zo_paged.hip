@@ -478,25 +478,22 @@ __global__ __launch_bounds__(64 * PG_W, 2) void k_paged_rows(PagedArgs a) {
 constexpr int PT_NG = 2;                  // 16-row groups per wave
 constexpr int PT_Q = 16 * PT_NG * PG_W;   // rows per workgroup
 constexpr int PT_K = 64;                  // keys per tile
-constexpr int PT_AHEAD = 3;               // LDS reads of a phase that go out before its first MFMA
+constexpr int PT_AHEAD = 2;               // LDS reads of a phase that go out before its first MFMA
 constexpr int PT_VALU = 24;               // vector instructions per 16 rows and 16 keys, for the scheduler
 
 // A workgroup of 4 waves takes PT_Q rows and a range of the keys.  Tiles of K and V come as stored (8-bit
 // codes too) by direct global -> LDS loads, two of each: while tile n is worked on, V of tile n + 1 and K of
 // tile n + 2 land, K of n + 1 has landed, and one barrier a tile is enough.  Tile n + 1's S runs under tile
-// n's exponentials.  A row of RB bytes keeps its 16-byte chunk c at c ^ f(row): f_k spreads the 16 rows of a K
-// fragment over all banks, f_v those of a transposed read of V.
+// n's exponentials.  A load fills 1024 bytes of LDS, some rows of RB bytes; each such block is followed by a pad,
+// and within a row the 16-byte chunks are permuted by an XOR with swz(row) in two bits, so that the 16 rows of a K
+// fragment, and the 8 (8-bit: 16) rows of a transposed read of V, lie on different banks.  A read's address is then
+// one of one (K) or four (V) per lane, the rest is an immediate offset.
 // P enters its product rounded once to 16 bits: each weight is off by at most 2^-8 (bf16) or 2^-11 (fp16) of
 // itself, as the output is by its own rounding, and the errors of many weights average out; the low parts
 // would cost half as many MFMAs again.
-template <int RB, bool E8>
-__device__ __forceinline__ int f_k(int r) {
-  return RB == 256 ? r & 15 : RB == 128 ? (r >> 1) & 7 : (r >> 2) & 3;
-}
-template <int RB, bool E8>
-__device__ __forceinline__ int f_v(int r) {
-  if (E8) return RB == 128 ? ((r >> 1) & 3) | ((r >> 2) & 4) : ((r >> 2) & 1) | ((r >> 3) & 2);
-  return RB == 256 ? 2 * (r & 7) : 2 * ((r >> 1) & 3);
+template <int RB>
+__device__ __forceinline__ int swz(int r) {
+  return RB == 256 ? r & 3 : RB == 128 ? (r >> 1) & 3 : (r >> 2) & 3;
 }
 
 template <bool F16, bool E8, int DH>
@@ -506,14 +503,18 @@ __global__ __launch_bounds__(64 * PG_W, 2) void k_paged_tile(PagedArgs a) {
   constexpr int EB = E8 ? 1 : 2, RB = DH * EB;  // bytes of a cached value, of a row
   constexpr int CPR = RB / 16;                  // chunks of a row
   constexpr int KCH = PT_K * CPR / NTH;         // loads per thread and tile
-  constexpr int TILE = PT_K * RB, RUN = 16 * RB;
+  constexpr int RUN = 16 * RB, RPB = 1024 / RB;  // bytes of 16 keys, rows of a block of LDS
+  constexpr int KBLK = 1024 + (RB == 64 ? 0 : 64), VBLK = 1024 + (E8 ? 32 : RB == 256 ? 128 : 0);
+  constexpr int NBLK = PT_K / RPB;               // blocks of a tile
+  constexpr int VX = E8 ? 1 : 2;                 // V's chunks are permuted one by one or in pairs
   constexpr bool PF16 = F16 && !E8;
   constexpr float SHIFT = PF16 ? 12.f : 0.f;
   constexpr int OROW = DH + 8;  // LDS row of the finished rows (16-bit elements)
-  static_assert(16 * OROW * 2 <= TILE, "16 finished rows of a wave fit a buffer");
+  static_assert(16 * OROW * 2 <= NBLK * 1024, "16 finished rows of a wave fit a buffer");
   // Four arrays, and steps that know at compile time which they use: the compiler then sees that a tile's reads
   // do not meet the loads under way, and does not wait for those.
-  __shared__ __attribute__((aligned(1024))) char Kb0[TILE], Kb1[TILE], Vb0[TILE], Vb1[TILE];
+  __shared__ __attribute__((aligned(1024))) char Kb0[NBLK * KBLK], Kb1[NBLK * KBLK], Vb0[NBLK * VBLK],
+      Vb1[NBLK * VBLK];
   __shared__ int bads[PG_W];
 
   // Workgroups are dealt to the 8 XCDs in turn; each XCD gets a contiguous range, a part of the key heads of
@@ -566,21 +567,21 @@ __global__ __launch_bounds__(64 * PG_W, 2) void k_paged_tile(PagedArgs a) {
   int bad = kv_cap(a.kv);
   const int rend = (rtile.kend + 15) >> 4;
 
-  // Load c of this wave fills 64 chunks of LDS, x = NTH c + tid: row x / CPR, place x % CPR; they lie in one run of
-  // 16 keys.  pg: the runs of tiles 16 win .. 16 win + 15, pgn those of the next 16.  K of a tile is loaded one
-  // tile before V, which lies in the same place of its tensor.
-  const int row0 = tid / CPR;  // of load 0; f does not depend on c
-  const unsigned offk = (unsigned)((row0 & 15) * RB + 16 * ((tid % CPR) ^ f_k<RB, E8>(row0)));
-  const unsigned offv = (unsigned)((row0 & 15) * RB + 16 * ((tid % CPR) ^ f_v<RB, E8>(row0)));
+  // Load c of this wave fills block 4 c + wave: rows RPB (4 c + wave) + lane / CPR, which lie in one run of 16 keys.
+  // pg: the runs of tiles 16 win .. 16 win + 15, pgn those of the next 16.  K of a tile is loaded one tile before
+  // V, which lies in the same place of its tensor.
+  const int brow = (RPB * wave + lane / CPR) & 15;  // of every c
+  const unsigned offk = (unsigned)(brow * RB + 16 * ((lane % CPR) ^ swz<RB>(brow)));
+  const unsigned offv = (unsigned)(brow * RB + 16 * ((lane % CPR) ^ (VX * swz<RB>(brow))));
   Runs<E8> pg, pgn;
   float ksp = 0.f, vsp = 0.f;  // 8-bit: the scales of the window before pg's
   int win = t0 >> 4;
-  auto dma = [&](const void* base, int tile, unsigned off, char* dst) {
+  auto dma = [&](const void* base, int tile, unsigned off, char* dst, int blk) {
 #pragma unroll
     for (int c = 0; c < KCH; ++c) {
-      const char* at = (const char*)base + pg.at(4 * (tile & 15) + (NTH * c + 64 * wave) / CPR / 16);
+      const char* at = (const char*)base + pg.at(4 * (tile & 15) + RPB * (PG_W * c + wave) / 16);
       const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void*)at, (short)0, RUN, 0x00020000);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_ptr_t)(dst + (NTH * c + 64 * wave) * 16), 16, off, 0, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_ptr_t)(dst + (PG_W * c + wave) * blk), 16, off, 0, 0, 0);
     }
   };
   auto load_k = [&](int tile, char* dst) {
@@ -593,55 +594,54 @@ __global__ __launch_bounds__(64 * PG_W, 2) void k_paged_tile(PagedArgs a) {
       pg = pgn;
       pgn.load(a, s, kvh, 64 * (win + 1), rend, RUN, lane, bad);
     }
-    dma(a.kv.K, tile, offk, dst);
+    dma(a.kv.K, tile, offk, dst, KBLK);
   };
   // V of the tile whose K was loaded last.
-  auto load_v = [&](int tile, char* dst) { dma(a.kv.V, tile, offv, dst); };
+  auto load_v = [&](int tile, char* dst) { dma(a.kv.V, tile, offv, dst, VBLK); };
   // Everything that this wave loads has landed; with the barrier, that of all waves.
   auto landed = [&]() {
     __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
     __syncthreads();
   };
 
-  // Where this lane reads: fragment kk (8 bits: pair of fragments) of K's row 16 t + l16 at (kat ^ 64 kk) + 16 RB t,
-  // V's column 16 t of rows 32 c + .. at (vat0 ^ 16 EB t) + 32 RB c (f does not depend on t or c, and the chunk
-  // numbers' bits are apart, so that their XOR is one of addresses).
-  const unsigned kat = (unsigned)(l16 * RB + 16 * (g ^ f_k<RB, E8>(l16)));
+  // Where this lane reads: fragment kk (8 bits: pair of fragments) of K's row 16 t + l16 at kat + 64 kk, row
+  // blocks ahead; V's column 16 t of key 32 c + .. at vat[t % 4] and whole 4 t ahead.
+  const int kat = l16 / RPB * KBLK + l16 % RPB * RB + 16 * (g ^ swz<RB>(l16));
   const int vrow = 4 * g + (E8 ? ((l16 >> 1) & 3) + 16 * (l16 >> 3) : l16 >> 2);
-  const unsigned vat0 = (unsigned)(vrow * RB + 16 * ((E8 ? 0 : (l16 >> 1) & 1) ^ f_v<RB, E8>(vrow)) + 8 * (l16 & 1));
-  // S^T of 16 keys (subtile t of the K tile whose reads start at `at`).
-  auto qk = [&](const char* kb, unsigned at, int t, f32x4 (*st)[4]) {
+  int vat[4];
 #pragma unroll
-    for (int gq = 0; gq < PT_NG; ++gq) st[gq][t] = (f32x4){0.f, 0.f, 0.f, 0.f};
+  for (int t = 0; t < 4; ++t)
+    vat[t] = vrow / RPB * VBLK + vrow % RPB * RB + 16 * VX * (t ^ swz<RB>(vrow)) + (E8 ? 0 : 16 * ((l16 >> 1) & 1)) + 8 * (l16 & 1);
+  // S^T of the four runs of 16 keys of a staged K tile.
+  auto qk = [&](const char* kb, f32x4 (*st)[4]) {
 #pragma unroll
-    for (int kk = 0; kk < KS; kk += E8 ? 2 : 1) {
-      const char* p = kb + (at ^ (E8 ? 32 * kk : 64 * kk)) + 16 * RB * t;
-      if constexpr (E8) {
-        const u32x4 x = *(const u32x4*)p;
-        const bf16x8 k0 = __builtin_bit_cast(bf16x8, widen8<F16>(x[0], x[1])), k1 = __builtin_bit_cast(bf16x8, widen8<F16>(x[2], x[3]));
+    for (int kk = 0; kk < KS; kk += E8 ? 2 : 1)
 #pragma unroll
-        for (int gq = 0; gq < PT_NG; ++gq) {
-          st[gq][t] = mfma16<F16>(k0, qf[gq][kk], st[gq][t]);
-          st[gq][t] = mfma16<F16>(k1, qf[gq][kk + 1], st[gq][t]);
+      for (int t = 0; t < 4; ++t) {
+        const char* p = kb + kat + 16 / RPB * KBLK * t + (E8 ? 32 * kk : 64 * kk);
+        if (kk == 0) {
+#pragma unroll
+          for (int gq = 0; gq < PT_NG; ++gq) st[gq][t] = (f32x4){0.f, 0.f, 0.f, 0.f};
         }
-      } else {
-        const bf16x8 kf = *(const bf16x8*)p;
+        if constexpr (E8) {
+          const u32x4 x = *(const u32x4*)p;
+          const bf16x8 k0 = __builtin_bit_cast(bf16x8, widen8<F16>(x[0], x[1])), k1 = __builtin_bit_cast(bf16x8, widen8<F16>(x[2], x[3]));
 #pragma unroll
-        for (int gq = 0; gq < PT_NG; ++gq) st[gq][t] = mfma16<F16>(kf, qf[gq][kk], st[gq][t]);
+          for (int gq = 0; gq < PT_NG; ++gq) {
+            st[gq][t] = mfma16<F16>(k0, qf[gq][kk], st[gq][t]);
+            st[gq][t] = mfma16<F16>(k1, qf[gq][kk + 1], st[gq][t]);
+          }
+        } else {
+          const bf16x8 kf = *(const bf16x8*)p;
+#pragma unroll
+          for (int gq = 0; gq < PT_NG; ++gq) st[gq][t] = mfma16<F16>(kf, qf[gq][kk], st[gq][t]);
+        }
       }
-    }
-  };
-  // Opaque, so that the addresses made from it are formed where they are used and not kept in registers
-  // through the loop.
-  auto opaque = [&](unsigned x) {
-    asm volatile("" : "+v"(x));
-    return x;
   };
   // One tile: its softmax and P V from V's buffer vt, st being its S.  NEXT: also the next tile's S (into sn,
   // from K's buffer kb); such a tile lies wholly before the workgroup's rows.
   auto tile = [&](auto NEXT, int n, const char* vt, const char* kb, f32x4 (*st)[4], f32x4 (*sn)[4]) {
     constexpr bool next = decltype(NEXT)::value;
-    const unsigned kn = opaque(kat), vn = opaque(vat0);
     const int k0 = PT_K * n;
     float vsc[4];
     if constexpr (E8) {
@@ -665,7 +665,7 @@ __global__ __launch_bounds__(64 * PG_W, 2) void k_paged_tile(PagedArgs a) {
             if (k0 + 16 * t + 4 * g + i > pos[gq]) st[gq][t][i] = -INFINITY;
       uint32_t odd = 0;
 #pragma unroll 4
-      for (int x = 0; x < TILE / 1024; ++x) odd |= odd_bits<PF16, E8>(*(const u32x4*)(vt + 1024 * x + 16 * lane));
+      for (int x = 0; x < NBLK; ++x) odd |= odd_bits<PF16, E8>(*(const u32x4*)(vt + VBLK * x + 16 * lane));
       clean = __ballot(odd != 0) != 0;
     }
 #pragma unroll
@@ -712,12 +712,12 @@ __global__ __launch_bounds__(64 * PG_W, 2) void k_paged_tile(PagedArgs a) {
 #pragma unroll
       for (int t = 0; t < DT; ++t) {
         u32x4 av;
-        const char* p = vt + (vn ^ (16 * EB * t)) + 32 * RB * c;
+        const char* p = vt + vat[t & 3] + 64 * VX * (t >> 2) + 32 / RPB * VBLK * c;
         if constexpr (E8) {
           const u32x2 v = ds_read_tr8(p);
           av = widen8<false>(v[0], v[1]);
         } else {
-          const u32x2 v0 = ds_read_tr((const uint16_t*)p), v1 = ds_read_tr((const uint16_t*)(p + 16 * RB));
+          const u32x2 v0 = ds_read_tr((const uint16_t*)p), v1 = ds_read_tr((const uint16_t*)(p + 16 / RPB * VBLK));
           av = (u32x4){v0[0], v0[1], v1[0], v1[1]};
         }
         if constexpr (decltype(CLEAN)::value)
@@ -732,8 +732,7 @@ __global__ __launch_bounds__(64 * PG_W, 2) void k_paged_tile(PagedArgs a) {
     constexpr int VR = E8 ? 1 : 2;                                       // V reads of a fragment
     __builtin_amdgcn_sched_barrier(0);
     if constexpr (next) {
-#pragma unroll
-      for (int t = 0; t < 4; ++t) qk(kb, kn, t, sn);
+      qk(kb, sn);
     }
     probs(0);
     if constexpr (next) {
@@ -751,8 +750,9 @@ __global__ __launch_bounds__(64 * PG_W, 2) void k_paged_tile(PagedArgs a) {
         probs(1);
         pv(0, std::true_type{});
         pv(1, std::true_type{});
-        add_odd_values<PF16, E8, DT, PT_NG>([&](int key, int d) { return vt + key * RB + 16 * ((d * EB / 16) ^ f_v<RB, E8>(key)) + (d * EB) % 16; },
-                                            k0, PT_K, g, pos, o);
+        add_odd_values<PF16, E8, DT, PT_NG>(
+            [&](int key, int d) { return vt + key / RPB * VBLK + key % RPB * RB + 16 * ((d * EB / 16) ^ (VX * swz<RB>(key))) + (d * EB) % 16; },
+            k0, PT_K, g, pos, o);
         return;
       }
     }
@@ -803,10 +803,7 @@ __global__ __launch_bounds__(64 * PG_W, 2) void k_paged_tile(PagedArgs a) {
     if (n + 1 < t1) load_v(n + 1, v1);
     f32x4 st[PT_NG][4];
     const bool mine = PT_K * n <= wlast;  // else every key of the tile is after the wave's rows
-    if (mine) {
-#pragma unroll
-      for (int t = 0; t < 4; ++t) qk(k0, kat, t, st);
-    }
+    if (mine) qk(k0, st);
     __syncthreads();
     if (n + 2 < t1) load_k(n + 2, k0);
     if (mine) tile(std::false_type{}, n, v0, k0, st, st);
@@ -815,8 +812,7 @@ __global__ __launch_bounds__(64 * PG_W, 2) void k_paged_tile(PagedArgs a) {
   if (n < tfull) {
     f32x4 sa[PT_NG][4], sb[PT_NG][4];
     landed();
-#pragma unroll
-    for (int t = 0; t < 4; ++t) qk(Kb0, kat, t, sa);
+    qk(Kb0, sa);
     for (;;) {
       whole(Kb0, Vb0, Kb1, Vb1, sa, sb);
       if (n >= tfull) break;
