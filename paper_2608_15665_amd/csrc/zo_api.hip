@@ -1019,6 +1019,8 @@ static int kv_args(const char* what, const zo_kv_cache* c, const zo_kv_batch* b,
   }
   ZO_CHECK((long long)b->max_pages << log2ps <= 0x7fffffffLL - 4096, "%s: max_pages = %d of %d positions exceed 2^31", what,
            b->max_pages, c->page_size);
+  ZO_CHECK(((long long)c->num_pages * c->kv_heads << (log2ps - 4)) < (1LL << 31), "%s: a cache of %d pages too large", what,
+           c->num_pages);
   ZO_CHECK(b->q_start || (b->rows >= b->nseq && (b->nseq == 0 || b->max_q >= 1)),
            "%s: rows = %d, max_q = %d without q_start (need one row of each of the %d sequences)", what, b->rows, b->max_q,
            b->nseq);

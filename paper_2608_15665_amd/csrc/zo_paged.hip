@@ -79,16 +79,16 @@ __device__ __forceinline__ RowTile row_tile(const PagedArgs& a, int s, int rt) {
   return t;
 }
 
-// Where 64 runs of 16 keys lie in K (and, in the same place, in V), one per lane, from run r0 on: bytes from
-// the cache's start.  Runs from `rend` on, and those of bad pages, lie in page 0, which exists: their keys are
+// Where 64 runs of 16 keys lie in K (and, in the same place, in V), one per lane, from run r0 on: as a number of
+// runs from the cache's start.  Runs from `rend` on, and those of bad pages, lie in page 0, which exists: their keys are
 // masked (or their rows NaN) and their values cleared or, in a tile that is masked anyway, harmless; their
 // scales are 0.  Without a branch at the load, the loads of a tile stay in flight together.
 // `bad`: the first position of a bad page.
 template <bool E8>
 struct Runs {
-  uint32_t lo, hi;
+  uint32_t run;
   float ks, vs;
-  __device__ __forceinline__ void load(const PagedArgs& a, int s, int kvh, int r0, int rend, int run_bytes, int lane, int& bad) {
+  __device__ __forceinline__ void load(const PagedArgs& a, int s, int kvh, int r0, int rend, int lane, int& bad) {
     const int r = r0 + lane, lr = a.kv.log2ps - 4;
     int page = 0;
     bool used = r < rend;
@@ -100,17 +100,16 @@ struct Runs {
         used = false;
       }
     }
-    const size_t head = (size_t)page * a.kv.kv_heads + kvh;
-    const size_t at = ((head << lr) + (r & ((1 << lr) - 1))) * run_bytes;
-    lo = (uint32_t)at;
-    hi = (uint32_t)(at >> 32);
+    const uint32_t head = (uint32_t)page * a.kv.kv_heads + kvh;
+    run = (head << lr) + (r & ((1 << lr) - 1));
     if constexpr (E8) {
       ks = used ? a.kv.ks[head] : 0.f;
       vs = used ? a.kv.vs[head] : 0.f;
     }
   }
+  template <int RUN>  // bytes of a run
   __device__ __forceinline__ size_t at(int l) const {
-    return (size_t)(uint32_t)__builtin_amdgcn_readlane(lo, l) | ((size_t)(uint32_t)__builtin_amdgcn_readlane(hi, l) << 32);
+    return (size_t)(uint32_t)__builtin_amdgcn_readlane(run, l) * RUN;
   }
 };
 
@@ -185,6 +184,15 @@ typedef int i32x2_t __attribute__((ext_vector_type(2)));
 // of row r_e, lane j thus receives column j of rows r_0 .. r_7.
 __device__ __forceinline__ u32x2 ds_read_tr8(const char* p) {
   return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) i32x2_t*)p));
+}
+
+// The sum of a pair of 16-bit values and an fp32 one, in one instruction (fp32 products with 1).
+template <bool F16>
+__device__ __forceinline__ float add_pair(uint32_t pk, float x) {
+  if constexpr (F16)
+    return __builtin_amdgcn_fdot2(__builtin_bit_cast(f16x2_t, pk), (f16x2_t){(_Float16)1.f, (_Float16)1.f}, x, false);
+  else
+    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, pk), (bf16x2_t){(__bf16)1.f, (__bf16)1.f}, x, false);
 }
 
 // A result o / l of a row at position p, from unnormalised sums: 0 where it has no keys, NaN where it
@@ -266,7 +274,7 @@ __global__ __launch_bounds__(64 * PG_W, 2) void k_paged_rows(PagedArgs a) {
   auto load_k = [&](int lane0) {
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-      const char* p = (const char*)a.kv.K + pg.at(lane0 + t);
+      const char* p = (const char*)a.kv.K + pg.template at<RUN>(lane0 + t);
 #pragma unroll
       for (int c = 0; c < KV4; ++c) kreg[t][c] = *(const u32x4*)(p + l16 * DH * EB + 16 * g + 64 * c);
     }
@@ -274,7 +282,7 @@ __global__ __launch_bounds__(64 * PG_W, 2) void k_paged_rows(PagedArgs a) {
   auto load_v = [&](int lane0) {
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-      const char* p = (const char*)a.kv.V + pg.at(lane0 + t);
+      const char* p = (const char*)a.kv.V + pg.template at<RUN>(lane0 + t);
 #pragma unroll
       for (int c = 0; c < KV4; ++c) vreg[t][c] = *(const u32x4*)(p + 16 * lane + 1024 * c);
     }
@@ -292,8 +300,8 @@ __global__ __launch_bounds__(64 * PG_W, 2) void k_paged_rows(PagedArgs a) {
     }
   };
   if (t0 + wave < t1) {
-    pg.load(a, s, kvh, NT * have, rend, RUN, lane, bad);
-    pgn.load(a, s, kvh, NT * (have + WT), rend, RUN, lane, bad);
+    pg.load(a, s, kvh, NT * have, rend, lane, bad);
+    pgn.load(a, s, kvh, NT * (have + WT), rend, lane, bad);
     load_k(NT * wave);
     load_v(NT * wave);
   }
@@ -306,7 +314,7 @@ __global__ __launch_bounds__(64 * PG_W, 2) void k_paged_rows(PagedArgs a) {
     if (more && next >= have + WT) {
       have += WT;
       pg = pgn;
-      pgn.load(a, s, kvh, NT * (have + WT), rend, RUN, lane, bad);
+      pgn.load(a, s, kvh, NT * (have + WT), rend, lane, bad);
     }
     const int lane0 = NT * (next - have);
     const int k0 = tile * PG_K;
@@ -478,8 +486,8 @@ __global__ __launch_bounds__(64 * PG_W, 2) void k_paged_rows(PagedArgs a) {
 constexpr int PT_NG = 2;                  // 16-row groups per wave
 constexpr int PT_Q = 16 * PT_NG * PG_W;   // rows per workgroup
 constexpr int PT_K = 64;                  // keys per tile
+constexpr float PT_RAW = 1048576.f;       // maxima from here on (in log2 units) are subtracted from the logits
 constexpr int PT_AHEAD = 2;               // LDS reads of a phase that go out before its first MFMA
-constexpr int PT_VALU = 24;               // vector instructions per 16 rows and 16 keys, for the scheduler
 
 // A workgroup of 4 waves takes PT_Q rows and a range of the keys.  Tiles of K and V come as stored (8-bit
 // codes too) by direct global -> LDS loads, two of each: while tile n is worked on, V of tile n + 1 and K of
@@ -555,14 +563,20 @@ __global__ __launch_bounds__(64 * PG_W, 2) void k_paged_tile(PagedArgs a) {
   const int wfirst = p0 + (rtile.row0 + min(wr0, rtile.nrows - 1)) / a.group;
   const int wlast = wr0 < rtile.nrows ? p0 + (rtile.row0 + min(wr0 + 16 * PT_NG, rtile.nrows) - 1) / a.group : -1;
 
+  // P = 2^(s scale + b), b = SHIFT - m scale rounded: its rounding is the same factor for all of a row's P, and
+  // from one maximum m to the next the exact b are subtracted.  Where m scale is so large that the rounding
+  // could be whole powers of two (`raw`, of the wave, from then on), m is subtracted from the logits first and b
+  // is SHIFT.
   f32x4 o[PT_NG][DT];
-  float mrow[PT_NG], lsum[PT_NG];
+  float mrow[PT_NG], brow[PT_NG], lsum[PT_NG];  // lsum: of this lane's keys
+  int raw = 0;
 #pragma unroll
   for (int gq = 0; gq < PT_NG; ++gq) {
 #pragma unroll
     for (int t = 0; t < DT; ++t) o[gq][t] = (f32x4){0.f, 0.f, 0.f, 0.f};
-    mrow[gq] = PG_LOW;
     lsum[gq] = 0.f;
+    mrow[gq] = PG_LOW;
+    brow[gq] = 0.f;
   }
   int bad = kv_cap(a.kv);
   const int rend = (rtile.kend + 15) >> 4;
@@ -570,16 +584,16 @@ __global__ __launch_bounds__(64 * PG_W, 2) void k_paged_tile(PagedArgs a) {
   // Load c of this wave fills block 4 c + wave: rows RPB (4 c + wave) + lane / CPR, which lie in one run of 16 keys.
   // pg: the runs of tiles 16 win .. 16 win + 15, pgn those of the next 16.  K of a tile is loaded one tile before
   // V, which lies in the same place of its tensor.
-  const int brow = (RPB * wave + lane / CPR) & 15;  // of every c
-  const unsigned offk = (unsigned)(brow * RB + 16 * ((lane % CPR) ^ swz<RB>(brow)));
-  const unsigned offv = (unsigned)(brow * RB + 16 * ((lane % CPR) ^ (VX * swz<RB>(brow))));
+  const int drow = (RPB * wave + lane / CPR) & 15;  // of every c
+  const unsigned offk = (unsigned)(drow * RB + 16 * ((lane % CPR) ^ swz<RB>(drow)));
+  const unsigned offv = (unsigned)(drow * RB + 16 * ((lane % CPR) ^ (VX * swz<RB>(drow))));
   Runs<E8> pg, pgn;
   float ksp = 0.f, vsp = 0.f;  // 8-bit: the scales of the window before pg's
   int win = t0 >> 4;
   auto dma = [&](const void* base, int tile, unsigned off, char* dst, int blk) {
 #pragma unroll
     for (int c = 0; c < KCH; ++c) {
-      const char* at = (const char*)base + pg.at(4 * (tile & 15) + RPB * (PG_W * c + wave) / 16);
+      const char* at = (const char*)base + pg.template at<RUN>(4 * (tile & 15) + RPB * (PG_W * c + wave) / 16);
       const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void*)at, (short)0, RUN, 0x00020000);
       __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_ptr_t)(dst + (PG_W * c + wave) * blk), 16, off, 0, 0, 0);
     }
@@ -592,7 +606,7 @@ __global__ __launch_bounds__(64 * PG_W, 2) void k_paged_tile(PagedArgs a) {
         vsp = pg.vs;
       }
       pg = pgn;
-      pgn.load(a, s, kvh, 64 * (win + 1), rend, RUN, lane, bad);
+      pgn.load(a, s, kvh, 64 * (win + 1), rend, lane, bad);
     }
     dma(a.kv.K, tile, offk, dst, KBLK);
   };
@@ -638,22 +652,41 @@ __global__ __launch_bounds__(64 * PG_W, 2) void k_paged_tile(PagedArgs a) {
         }
       }
   };
-  // One tile: its softmax and P V from V's buffer vt, st being its S.  NEXT: also the next tile's S (into sn,
-  // from K's buffer kb); such a tile lies wholly before the workgroup's rows.
-  auto tile = [&](auto NEXT, int n, const char* vt, const char* kb, f32x4 (*st)[4], f32x4 (*sn)[4]) {
+  // 8-bit: the scales of tile n's four runs, of keys or values.
+  auto scales = [&](int n, float now, float before, float* out) {
+#pragma unroll
+    for (int t = 0; t < 4; ++t) out[t] = lane_f((n >> 4) == win ? now : before, 4 * (n & 15) + t);
+  };
+  auto scale_s = [&](int n, f32x4 (*st)[4]) {
+    if constexpr (E8) {
+      float ks[4];
+      scales(n, pg.ks, ksp, ks);
+#pragma unroll
+      for (int gq = 0; gq < PT_NG; ++gq)
+#pragma unroll
+        for (int t = 0; t < 4; ++t) st[gq][t] *= ks[t];
+    }
+  };
+  auto top_of = [&](f32x4 (*st)[4], float* tmax) {
+#pragma unroll
+    for (int gq = 0; gq < PT_NG; ++gq) {
+      tmax[gq] = -INFINITY;
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) tmax[gq] = fmaxf(tmax[gq], st[gq][t][i]);
+      tmax[gq] = max_groups(tmax[gq]);
+    }
+  };
+  // One tile: its softmax and P V from V's buffer vt, st being its S and tmax S's largest entries (of whole tiles).
+  // NEXT: also the next tile's S (into sn, from K's buffer kb) and its tmax; such a tile lies wholly before the
+  // workgroup's rows.
+  auto tile = [&](auto NEXT, int n, const char* vt, const char* kb, f32x4 (*st)[4], f32x4 (*sn)[4], float* tmax) {
     constexpr bool next = decltype(NEXT)::value;
     const int k0 = PT_K * n;
     float vsc[4];
-    if constexpr (E8) {
-      const float kw = (n >> 4) == win ? pg.ks : ksp, vw = (n >> 4) == win ? pg.vs : vsp;
-#pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        const float ksc = lane_f(kw, 4 * (n & 15) + t);
-        vsc[t] = lane_f(vw, 4 * (n & 15) + t);
-#pragma unroll
-        for (int gq = 0; gq < PT_NG; ++gq) st[gq][t] *= ksc;
-      }
-    }
+    if constexpr (E8) scales(n, pg.vs, vsp, vsc);
+    if constexpr (!next) scale_s(n, st);
     bool clean = false;  // V of the tile is not finite, and rows see only a part of it
     if (!next && k0 + PT_K > wfirst + 1) {
 #pragma unroll
@@ -668,23 +701,43 @@ __global__ __launch_bounds__(64 * PG_W, 2) void k_paged_tile(PagedArgs a) {
       for (int x = 0; x < NBLK; ++x) odd |= odd_bits<PF16, E8>(*(const u32x4*)(vt + VBLK * x + 16 * lane));
       clean = __ballot(odd != 0) != 0;
     }
+    if constexpr (!next) top_of(st, tmax);
 #pragma unroll
     for (int gq = 0; gq < PT_NG; ++gq) {
-      float tmax = -INFINITY;
-#pragma unroll
-      for (int t = 0; t < 4; ++t)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) tmax = fmaxf(tmax, st[gq][t][i]);
-      tmax = max_groups(tmax);
       const float m = mrow[gq];
-      if (__builtin_expect(__ballot((tmax - m) * a.scale_log2 > 3.f) != 0, 0)) {
-        const float mnew = fmaxf(m, tmax);
-        const float alpha = __builtin_amdgcn_exp2f((m - mnew) * a.scale_log2);
+      if (__builtin_expect(__ballot((tmax[gq] - m) * a.scale_log2 > 3.f) != 0, 0)) {
+        const float mnew = fmaxf(m, tmax[gq]), b = brow[gq];
+        const bool was = raw != 0;
+        raw |= __ballot(mnew > PG_LOW && !(fabsf(mnew * a.scale_log2) < PT_RAW)) != 0;
+        const float bnew = raw ? SHIFT : fmaf(-mnew, a.scale_log2, SHIFT);
+        // 2^(what P = 1 now stands for, relative to before)
+        float d = was ? (m - mnew) * a.scale_log2 : raw ? SHIFT - fmaf(mnew, a.scale_log2, b) : bnew - b;
+        if (m == PG_LOW) d = mnew == PG_LOW ? 0.f : -INFINITY;
+        const float alpha = __builtin_amdgcn_exp2f(d);
         mrow[gq] = mnew;
+        brow[gq] = bnew;
         lsum[gq] *= alpha;
 #pragma unroll
         for (int t = 0; t < DT; ++t) o[gq][t] *= alpha;
+        if (raw && !was) {
+          // the other rows of the wave, from their b to their maximum
+#pragma unroll
+          for (int x = 0; x < PT_NG; ++x)
+            if (x != gq) {
+              const float f = mrow[x] == PG_LOW ? 1.f : __builtin_amdgcn_exp2f(SHIFT - fmaf(mrow[x], a.scale_log2, brow[x]));
+              brow[x] = SHIFT;
+              lsum[x] *= f;
+#pragma unroll
+              for (int t = 0; t < DT; ++t) o[x][t] *= f;
+            }
+        }
       }
+    }
+    if (__builtin_expect(raw, 0)) {
+#pragma unroll
+      for (int gq = 0; gq < PT_NG; ++gq)
+#pragma unroll
+        for (int t = 0; t < 4; ++t) st[gq][t] -= mrow[gq];
     }
     bf16x8 bh[2][PT_NG];
     auto probs = [&](int c) {
@@ -694,14 +747,15 @@ __global__ __launch_bounds__(64 * PG_W, 2) void k_paged_tile(PagedArgs a) {
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
           const int t = 2 * c + (x >> 1), i = 2 * (x & 1);
-          float q0 = __builtin_amdgcn_exp2f(fmaf(st[gq][t][i] - mrow[gq], a.scale_log2, SHIFT));
-          float q1 = __builtin_amdgcn_exp2f(fmaf(st[gq][t][i + 1] - mrow[gq], a.scale_log2, SHIFT));
-          lsum[gq] += q0 + q1;
+          float q0 = __builtin_amdgcn_exp2f(fmaf(st[gq][t][i], a.scale_log2, brow[gq]));
+          float q1 = __builtin_amdgcn_exp2f(fmaf(st[gq][t][i + 1], a.scale_log2, brow[gq]));
           if constexpr (E8) {
+            lsum[gq] += q0 + q1;
             q0 *= vsc[t];
             q1 *= vsc[t];
           }
           hp[x] = cvt_pk<PF16>(q0, q1);
+          if constexpr (!E8) lsum[gq] = add_pair<PF16>(hp[x], lsum[gq]);
         }
         bh[c][gq] = __builtin_bit_cast(bf16x8, hp);
       }
@@ -730,6 +784,7 @@ __global__ __launch_bounds__(64 * PG_W, 2) void k_paged_tile(PagedArgs a) {
     // The first reads of a phase go out together; each later one while the MFMAs of an earlier one run.
     constexpr int KR = E8 ? 2 * KS : 4 * KS, KM = 4 * KS * PT_NG / KR;   // K reads, MFMAs of each
     constexpr int VR = E8 ? 1 : 2;                                       // V reads of a fragment
+    constexpr int KV = (E8 ? 136 : 48) / KR, VV = (E8 ? 104 : 48) / DT;  // vector instructions beside each
     __builtin_amdgcn_sched_barrier(0);
     if constexpr (next) {
       qk(kb, sn);
@@ -739,7 +794,7 @@ __global__ __launch_bounds__(64 * PG_W, 2) void k_paged_tile(PagedArgs a) {
       __builtin_amdgcn_sched_group_barrier(0x100, PT_AHEAD, 0);
 #pragma unroll
       for (int x = 0; x < KR; ++x) {
-        __builtin_amdgcn_sched_group_barrier(0x002, 4 * PT_VALU / KR, 0);
+        __builtin_amdgcn_sched_group_barrier(0x002, KV, 0);
         __builtin_amdgcn_sched_group_barrier(0x008, KM, 0);
         if (x + PT_AHEAD < KR) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
       }
@@ -761,15 +816,20 @@ __global__ __launch_bounds__(64 * PG_W, 2) void k_paged_tile(PagedArgs a) {
     __builtin_amdgcn_sched_group_barrier(0x100, VR * PT_AHEAD, 1);
 #pragma unroll
     for (int x = 0; x < DT; ++x) {
-      __builtin_amdgcn_sched_group_barrier(0x002, 4 * PT_VALU / DT, 1);
+      __builtin_amdgcn_sched_group_barrier(0x002, VV, 1);
       __builtin_amdgcn_sched_group_barrier(0x008, PT_NG, 1);
       if (x + PT_AHEAD < DT) __builtin_amdgcn_sched_group_barrier(0x100, VR, 1);
     }
     __builtin_amdgcn_sched_barrier(0);
     pv(1, std::false_type{});
+    if constexpr (next) {
+      scale_s(n + 1, sn);
+      top_of(sn, tmax);
+    }
     __builtin_amdgcn_sched_group_barrier(0x100, VR * PT_AHEAD, 2);
 #pragma unroll
     for (int x = 0; x < DT; ++x) {
+      __builtin_amdgcn_sched_group_barrier(0x002, (next ? 32 : 0) / DT, 2);
       __builtin_amdgcn_sched_group_barrier(0x008, PT_NG, 2);
       if (x + PT_AHEAD < DT) __builtin_amdgcn_sched_group_barrier(0x100, VR, 2);
     }
@@ -781,19 +841,20 @@ __global__ __launch_bounds__(64 * PG_W, 2) void k_paged_tile(PagedArgs a) {
   const int tfull = min(t1, (p0 + rtile.row0 / a.group + 1) / PT_K);
   int n = t0;
   if (n < t1) {
-    pg.load(a, s, kvh, 64 * win, rend, RUN, lane, bad);
-    pgn.load(a, s, kvh, 64 * (win + 1), rend, RUN, lane, bad);
+    pg.load(a, s, kvh, 64 * win, rend, lane, bad);
+    pgn.load(a, s, kvh, 64 * (win + 1), rend, lane, bad);
     load_k(n, Kb0);
     load_v(n, Vb0);
     if (n + 1 < t1) load_k(n + 1, Kb1);
   }
   // A whole tile with K and V in buffers k0 / v0, the next in k1 / v1.  At its top K(n + 1) and V(n) have landed,
   // and every wave is done with K(n) and V(n - 1).
+  float tmax[PT_NG];
   auto whole = [&](char* k0, char* v0, char* k1, char* v1, f32x4 (*st)[4], f32x4 (*sn)[4]) {
     landed();
     if (n + 1 < t1) load_v(n + 1, v1);
     if (n + 2 < t1) load_k(n + 2, k0);
-    tile(std::true_type{}, n, v0, k1, st, sn);
+    tile(std::true_type{}, n, v0, k1, st, sn, tmax);
     ++n;
   };
   // A tile that is masked, or beyond the rows of some waves: S(n) is formed first, and K(n)'s buffer is not
@@ -806,13 +867,15 @@ __global__ __launch_bounds__(64 * PG_W, 2) void k_paged_tile(PagedArgs a) {
     if (mine) qk(k0, st);
     __syncthreads();
     if (n + 2 < t1) load_k(n + 2, k0);
-    if (mine) tile(std::false_type{}, n, v0, k0, st, st);
+    if (mine) tile(std::false_type{}, n, v0, k0, st, st, tmax);
     ++n;
   };
   if (n < tfull) {
     f32x4 sa[PT_NG][4], sb[PT_NG][4];
     landed();
     qk(Kb0, sa);
+    scale_s(n, sa);
+    top_of(sa, tmax);
     for (;;) {
       whole(Kb0, Vb0, Kb1, Vb1, sa, sb);
       if (n >= tfull) break;
@@ -843,6 +906,11 @@ __global__ __launch_bounds__(64 * PG_W, 2) void k_paged_tile(PagedArgs a) {
     const int row = wr0 + 16 * gq + l16;
     if (nsp > 1) {
       if (row >= rtile.nrows) continue;
+      // relative to the maximum itself, without b's rounding
+      const float f = raw || mrow[gq] == PG_LOW ? 1.f : __builtin_amdgcn_exp2f(SHIFT - fmaf(mrow[gq], a.scale_log2, brow[gq]));
+      l *= f;
+#pragma unroll
+      for (int t = 0; t < DT; ++t) o[gq][t] *= f;
       const size_t at = ((((size_t)s * a.kv.kv_heads + kvh) * a.tiles + rt) * a.nsplit + split) * a.prows + row;
 #pragma unroll
       for (int t = 0; t < DT; ++t) *(f32x4*)&a.part[at * DH + 16 * t + 4 * g] = o[gq][t];
