@@ -48,6 +48,7 @@ __device__ __forceinline__ int splits_of(const PagedArgs& a, int keys) {
 // The sequence that is i-th when every 64 consecutive ones are ordered by their lengths, the longest first:
 // workgroups start in that order, so that the long ones are not the last to end.
 __device__ __forceinline__ int by_length(const KvArgs& a, int i, int lane) {
+  if (a.nseq == 1) return 0;
   const int s0 = i & ~63, n = min(64, a.nseq - s0);
   const int len = lane < n ? a.kv_len[s0 + lane] : -0x7fffffff - 1;
   int rank = 0;
@@ -857,17 +858,19 @@ __global__ __launch_bounds__(64 * PG_W, 2) void k_paged_tile(PagedArgs a) {
     tile(std::true_type{}, n, v0, k1, st, sn, tmax);
     ++n;
   };
-  // A tile that is masked, or beyond the rows of some waves: S(n) is formed first, and K(n)'s buffer is not
-  // written until every wave has it.
-  auto part = [&](char* k0, char* v0, char* v1) {
+  // A tile that is masked, or beyond the rows of some waves: its S comes first, so that K is loaded one tile ahead
+  // only (kin: K(n + 1) is on its way already).
+  auto part = [&](char* k0, char* v0, char* k1, char* v1, bool kin) {
     landed();
-    if (n + 1 < t1) load_v(n + 1, v1);
-    f32x4 st[PT_NG][4];
-    const bool mine = PT_K * n <= wlast;  // else every key of the tile is after the wave's rows
-    if (mine) qk(k0, st);
-    __syncthreads();
-    if (n + 2 < t1) load_k(n + 2, k0);
-    if (mine) tile(std::false_type{}, n, v0, k0, st, st, tmax);
+    if (n + 1 < t1) {
+      if (!kin) load_k(n + 1, k1);
+      load_v(n + 1, v1);
+    }
+    if (PT_K * n <= wlast) {  // else every key of the tile is after the wave's rows
+      f32x4 st[PT_NG][4];
+      qk(k0, st);
+      tile(std::false_type{}, n, v0, k0, st, st, tmax);
+    }
     ++n;
   };
   if (n < tfull) {
@@ -883,10 +886,15 @@ __global__ __launch_bounds__(64 * PG_W, 2) void k_paged_tile(PagedArgs a) {
       if (n >= tfull) break;
     }
   }
-  if (n < t1 && ((n - t0) & 1)) part(Kb1, Vb1, Vb0);
+  bool kin = true;
+  if (n < t1 && ((n - t0) & 1)) {
+    part(Kb1, Vb1, Kb0, Vb0, true);
+    kin = false;
+  }
   while (n < t1) {
-    part(Kb0, Vb0, Vb1);
-    if (n < t1) part(Kb1, Vb1, Vb0);
+    part(Kb0, Vb0, Kb1, Vb1, kin);
+    kin = false;
+    if (n < t1) part(Kb1, Vb1, Kb0, Vb0, false);
   }
 
 #pragma unroll
