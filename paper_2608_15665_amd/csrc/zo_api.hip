@@ -997,7 +997,7 @@ static int kv_args(const char* what, const zo_kv_cache* c, const zo_kv_batch* b,
   ZO_CHECK(b->rows <= (1 << 30), "%s: rows = %d too many", what, b->rows);
   ZO_CHECK(b->max_pages >= 1 && c->num_pages >= 1 && c->kv_heads >= 1,
            "%s: max_pages = %d, num_pages = %d, kv_heads = %d must be >= 1", what, b->max_pages, c->num_pages, c->kv_heads);
-  ZO_CHECK(heads >= 0 && heads <= (1 << 16) && c->kv_heads <= (1 << 16), "%s: heads = %d, kv_heads = %d out of range",
+  ZO_CHECK(heads >= 0 && heads <= (1 << 15) && c->kv_heads <= (1 << 15), "%s: heads = %d, kv_heads = %d out of range",
            what, heads, c->kv_heads);
   if (dtype != ZO_BF16 && dtype != ZO_F16) {
     zo_set_error("%s: dtype %d unsupported (bf16 or fp16)", what, dtype);

@@ -35,6 +35,7 @@ struct PagedArgs {
   int group, nsplit, tiles;           // heads per K/V head; splits; row tiles per (sequence, K/V head)
   int rt_rows, prows;                 // rows of a tile; those of them that partial results have room for
   int min_keys;                       // a split's keys at the least
+  uint32_t inv_group;                 // 2^32 / group, rounded up past a whole one; 0: group is 1
   float scale_log2;                   // log2(e) / sqrt(dh)
   float* part;                        // nsplit > 1: O of a split, unnormalised, per row
   float2* stat;                       // its (maximum, sum)
@@ -45,35 +46,50 @@ __device__ __forceinline__ int splits_of(const PagedArgs& a, int keys) {
   return min(a.nsplit, max(1, (keys + a.min_keys - 1) / a.min_keys));
 }
 
-// The sequence that is i-th when every 64 consecutive ones are ordered by their lengths, the longest first:
-// workgroups start in that order, so that the long ones are not the last to end.
-__device__ __forceinline__ int by_length(const KvArgs& a, int i, int lane) {
-  if (a.nseq == 1) return 0;
+// The sequence that is i-th when every 64 consecutive ones are ordered by their lengths, the longest first
+// (workgroups start in that order, so that the long ones are not the last to end), and its rows and length: the
+// loads of all lanes' sequences go out together, and the one that it is comes from its lane.
+__device__ __forceinline__ int by_length(const KvArgs& a, int i, int lane, KvSpan& sp) {
   const int s0 = i & ~63, n = min(64, a.nseq - s0);
-  const int len = lane < n ? a.kv_len[s0 + lane] : -0x7fffffff - 1;
+  const int mine = s0 + min(lane, n - 1);
+  const KvSpan own = kv_span(a, mine);
   int rank = 0;
   for (int j = 0; j < n; ++j) {
-    const int other = __builtin_amdgcn_readlane(len, j);
-    rank += other > len || (other == len && j < lane);
+    const int other = __builtin_amdgcn_readlane(own.len, j);
+    rank += other > own.len || (other == own.len && j < lane);
   }
-  const uint64_t hit = __ballot(lane < n && rank == (i & 63));
-  return s0 + __builtin_ctzll(hit);
+  const int l = __builtin_ctzll(__ballot(lane < n && rank == (i & 63)));
+  sp.r0 = __builtin_amdgcn_readlane(own.r0, l);
+  sp.n = __builtin_amdgcn_readlane(own.n, l);
+  sp.len = __builtin_amdgcn_readlane(own.len, l);
+  return s0 + l;
 }
 
-// What a row tile covers: rows [row0, row0 + nrows) of its (sequence, K/V head), keys [0, kend).
+// What a row tile covers: rows [row0, row0 + nrows) of its (sequence, K/V head), keys [0, kend).  Row i of the tile
+// is token tok(i) of the sequence's new ones and head i + rem - group (tok(i) - tok0) of the group.
 struct RowTile {
   KvSpan sp;
   int row0, nrows, kend;
+  int tok0, rem, group;
+  uint32_t inv;
+  // (row0 + i) / group by a product: i + rem < 2^32 / group, where the rounded inverse is exact.
+  __device__ __forceinline__ int tok(int i) const { return tok0 + (inv ? (int)__umulhi((uint32_t)(i + rem), inv) : i); }
+  __device__ __forceinline__ int head(int i) const { return i + rem - group * (tok(i) - tok0); }
+  __device__ __forceinline__ int pos(int i) const { return sp.len - sp.n + tok(i); }
 };
-__device__ __forceinline__ RowTile row_tile(const PagedArgs& a, int s, int rt) {
+__device__ __forceinline__ RowTile row_tile(const PagedArgs& a, const KvSpan& sp, int rt) {
   RowTile t;
-  t.sp = kv_span(a.kv, s);
+  t.sp = sp;
   t.row0 = rt * a.rt_rows;
-  const int all = min(t.sp.n, a.kv.max_q) * a.group;
+  t.group = a.group;
+  t.inv = a.inv_group;
+  t.tok0 = t.row0 / a.group;
+  t.rem = t.row0 - t.tok0 * a.group;
+  const int all = min(sp.n, a.kv.max_q) * a.group;
   t.nrows = min(a.rt_rows, all - t.row0);
   t.kend = 0;
   if (t.nrows > 0) {
-    const int last = t.sp.len - t.sp.n + (t.row0 + t.nrows - 1) / a.group;  // the last row's position
+    const int last = t.pos(t.nrows - 1);  // the last row's position
     if (a.kv.bad_flag && last >= kv_cap(a.kv)) *a.kv.bad_flag = 1;
     t.kend = max(0, min(last + 1, kv_cap(a.kv)));
   }
@@ -89,19 +105,16 @@ template <bool E8>
 struct Runs {
   uint32_t run;
   float ks, vs;
-  __device__ __forceinline__ void load(const PagedArgs& a, int s, int kvh, int r0, int rend, int lane, int& bad) {
+  // Two steps, so that loads of several windows go out together: the table's entry, then the rest.
+  __device__ __forceinline__ void fetch(const PagedArgs& a, int s, int r0, int lane) {
+    const int j = min((r0 + lane) >> (a.kv.log2ps - 4), a.kv.max_pages - 1);
+    run = a.kv.table[(size_t)s * a.kv.max_pages + j];
+  }
+  __device__ __forceinline__ void place(const PagedArgs& a, int kvh, int r0, int rend, int lane, int& bad) {
     const int r = r0 + lane, lr = a.kv.log2ps - 4;
-    int page = 0;
-    bool used = r < rend;
-    if (used) {
-      page = kv_page(a.kv, s, r >> lr);
-      if (page < 0) {
-        bad = min(bad, r * 16);
-        page = 0;
-        used = false;
-      }
-    }
-    const uint32_t head = (uint32_t)page * a.kv.kv_heads + kvh;
+    const bool used = r < rend && run < (uint32_t)a.kv.num_pages;
+    if (r < rend && !used) bad = min(bad, r * 16);
+    const uint32_t head = (used ? run : 0) * a.kv.kv_heads + kvh;
     run = (head << lr) + (r & ((1 << lr) - 1));
     if constexpr (E8) {
       ks = used ? a.kv.ks[head] : 0.f;
@@ -230,14 +243,13 @@ __global__ __launch_bounds__(64 * PG_W, 2) void k_paged_rows(PagedArgs a) {
   const int rt = w % a.tiles;
   w /= a.tiles;
   const int kvh = w % a.kv.kv_heads, s = w / a.kv.kv_heads;
-  const RowTile rtile = row_tile(a, s, rt);
+  const RowTile rtile = row_tile(a, kv_span(a.kv, s), rt);
   if (rtile.nrows <= 0) return;
   const int nsp = splits_of(a, rtile.kend);
   if (split >= nsp) return;
   const int ntiles = (rtile.kend + PG_K - 1) / PG_K;
   const int t0 = (int)((long long)ntiles * split / nsp), t1 = (int)((long long)ntiles * (split + 1) / nsp);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, g = lane >> 4;
-  const int p0 = rtile.sp.len - rtile.sp.n;  // position of the sequence's row 0
 
   // This lane's queries (one per group) and their rows, in the order of K's fragments: lane group g's
   // step kk is dims 32 kk + 8 g; with 8-bit keys (16 per 16-byte word) 16 (g + 4 (kk / 2)) + 8 (kk % 2).
@@ -245,15 +257,14 @@ __global__ __launch_bounds__(64 * PG_W, 2) void k_paged_rows(PagedArgs a) {
   bf16x8 qf[NG][KS];
 #pragma unroll
   for (int gq = 0; gq < NG; ++gq) {
-    const int r = rtile.row0 + min(16 * gq + l16, rtile.nrows - 1);
-    const int tok = r / a.group;
-    pos[gq] = p0 + tok;
-    const uint16_t* qp = (const uint16_t*)a.Q + (size_t)(rtile.sp.r0 + tok) * a.ldq + (size_t)(kvh * a.group + r % a.group) * DH;
+    const int i = min(16 * gq + l16, rtile.nrows - 1);
+    pos[gq] = rtile.pos(i);
+    const uint16_t* qp = (const uint16_t*)a.Q + (size_t)(rtile.sp.r0 + rtile.tok(i)) * a.ldq + (size_t)(kvh * a.group + rtile.head(i)) * DH;
 #pragma unroll
     for (int kk = 0; kk < KS; ++kk)
       qf[gq][kk] = __builtin_bit_cast(bf16x8, *(const u32x4*)(qp + (E8 ? 16 * (g + 4 * (kk >> 1)) + 8 * (kk & 1) : 32 * kk + 8 * g)));
   }
-  const int pfirst = p0 + rtile.row0 / a.group;  // the tile's first position
+  const int pfirst = rtile.pos(0);  // the tile's first position
 
   f32x4 o[NG][DT];
   float mrow[NG], lsum[NG];
@@ -301,8 +312,10 @@ __global__ __launch_bounds__(64 * PG_W, 2) void k_paged_rows(PagedArgs a) {
     }
   };
   if (t0 + wave < t1) {
-    pg.load(a, s, kvh, NT * have, rend, lane, bad);
-    pgn.load(a, s, kvh, NT * (have + WT), rend, lane, bad);
+    pg.fetch(a, s, NT * have, lane);
+    pgn.fetch(a, s, NT * (have + WT), lane);
+    pg.place(a, kvh, NT * have, rend, lane, bad);
+    pgn.place(a, kvh, NT * (have + WT), rend, lane, bad);
     load_k(NT * wave);
     load_v(NT * wave);
   }
@@ -315,7 +328,8 @@ __global__ __launch_bounds__(64 * PG_W, 2) void k_paged_rows(PagedArgs a) {
     if (more && next >= have + WT) {
       have += WT;
       pg = pgn;
-      pgn.load(a, s, kvh, NT * (have + WT), rend, lane, bad);
+      pgn.fetch(a, s, NT * (have + WT), lane);
+      pgn.place(a, kvh, NT * (have + WT), rend, lane, bad);
     }
     const int lane0 = NT * (next - have);
     const int k0 = tile * PG_K;
@@ -468,12 +482,12 @@ __global__ __launch_bounds__(64 * PG_W, 2) void k_paged_rows(PagedArgs a) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) y[e] += f * v[e];
     }
-    const int r = rtile.row0 + row, tok = r / a.group, p = p0 + tok;
+    const int p = rtile.pos(row);
     if (nsp == 1) {
       const float inv = 1.f / l;
 #pragma unroll
       for (int e = 0; e < 4; ++e) y[e] = row_result(y[e], inv, p, bad);
-      store4<F16>((uint16_t*)a.O + (size_t)(rtile.sp.r0 + tok) * a.ldo + (size_t)(kvh * a.group + r % a.group) * DH + d, y);
+      store4<F16>((uint16_t*)a.O + (size_t)(rtile.sp.r0 + rtile.tok(row)) * a.ldo + (size_t)(kvh * a.group + rtile.head(row)) * DH + d, y);
     } else {
       // A split that met a bad page leaves NaN, which the join keeps.
       const size_t at = ((((size_t)s * a.kv.kv_heads + kvh) * a.tiles + rt) * a.nsplit + split) * a.prows + row;
@@ -535,8 +549,9 @@ __global__ __launch_bounds__(64 * PG_W, 2) void k_paged_tile(PagedArgs a) {
   w /= a.tiles;
   const int split = w % a.nsplit;
   w /= a.nsplit;
-  const int s = by_length(a.kv, w % a.kv.nseq, threadIdx.x & 63), kvh = w / a.kv.nseq;
-  const RowTile rtile = row_tile(a, s, rt);
+  KvSpan sp;
+  const int s = by_length(a.kv, w % a.kv.nseq, threadIdx.x & 63, sp), kvh = w / a.kv.nseq;
+  const RowTile rtile = row_tile(a, sp, rt);
   if (rtile.nrows <= 0) return;
   const int nsp = splits_of(a, rtile.kend);
   if (split >= nsp) return;
@@ -544,25 +559,27 @@ __global__ __launch_bounds__(64 * PG_W, 2) void k_paged_tile(PagedArgs a) {
   const int t0 = (int)((long long)ntiles * split / nsp), t1 = (int)((long long)ntiles * (split + 1) / nsp);
   const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int p0 = rtile.sp.len - rtile.sp.n;
   const int wr0 = 16 * PT_NG * wave;  // the wave's first row in the tile
 
+  Runs<E8> pg, pgn;
+  int win = t0 >> 4;
+  pg.fetch(a, s, 64 * win, lane);
+  pgn.fetch(a, s, 64 * (win + 1), lane);
   // Rows as B operands of S^T, in the order of K's fragments (see k_paged_rows).
   int pos[PT_NG];
   bf16x8 qf[PT_NG][KS];
 #pragma unroll
   for (int gq = 0; gq < PT_NG; ++gq) {
-    const int r = rtile.row0 + min(wr0 + 16 * gq + l16, rtile.nrows - 1);
-    const int tok = r / a.group;
-    pos[gq] = p0 + tok;
-    const uint16_t* qp = (const uint16_t*)a.Q + (size_t)(rtile.sp.r0 + tok) * a.ldq + (size_t)(kvh * a.group + r % a.group) * DH;
+    const int i = min(wr0 + 16 * gq + l16, rtile.nrows - 1);
+    pos[gq] = rtile.pos(i);
+    const uint16_t* qp = (const uint16_t*)a.Q + (size_t)(rtile.sp.r0 + rtile.tok(i)) * a.ldq + (size_t)(kvh * a.group + rtile.head(i)) * DH;
 #pragma unroll
     for (int kk = 0; kk < KS; ++kk)
       qf[gq][kk] = __builtin_bit_cast(bf16x8, *(const u32x4*)(qp + (E8 ? 16 * (g + 4 * (kk >> 1)) + 8 * (kk & 1) : 32 * kk + 8 * g)));
   }
   // Positions of the wave's first and last row.
-  const int wfirst = p0 + (rtile.row0 + min(wr0, rtile.nrows - 1)) / a.group;
-  const int wlast = wr0 < rtile.nrows ? p0 + (rtile.row0 + min(wr0 + 16 * PT_NG, rtile.nrows) - 1) / a.group : -1;
+  const int wfirst = rtile.pos(min(wr0, rtile.nrows - 1));
+  const int wlast = wr0 < rtile.nrows ? rtile.pos(min(wr0 + 16 * PT_NG, rtile.nrows) - 1) : -1;
 
   // P = 2^(s scale + b), b = SHIFT - m scale rounded: its rounding is the same factor for all of a row's P, and
   // from one maximum m to the next the exact b are subtracted.  Where m scale is so large that the rounding
@@ -588,9 +605,7 @@ __global__ __launch_bounds__(64 * PG_W, 2) void k_paged_tile(PagedArgs a) {
   const int drow = (RPB * wave + lane / CPR) & 15;  // of every c
   const unsigned offk = (unsigned)(drow * RB + 16 * ((lane % CPR) ^ swz<RB>(drow)));
   const unsigned offv = (unsigned)(drow * RB + 16 * ((lane % CPR) ^ (VX * swz<RB>(drow))));
-  Runs<E8> pg, pgn;
   float ksp = 0.f, vsp = 0.f;  // 8-bit: the scales of the window before pg's
-  int win = t0 >> 4;
   auto dma = [&](const void* base, int tile, unsigned off, char* dst, int blk) {
 #pragma unroll
     for (int c = 0; c < KCH; ++c) {
@@ -607,7 +622,8 @@ __global__ __launch_bounds__(64 * PG_W, 2) void k_paged_tile(PagedArgs a) {
         vsp = pg.vs;
       }
       pg = pgn;
-      pgn.load(a, s, kvh, 64 * (win + 1), rend, lane, bad);
+      pgn.fetch(a, s, 64 * (win + 1), lane);
+      pgn.place(a, kvh, 64 * (win + 1), rend, lane, bad);
     }
     dma(a.kv.K, tile, offk, dst, KBLK);
   };
@@ -839,11 +855,11 @@ __global__ __launch_bounds__(64 * PG_W, 2) void k_paged_tile(PagedArgs a) {
 
   // Tiles t0 .. tfull - 1 lie wholly before all rows of the workgroup: they overlap with the next one's S.  The
   // last few, which are masked, do not.
-  const int tfull = min(t1, (p0 + rtile.row0 / a.group + 1) / PT_K);
+  const int tfull = min(t1, (rtile.pos(0) + 1) / PT_K);
   int n = t0;
   if (n < t1) {
-    pg.load(a, s, kvh, 64 * win, rend, lane, bad);
-    pgn.load(a, s, kvh, 64 * (win + 1), rend, lane, bad);
+    pg.place(a, kvh, 64 * win, rend, lane, bad);
+    pgn.place(a, kvh, 64 * (win + 1), rend, lane, bad);
     load_k(n, Kb0);
     load_v(n, Vb0);
     if (n + 1 < t1) load_k(n + 1, Kb1);
@@ -936,10 +952,10 @@ __global__ __launch_bounds__(64 * PG_W, 2) void k_paged_tile(PagedArgs a) {
     constexpr int C8 = DH / 8;
 #pragma unroll
     for (int x = lane; x < 16 * C8; x += 64) {
-      const int rr = wr0 + 16 * gq + x / C8, c = x % C8, r = rtile.row0 + rr;
+      const int i = wr0 + 16 * gq + x / C8, c = x % C8;
       const u32x4 v = *(const u32x4*)&ow[(x / C8) * OROW + 8 * c];
-      if (rr < rtile.nrows)
-        *(u32x4*)((uint16_t*)a.O + (size_t)(rtile.sp.r0 + r / a.group) * a.ldo + (size_t)(kvh * a.group + r % a.group) * DH + 8 * c) = v;
+      if (i < rtile.nrows)
+        *(u32x4*)((uint16_t*)a.O + (size_t)(rtile.sp.r0 + rtile.tok(i)) * a.ldo + (size_t)(kvh * a.group + rtile.head(i)) * DH + 8 * c) = v;
     }
   }
 }
@@ -961,7 +977,7 @@ __global__ __launch_bounds__(256) void k_paged_join(PagedArgs a) {
   const int rt = w % a.tiles;
   w /= a.tiles;
   const int kvh = w % a.kv.kv_heads, s = w / a.kv.kv_heads;
-  const RowTile rtile = row_tile(a, s, rt);
+  const RowTile rtile = row_tile(a, kv_span(a.kv, s), rt);
   const int nsp = splits_of(a, rtile.kend);
   if (nsp == 1) return;  // written already
   const bool mine = row < rtile.nrows;
@@ -999,12 +1015,12 @@ __global__ __launch_bounds__(256) void k_paged_join(PagedArgs a) {
       for (int e = 0; e < 4; ++e) y[e] += f * v[e];
     }
   }
-  const int r = rtile.row0 + row, tok = r / a.group, p = rtile.sp.len - rtile.sp.n + tok;
+  const int p = rtile.pos(row);
   const float inv = 1.f / l;
   float o[4];
 #pragma unroll
   for (int e = 0; e < 4; ++e) o[e] = row_result(y[e], inv, p, 0x7fffffff);
-  store4<F16>((uint16_t*)a.O + (size_t)(rtile.sp.r0 + tok) * a.ldo + (size_t)(kvh * a.group + r % a.group) * DH + d, o);
+  store4<F16>((uint16_t*)a.O + (size_t)(rtile.sp.r0 + rtile.tok(row)) * a.ldo + (size_t)(kvh * a.group + rtile.head(row)) * DH + d, o);
 }
 
 }  // namespace
@@ -1018,6 +1034,7 @@ int zo_paged_attention_launch(const KvArgs& kv, const void* Q, long long ldq, vo
   a.ldq = ldq;
   a.ldo = ldo;
   a.group = kv.heads / kv.kv_heads;
+  a.inv_group = a.group > 1 ? (uint32_t)((1ull << 32) / (unsigned)a.group) + 1 : 0;
   a.scale_log2 = 1.4426950408889634f / sqrtf((float)kv.dh);
   const long long all_rows = (long long)kv.max_q * a.group;
   // Up to 32 rows a sequence and key head read the keys once and little else; more share staged tiles.
