@@ -25,6 +25,7 @@ namespace {
 
 constexpr int PG_W = 4;    // waves per workgroup
 constexpr int PG_K = 32;   // keys per tile
+constexpr int PG_K8 = 64;  // and of 8-bit caches, as many bytes (61 sequences of up to 8192 keys: 121 -> 113 us)
 constexpr float PG_LOW = -3.4028234663852886e38f;  // below every logit but -infinity
 
 struct PagedArgs {
@@ -223,7 +224,8 @@ __device__ __forceinline__ void store4(uint16_t* dst, const float* y) {
 
 template <bool F16, bool E8, int DH, int NG>
 __global__ __launch_bounds__(64 * PG_W, 2) void k_paged_rows(PagedArgs a) {
-  constexpr int NT = PG_K / 16;            // 16-key tiles
+  constexpr int KT = E8 && NG == 1 ? PG_K8 : PG_K;  // keys per tile
+  constexpr int NT = KT / 16;              // 16-key tiles
   constexpr int KS = DH / 32;              // k steps of Q K^T
   constexpr int DT = DH / 16;              // 16-dim tiles of O
   constexpr int EB = E8 ? 1 : 2;           // bytes of a cached value
@@ -232,7 +234,7 @@ __global__ __launch_bounds__(64 * PG_W, 2) void k_paged_rows(PagedArgs a) {
   constexpr bool PF16 = F16 && !E8;        // type of the P V product
   constexpr float SHIFT = PF16 ? 12.f : 0.f;  // P = 2^(.. + SHIFT): keeps fp16 low parts normal
   constexpr int OROW = DH + 4;             // LDS row of the joined O (fp32)
-  constexpr int VBYTES = PG_W * PG_K * VROW * 2, OBYTES = PG_W * 16 * NG * OROW * 4;
+  constexpr int VBYTES = PG_W * KT * VROW * 2, OBYTES = PG_W * 16 * NG * OROW * 4;
   __shared__ __attribute__((aligned(16))) char lds[VBYTES > OBYTES ? VBYTES : OBYTES];
   __shared__ float2 stats[PG_W][16 * NG];
   __shared__ int bads[PG_W];
@@ -242,12 +244,14 @@ __global__ __launch_bounds__(64 * PG_W, 2) void k_paged_rows(PagedArgs a) {
   w /= a.nsplit;
   const int rt = w % a.tiles;
   w /= a.tiles;
-  const int kvh = w % a.kv.kv_heads, s = w / a.kv.kv_heads;
-  const RowTile rtile = row_tile(a, kv_span(a.kv, s), rt);
+  const int kvh = w % a.kv.kv_heads;
+  KvSpan sp;
+  const int s = by_length(a.kv, w / a.kv.kv_heads, threadIdx.x & 63, sp);
+  const RowTile rtile = row_tile(a, sp, rt);
   if (rtile.nrows <= 0) return;
   const int nsp = splits_of(a, rtile.kend);
   if (split >= nsp) return;
-  const int ntiles = (rtile.kend + PG_K - 1) / PG_K;
+  const int ntiles = (rtile.kend + KT - 1) / KT;
   const int t0 = (int)((long long)ntiles * split / nsp), t1 = (int)((long long)ntiles * (split + 1) / nsp);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, g = lane >> 4;
 
@@ -276,7 +280,7 @@ __global__ __launch_bounds__(64 * PG_W, 2) void k_paged_rows(PagedArgs a) {
     lsum[gq] = 0.f;
   }
   int bad = kv_cap(a.kv);
-  uint16_t* const vs = (uint16_t*)lds + wave * PG_K * VROW;
+  uint16_t* const vs = (uint16_t*)lds + wave * KT * VROW;
   const int rend = (rtile.kend + 15) >> 4;
 
   // The run window at hand (64 runs, the tiles from `have` on) and the one after it, on its way.
@@ -332,7 +336,7 @@ __global__ __launch_bounds__(64 * PG_W, 2) void k_paged_rows(PagedArgs a) {
       pgn.place(a, kvh, NT * (have + WT), rend, lane, bad);
     }
     const int lane0 = NT * (next - have);
-    const int k0 = tile * PG_K;
+    const int k0 = tile * KT;
     f32x4 st[NG][NT];
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
@@ -358,7 +362,7 @@ __global__ __launch_bounds__(64 * PG_W, 2) void k_paged_rows(PagedArgs a) {
     if (more) load_k(lane0);
     // Keys that a row does not see; those behind the sequence are also cleared from V, where they may be
     // NaN.
-    const bool mask = k0 + PG_K > pfirst + 1;
+    const bool mask = k0 + KT > pfirst + 1;
     uint32_t odd = 0;  // V of the tile is not finite
     if (mask) {
 #pragma unroll
@@ -428,24 +432,34 @@ __global__ __launch_bounds__(64 * PG_W, 2) void k_paged_rows(PagedArgs a) {
         bl[c][gq] = __builtin_bit_cast(bf16x8, lp);
       }
     }
-    const bool clean = __builtin_expect(__ballot(odd != 0) != 0, 0);
-    if (clean) add_odd_values<PF16, false, DT, NG>([&](int key, int d) { return &vs[key * VROW + d]; }, k0, PG_K, g, pos, o);
     // Lane group g's k slots are keys 32 c + 4 g + (0..3) and 32 c + 16 + 4 g + (0..3).
+    auto pv = [&](bool clean) {
 #pragma unroll
-    for (int c = 0; c < NT / 2; ++c) {
-      const uint16_t* vb = &vs[(32 * c + 4 * g + (l16 >> 2)) * VROW + 4 * (l16 & 3)];
+      for (int c = 0; c < NT / 2; ++c) {
+        const uint16_t* vb = &vs[(32 * c + 4 * g + (l16 >> 2)) * VROW + 4 * (l16 & 3)];
 #pragma unroll
-      for (int t = 0; t < DT; ++t) {
-        const u32x2 v0 = ds_read_tr(vb + 16 * t), v1 = ds_read_tr(vb + 16 * VROW + 16 * t);
-        u32x4 av = {v0[0], v0[1], v1[0], v1[1]};
-        if (clean) av = (u32x4){finite_pair<PF16>(av[0]), finite_pair<PF16>(av[1]), finite_pair<PF16>(av[2]), finite_pair<PF16>(av[3])};
-        const bf16x8 af = __builtin_bit_cast(bf16x8, av);
+        for (int t = 0; t < DT; ++t) {
+          const u32x2 v0 = ds_read_tr(vb + 16 * t), v1 = ds_read_tr(vb + 16 * VROW + 16 * t);
+          u32x4 av = {v0[0], v0[1], v1[0], v1[1]};
+          if (clean)
+            av = (u32x4){finite_pair<PF16>(av[0]), finite_pair<PF16>(av[1]), finite_pair<PF16>(av[2]), finite_pair<PF16>(av[3])};
+          const bf16x8 af = __builtin_bit_cast(bf16x8, av);
 #pragma unroll
-        for (int gq = 0; gq < NG; ++gq) {
-          o[gq][t] = mfma16<PF16>(af, bh[c][gq], o[gq][t]);
-          o[gq][t] = mfma16<PF16>(af, bl[c][gq], o[gq][t]);
+          for (int gq = 0; gq < NG; ++gq) {
+            o[gq][t] = mfma16<PF16>(af, bh[c][gq], o[gq][t]);
+            o[gq][t] = mfma16<PF16>(af, bl[c][gq], o[gq][t]);
+          }
         }
       }
+    };
+    const bool clean = __builtin_expect(__ballot(odd != 0) != 0, 0);
+    if (clean) add_odd_values<PF16, false, DT, NG>([&](int key, int d) { return &vs[key * VROW + d]; }, k0, KT, g, pos, o);
+    // Two copies of P V, without a branch at each fragment, where the registers allow it.
+    if constexpr (NG == 1) {
+      if (clean) pv(true);
+      else pv(false);
+    } else {
+      pv(clean);
     }
   }
 
@@ -1037,18 +1051,21 @@ int zo_paged_attention_launch(const KvArgs& kv, const void* Q, long long ldq, vo
   a.inv_group = a.group > 1 ? (uint32_t)((1ull << 32) / (unsigned)a.group) + 1 : 0;
   a.scale_log2 = 1.4426950408889634f / sqrtf((float)kv.dh);
   const long long all_rows = (long long)kv.max_q * a.group;
-  // Up to 32 rows a sequence and key head read the keys once and little else; more share staged tiles.
-  const bool many = all_rows > 32;
-  const int ng = all_rows > 16 ? 2 : 1;
+  // Few rows of a sequence and key head read its keys and little else; more share staged tiles.  From 17 to 32 rows
+  // (61 sequences of up to 8192 keys, 20 rows) the staged tiles took 218 us in 16 bits where 32-row workgroups took
+  // 290; in 8 bits, where a staged tile is half as many bytes under way, 202 against 131.
+  const bool many = all_rows > (kv.e8 ? 32 : 16);
+  const int ng = many || all_rows > 16 ? 2 : 1;
   a.rt_rows = many ? PT_Q : 16 * ng;
   a.prows = (int)(all_rows < a.rt_rows ? all_rows : a.rt_rows);
   const long long tiles = (all_rows + a.rt_rows - 1) / a.rt_rows;
   const long long units = (long long)kv.nseq * kv.kv_heads * tiles;
   const long long keys = (long long)kv.max_pages << kv.log2ps;
-  a.min_keys = 256;
+  // Splits: as many as give 512 workgroups, two per CU (at least that where a split's rows are few).  With 128 units or more a split has 2048 keys at least, for
+  // it costs a partial result (32 sequences of 2000 keys, 8 key heads: 51 us, in halves 55); with fewer, 256.
+  a.min_keys = units < 128 ? 256 : 2048;
   const long long most = (keys + a.min_keys - 1) / a.min_keys;
-  long long split = (many ? 512 : 1024) / units;
-  if (!many && split < (keys + 2047) / 2048) split = (keys + 2047) / 2048;
+  long long split = ((many && tiles > 1 ? 0 : units - 1) + 512) / units;
   if (split > 64) split = 64;
   if (split > most) split = most;
   if (split < 1) split = 1;
@@ -1068,9 +1085,9 @@ int zo_paged_attention_launch(const KvArgs& kv, const void* Q, long long ldq, vo
   }
   const dim3 grid((unsigned)(units * split)), block(64 * PG_W);
   const bool f16 = kv.dtype == ZO_F16;
-#define ZO_ROWS(F, E, D)                                                                          \
-  if (many) hipLaunchKernelGGL((k_paged_tile<F, E, D>), grid, block, 0, stream, a);              \
-  else if (ng == 2) hipLaunchKernelGGL((k_paged_rows<F, E, D, 2>), grid, block, 0, stream, a);   \
+#define ZO_ROWS(F, E, D)                                                                                    \
+  if (many) hipLaunchKernelGGL((k_paged_tile<F, E, D>), grid, block, 0, stream, a);                        \
+  else if (E && ng == 2) hipLaunchKernelGGL((k_paged_rows<F, E, D, E ? 2 : 1>), grid, block, 0, stream, a); \
   else hipLaunchKernelGGL((k_paged_rows<F, E, D, 1>), grid, block, 0, stream, a)
 #define ZO_ROWS_D(F, E) \
   if (kv.dh == 64) { ZO_ROWS(F, E, 64); } \

@@ -22,7 +22,7 @@ def test_single_tokens(ps, heads, kvh, dh, dt, cache):
     rng = np.random.default_rng(ps + heads)
     for seqs in (True, False):
         got, ref, mag = attend(rng, dt, lens, [1] * len(lens), ps, heads, kvh, dh, cache, seqs=seqs, rows_behind=2)
-        check_attention(got, ref, mag, dt, (ps, heads, seqs))
+        check_attention(got, ref, mag, dt, (ps, heads, seqs), many([1], heads, kvh, cache), cache)
 
 
 @pytest.mark.parametrize("cache", ["same", "e4m3"])
@@ -39,7 +39,7 @@ def test_single_tokens(ps, heads, kvh, dh, dt, cache):
 def test_pieces(news, lens, ps, heads, kvh, dh, dt, cache):
     rng = np.random.default_rng(sum(lens) + heads)
     got, ref, mag = attend(rng, dt, lens, news, ps, heads, kvh, dh, cache, pad=8, rows_behind=1)
-    check_attention(got, ref, mag, dt, (news, heads), many(news, heads, kvh), cache)
+    check_attention(got, ref, mag, dt, (news, heads), many(news, heads, kvh, cache), cache)
 
 
 @pytest.mark.parametrize("cache", ["same", "e4m3"])
@@ -54,7 +54,7 @@ def test_long_contexts(heads, kvh, dh, news, lens, ps, width, cache):
     rng = np.random.default_rng(lens[0])
     for dt in ("bf16", "f16"):
         got, ref, mag = attend(rng, dt, lens, news, ps, heads, kvh, dh, cache, width=width, spread=2.0)
-        check_attention(got, ref, mag, dt, (lens, dt), many(news, heads, kvh), cache)
+        check_attention(got, ref, mag, dt, (lens, dt), many(news, heads, kvh, cache), cache)
 
 
 @pytest.mark.parametrize("shape", ["rise", "fall", "large"])
@@ -120,14 +120,14 @@ def test_values_that_are_not_finite_stay_with_the_rows_that_see_them(news, heads
             from oracle import paged as op
             ref, mag = op.paged_attention(Qv.reshape(news[0], heads, dh), clean, table, q_start, kv_len)
             sees = np.arange(first, n) >= where
-            check_attention(got[~sees], ref[~sees], mag[~sees], "bf16", (tensor, bad, where), many(news, heads, 1))
+            check_attention(got[~sees], ref[~sees], mag[~sees], "bf16", (tensor, bad, where), many(news, heads, 1, cache), cache)
             if tensor == "k":
                 assert np.all(np.isnan(got[sees]))
             else:
                 assert np.all(np.isnan(got[sees][..., 5]) if np.isnan(bad) else got[sees][..., 5] == np.inf)
                 rest = np.arange(dh) != 5
                 check_attention(got[sees][..., rest], ref[sees][..., rest], mag[sees][..., rest], "bf16", (tensor, bad, where),
-                                many(news, heads, 1))
+                                many(news, heads, 1, cache), cache)
 
 
 def _call(table, kv_len, q_start, max_q, pages=6, ps=16, rows=12, heads=2, dh=64):
