@@ -2,8 +2,12 @@
 // what a layer of the LLaMA family does between its q, k, v products and its attention when it
 // answers token by token (the rotation of zo_rope, at positions that are not 0, 1, ...).
 //
-// A row's angles are the same for all its heads: a team of waves forms the dh / 2 sines and cosines
-// of a row once, in LDS, and then turns every head of Q and K and copies V with 16-byte accesses.
+// Bound by the bytes of Q, K and V in and out, or by the latency of a few dependent loads (a length, a page, the
+// row).  A row's angles are the same for all its heads, so a workgroup takes (a part of) one row: 256 items of
+// 16 bytes copied or 32 turned, one per thread, loaded before its first waves form the row's dh / 2 sines and
+// cosines in LDS.  One row per wave instead, eight items after one another, took 37 us where this takes 29 (16 prompts
+// of up to 512 rows, 40 query and 8 key heads of 128: 5.1 TB/s), and a workgroup per whole row 38.
+// The 8-bit form: a wave takes one page of one head and tensor, for which it needs the largest magnitude first.
 #include "zo_attn.h"
 #include "zo_kv.h"
 
@@ -14,10 +18,10 @@ struct AppendArgs {
   const void *Q, *K, *V;
   void* Qo;
   long long ldq, ldqo, ldk, ldv;
-  double k;    // log2 of the frequency of dimension 1: -2 log2(base) / dh; 0: no rotation
-  int tiles;   // workgroups along a sequence (16-bit), pages of a sequence (8-bit)
-  int parts;   // workgroups per row (16-bit), head groups (8-bit)
-  int qblocks; // 8-bit: workgroups that rotate Q, before those of the pages
+  double k;     // log2 of the frequency of dimension 1: -2 log2(base) / dh; 0: no rotation
+  int parts;    // workgroups per row
+  int pages, groups;  // 8-bit: pages that max_q positions touch at most, workgroups (pairs of heads) per page
+  int qblocks;  // 8-bit: workgroups that rotate Q, before those of the pages
 };
 
 // Sine and cosine of `turns` full turns: the nearest quarter turn is taken off in fp64, the rest
@@ -54,74 +58,78 @@ __device__ __forceinline__ void rotate8(float* a, float* b, const float2* cs) {
   }
 }
 
-// Fills t[i] = (cos, sin) of row position p, i = first, first + step, ... < half.
-__device__ __forceinline__ void fill_turns(float2* t, int half, int first, int step, int p, double k) {
-  for (int i = first; i < half; i += step) {
-    float sn, cs;
-    turn((double)p * (exp2((double)i * k) * kInv2Pi), sn, cs);
-    t[i] = make_float2(cs, sn);
+// Eight 16-bit values widened.
+template <int DT>
+__device__ __forceinline__ void widen(u32x4 w, float* v) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    v[2 * e] = unpk<DT == ZO_F16>(w[e], 0);
+    v[2 * e + 1] = unpk<DT == ZO_F16>(w[e], 1);
   }
 }
 
-// Row `row` of the call: items y = 0 .. heads dh / 16 - 1 turn Q, the next kv_heads dh / 16 turn K,
-// the rest copy V (without a rotation: K, then V) into slot `slot` of the cache, in elements of
-// head 0's page (-1: not stored).
-template <int DT, int WPT>
-__device__ __forceinline__ void append_rows(const AppendArgs& a, int s, int tile, int part, float2 (*turns)[64]) {
-  const int dh = a.kv.dh, half = dh / 2, TB = 4 / WPT;
+// New row i of sequence s, items 256 part .. + 255: the first heads dh / 16 turn Q, the next kv_heads dh / 16 turn
+// K, the rest copy V (without a rotation: K, then V) into the row's slot of the cache.  KV: else Q alone.
+template <int DT, bool KV>
+__device__ __forceinline__ void append_row(const AppendArgs& a, int s, int i, int part, float2* turns) {
+  const int dh = a.kv.dh, half = dh / 2;
   const KvSpan sp = kv_span(a.kv, s);
-  const int nq = min(sp.n, a.kv.max_q);
-  if (tile * TB >= nq) return;
-  const int team = threadIdx.x / (64 * WPT), tl = threadIdx.x % (64 * WPT);
-  const int i = tile * TB + team;
-  const bool mine = i < nq;
-  const int p = sp.len - sp.n + i, pr = max(p, 0);
-  if (a.k != 0.0 && mine) fill_turns(turns[team], half, tl, 64 * WPT, pr, a.k);
-  long long slot = -1;  // element of head 0 in the cache
-  if (mine && p >= 0 && a.kv.K) {
+  if (i >= min(sp.n, a.kv.max_q)) return;
+  const int p = sp.len - sp.n + i;
+  const long long row = sp.r0 + i;
+  const bool rot = a.k != 0.0;
+  const int cph = dh / 16, lcph = dh == 128 ? 3 : 2;  // rotated chunks (8 pairs) per head
+  const int nq = rot && a.Q ? a.kv.heads * cph : 0, nk = KV ? a.kv.kv_heads * cph : 0;
+  const int n_rot = nq + (rot ? nk : 0), n_all = n_rot + (rot ? 2 * nk : 4 * nk);
+  const int y = part * 256 + threadIdx.x;
+  // What this thread turns (isq: of Q, else of K) or copies (isk: K, else V): item x of it.
+  const bool turned = y < n_rot, isq = y < nq, isk = turned || (!rot && y < 2 * nk);
+  const int x = turned ? (isq ? y : y - nq) : y - n_rot - (rot || isk ? 0 : 2 * nk);
+  const uint16_t* src = (const uint16_t*)(isq ? a.Q : isk ? a.K : a.V) + row * (isq ? a.ldq : isk ? a.ldk : a.ldv);
+  u32x4 u = {0, 0, 0, 0}, v = {0, 0, 0, 0};
+  if (turned) {
+    src += (x >> lcph) * dh + 8 * (x & (cph - 1));
+    u = *(const u32x4*)src;
+    v = *(const u32x4*)(src + half);
+  } else if (y < n_all) {
+    u = *(const u32x4*)(src + 8 * x);
+  }
+  if (rot) {
+    if ((int)threadIdx.x < half) {
+      float sn, cs;
+      turn((double)max(p, 0) * (exp2((double)threadIdx.x * a.k) * kInv2Pi), sn, cs);
+      turns[threadIdx.x] = make_float2(cs, sn);
+    }
+  }
+  long long slot = -1;  // element of head 0 in the cache; -1: the row is not stored
+  if (KV && p >= 0) {
     const int page = kv_page(a.kv, s, p >> a.kv.log2ps);
     if (page >= 0) slot = ((((long long)page * a.kv.kv_heads) << a.kv.log2ps) + (p & ((1 << a.kv.log2ps) - 1))) * dh;
     else if (a.kv.bad_flag) *a.kv.bad_flag = 1;
   }
-  __syncthreads();
-  if (!mine) return;
-  const long long row = sp.r0 + i;
-  const bool rot = a.k != 0.0;
-  const int cph = dh / 16;  // rotated chunks (8 pairs) per head
-  const int nq_items = rot && a.Q ? a.kv.heads * cph : 0, nk = a.kv.K ? a.kv.kv_heads * cph : 0;
-  const int n_rot = nq_items + (rot ? nk : 0), n_all = n_rot + (rot ? 2 * nk : 4 * nk);
-  const int lcph = dh == 128 ? 3 : 2;
+  if (rot) __syncthreads();
   const long long hstride = (long long)dh << a.kv.log2ps;
-  for (int y = part * 64 * WPT + tl; y < n_all; y += a.parts * 64 * WPT) {
-    if (y < n_rot) {
-      const bool isq = y < nq_items;
-      const int x = isq ? y : y - nq_items;
-      const int h = x >> lcph, c = x & (cph - 1);
-      const size_t src = (isq ? row * a.ldq : row * a.ldk) + (size_t)h * dh + 8 * c;
-      float u[8], v[8];
-      load8<DT>(isq ? a.Q : a.K, src, u);
-      load8<DT>(isq ? a.Q : a.K, src + half, v);
-      rotate8(u, v, &turns[team][8 * c]);
-      if (!isq && slot < 0) continue;
-      const size_t dst = isq ? (size_t)(row * a.ldqo) + (size_t)h * dh + 8 * c : (size_t)(slot + h * hstride) + 8 * c;
-      store8<DT>(isq ? a.Qo : a.kv.K, dst, u);
-      store8<DT>(isq ? a.Qo : a.kv.K, dst + half, v);
-    } else if (slot >= 0) {
-      const int x = y - n_rot;
-      const bool isk = !rot && x < 2 * nk;
-      const int z = !rot && !isk ? x - 2 * nk : x;
-      const int h = z >> (lcph + 1), c = z & (2 * cph - 1);
-      const uint16_t* src = (const uint16_t*)(isk ? a.K : a.V) + (isk ? row * a.ldk : row * a.ldv) + (size_t)h * dh + 8 * c;
-      *(u32x4*)((uint16_t*)(isk ? a.kv.K : a.kv.V) + (size_t)(slot + h * hstride) + 8 * c) = *(const u32x4*)src;
-    }
+  if (turned) {
+    const int h = x >> lcph, c = x & (cph - 1);
+    float f[8], g[8];
+    widen<DT>(u, f);
+    widen<DT>(v, g);
+    rotate8(f, g, &turns[8 * c]);
+    if (!isq && slot < 0) return;
+    const size_t dst = isq ? (size_t)(row * a.ldqo) + (size_t)h * dh + 8 * c : (size_t)(slot + h * hstride) + 8 * c;
+    store8<DT>(isq ? a.Qo : a.kv.K, dst, f);
+    store8<DT>(isq ? a.Qo : a.kv.K, dst + half, g);
+  } else if (y < n_all && slot >= 0) {
+    const int h = x >> (lcph + 1), c = x & (2 * cph - 1);
+    *(u32x4*)((uint16_t*)(isk ? a.kv.K : a.kv.V) + (size_t)(slot + h * hstride) + 8 * c) = u;
   }
 }
 
-template <int DT, int WPT>
+template <int DT, bool KV>
 __global__ __launch_bounds__(256) void k_kv_append(AppendArgs a) {
-  __shared__ float2 turns[4][64];
+  __shared__ float2 turns[64];
   const int w = blockIdx.x, part = w % a.parts, t = w / a.parts;
-  append_rows<DT, WPT>(a, t / a.tiles, t % a.tiles, part, turns);
+  append_row<DT, KV>(a, t / a.kv.max_q, t % a.kv.max_q, part, turns);
 }
 
 // ---------------------------------------------------------------- 8-bit cache
@@ -152,116 +160,125 @@ __device__ __forceinline__ u32x2 codes8(const float* v, float inv) {
   return (u32x2){codes4(x), codes4(x + 4)};
 }
 
-// One page of one sequence, for the head group `part`: wave w takes tensor w & 1 (K, V) of heads
-// w >> 1, w >> 1 + 2, ... of the group.  Two passes over the page's new rows (the largest magnitude,
-// then the codes; the second reads them from the caches), and one over its earlier slots where the
-// scale grows.
-template <int DT>
+// One page of one sequence, heads 2 part and 2 part + 1: wave w takes tensor w & 1 (K, V) of head w >> 1.  Two passes
+// over the page's new rows, the largest magnitude and then the codes (the second reads the rows from the caches: held
+// in registers, they left room for half as many waves, and 16 prompts of 512 rows, 8 heads of 128, took 94 us
+// where this takes 57), and one over its earlier slots where the scale grows.
+template <int DT, int DH, bool ROT>
 __device__ __forceinline__ void append_page8(const AppendArgs& a, int s, int jpage, int part, float2 (*turns)[64]) {
   const KvArgs& kv = a.kv;
-  const int dh = kv.dh, half = dh / 2, ps = 1 << kv.log2ps, cph = dh / 16;
+  constexpr int half = DH / 2, CPH = DH / 16, UN = 2;  // chunks of 8 pairs of a row; items of a lane loaded together
+  const int ps = 1 << kv.log2ps;
   const KvSpan sp = kv_span(kv, s);
-  const int p0 = sp.len - sp.n;                                // position of the sequence's row 0
-  const int pend = min(p0 + min(sp.n, kv.max_q), kv_cap(kv));  // positions stored end here
+  const int p0 = sp.len - sp.n;  // position of the sequence's row 0
+  const int plast = p0 + min(sp.n, kv.max_q), pend = min(plast, kv_cap(kv));  // positions stored end at pend
   const int pbeg = max(p0, 0);
   const int j = (pbeg >> kv.log2ps) + jpage;
   const int lo = max(pbeg, j << kv.log2ps), hi = min(pend, (j + 1) << kv.log2ps);
-  if (jpage == 0 && part == 0 && threadIdx.x == 0 && kv.bad_flag && p0 + min(sp.n, kv.max_q) > kv_cap(kv)) *kv.bad_flag = 1;
+  if (jpage == 0 && part == 0 && threadIdx.x == 0 && kv.bad_flag && plast > kv_cap(kv)) *kv.bad_flag = 1;
   if (lo >= hi) return;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int nt = hi - lo, old = lo & (ps - 1);
+  const int h = 2 * part + (wave >> 1);
+  const bool isk = (wave & 1) == 0, mine = h < kv.kv_heads;
+  const uint16_t* src = (const uint16_t*)(isk ? a.K : a.V) + (size_t)h * DH;
+  const long long ld = isk ? a.ldk : a.ldv, row0 = sp.r0 + (lo - p0);
   const int page = kv_page(kv, s, j);
-  if (page < 0) {
+  if (page < 0) {  // of all waves
     if (kv.bad_flag && threadIdx.x == 0) *kv.bad_flag = 1;
     return;
   }
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const int nt = hi - lo, old = lo & (ps - 1);
-  const int hper = (kv.kv_heads + a.parts - 1) / a.parts;
-  const int h0 = part * hper, h1 = min(h0 + hper, kv.kv_heads);
-  const int lcph = dh == 128 ? 3 : 2;
-  const bool rot = a.k != 0.0;
-  const bool isk = (wave & 1) == 0;
-  const double theta = rot ? exp2((double)(threadIdx.x & (half - 1)) * a.k) * kInv2Pi : 0.0;
-  const long long row0 = sp.r0 + (lo - p0);
-  const uint16_t* src = (const uint16_t*)(isk ? a.K : a.V);
-  const long long ld = isk ? a.ldk : a.ldv;
-  // Heads in steps of 2; the rows in chunks of 64, whose turns fit LDS.  All waves take the same
-  // steps, so that they meet at the barriers.
-  for (int hb = h0; hb < h1; hb += 2) {
-    const int h = hb + (wave >> 1);
-    const bool mine = h < h1;
-    float amax = 0.f, inv = 0.f;
-    uint8_t* base = (uint8_t*)(isk ? kv.K : kv.V) + ((((size_t)page * kv.kv_heads + (mine ? h : 0)) << kv.log2ps) * dh);
-    for (int pass = 0; pass < 2; ++pass) {
-      for (int c0 = 0; c0 < nt; c0 += 64) {
-        const int cn = min(64, nt - c0);
-        if (rot && (nt > 64 || (hb == h0 && pass == 0))) {
-          __syncthreads();  // the chunk before has been used
-          for (int t = threadIdx.x / half; t < cn; t += 256 / half) {
-            float sn, cs;
-            turn((double)(lo + c0 + t) * theta, sn, cs);
-            turns[t][threadIdx.x & (half - 1)] = make_float2(cs, sn);
-          }
-          __syncthreads();
-        }
-        if (!mine) continue;
-        for (int x = lane; x < cn * cph; x += 64) {
-          const int t = x >> lcph, c = x & (cph - 1);
-          const size_t at = (size_t)((row0 + c0 + t) * ld) + (size_t)h * dh + 8 * c;
-          float u[8], v[8];
-          load8<DT>(src, at, u);
-          load8<DT>(src, at + half, v);
-          if (rot && isk) rotate8(u, v, &turns[t][8 * c]);
-          if (pass == 0) {
+  const size_t head = (size_t)page * kv.kv_heads + (mine ? h : 0);
+  float* const sc = (isk ? kv.ks : kv.vs) + head;
+  uint8_t* const base = (uint8_t*)(isk ? kv.K : kv.V) + ((head << kv.log2ps) * DH);
+  const float was = old > 0 ? *sc : 0.f;
+  const double theta = ROT ? exp2((double)(threadIdx.x & (half - 1)) * a.k) * kInv2Pi : 0.0;
+  float amax = 0.f, inv = 0.f;
+#pragma unroll 1
+  for (int pass = 0; pass < 2; ++pass) {
+    // 64 rows at a time: their turns fit LDS (and serve both passes where they are all).
+    for (int c0 = 0; c0 < nt; c0 += 64) {
+      const int cn = min(64, nt - c0), items = mine ? cn * CPH : 0;
+      u32x4 u[UN], v[UN];
+      auto load = [&](int x0) {  // item x: chunk x % CPH of row x / CPH
 #pragma unroll
-            for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fmaxf(finite_abs(u[e]), finite_abs(v[e])));
-          } else {
-            uint8_t* dst = base + (size_t)(old + c0 + t) * dh + 8 * c;
-            *(u32x2*)dst = codes8(u, inv);
-            *(u32x2*)(dst + half) = codes8(v, inv);
+        for (int q = 0; q < UN; ++q)
+          if (x0 + 64 * q < items) {
+            const uint16_t* p = src + (row0 + c0 + (x0 + 64 * q) / CPH) * ld + 8 * ((x0 + 64 * q) % CPH);
+            u[q] = *(const u32x4*)p;
+            v[q] = *(const u32x4*)(p + half);
           }
+      };
+      load(lane);
+      if (ROT && (nt > 64 || pass == 0)) {
+        __syncthreads();  // those before have been used
+        for (int t = threadIdx.x / half; t < cn; t += 256 / half) {
+          float sn, cs;
+          turn((double)(lo + c0 + t) * theta, sn, cs);
+          turns[t][threadIdx.x & (half - 1)] = make_float2(cs, sn);
         }
+        __syncthreads();
       }
-      if (pass == 0 && mine) {
+      for (int x0 = lane; x0 < items; x0 += 64 * UN) {
 #pragma unroll
-        for (int off = 32; off > 0; off >>= 1) amax = fmaxf(amax, __shfl_xor(amax, off, 64));
-        float* sc = (isk ? kv.ks : kv.vs) + (size_t)page * kv.kv_heads + h;
-        float to = need_scale(amax);
-        if (old > 0) {
-          const float was = *sc;
-          to = fmaxf(was, to);
-          if (to > was) {
-            const float ratio = was / to;
-            for (int x = lane; x < old * dh / 8; x += 64) {
-              const u32x2 w = *(const u32x2*)(base + 8 * x);
-              float v[8];
+        for (int q = 0; q < UN; ++q) {
+          const int x = x0 + 64 * q;
+          if (x < items) {
+            float f[8], g[8];
+            widen<DT>(u[q], f);
+            widen<DT>(v[q], g);
+            if (ROT && isk) rotate8(f, g, &turns[x / CPH][8 * (x % CPH)]);
+            if (pass == 0) {
 #pragma unroll
-              for (int e = 0; e < 2; ++e) {
-                v[4 * e] = __builtin_amdgcn_cvt_f32_fp8(w[e], 0) * ratio;
-                v[4 * e + 1] = __builtin_amdgcn_cvt_f32_fp8(w[e], 1) * ratio;
-                v[4 * e + 2] = __builtin_amdgcn_cvt_f32_fp8(w[e], 2) * ratio;
-                v[4 * e + 3] = __builtin_amdgcn_cvt_f32_fp8(w[e], 3) * ratio;
-              }
-              *(u32x2*)(base + 8 * x) = (u32x2){codes4(v), codes4(v + 4)};
+              for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fmaxf(finite_abs(f[e]), finite_abs(g[e])));
+            } else {
+              uint8_t* dst = base + (size_t)(old + c0 + x / CPH) * DH + 8 * (x % CPH);
+              *(u32x2*)dst = codes8(f, inv);
+              *(u32x2*)(dst + half) = codes8(g, inv);
             }
           }
         }
-        if (lane == 0) *sc = to;
-        inv = 1.f / to;
+        load(x0 + 64 * UN);
       }
+    }
+    if (pass == 0 && mine) {
+#pragma unroll
+      for (int off = 32; off > 0; off >>= 1) amax = fmaxf(amax, __shfl_xor(amax, off, 64));
+      float to = need_scale(amax);
+      if (old > 0) {
+        to = fmaxf(was, to);
+        if (to > was) {
+          const float ratio = was / to;
+          for (int x = lane; x < old * DH / 8; x += 64) {
+            const u32x2 w = *(const u32x2*)(base + 8 * x);
+            float v[8];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              v[4 * e] = __builtin_amdgcn_cvt_f32_fp8(w[e], 0) * ratio;
+              v[4 * e + 1] = __builtin_amdgcn_cvt_f32_fp8(w[e], 1) * ratio;
+              v[4 * e + 2] = __builtin_amdgcn_cvt_f32_fp8(w[e], 2) * ratio;
+              v[4 * e + 3] = __builtin_amdgcn_cvt_f32_fp8(w[e], 3) * ratio;
+            }
+            *(u32x2*)(base + 8 * x) = (u32x2){codes4(v), codes4(v + 4)};
+          }
+        }
+      }
+      if (lane == 0) *sc = to;
+      inv = 1.f / to;
     }
   }
 }
 
-template <int DT>
-__global__ __launch_bounds__(256) void k_kv_append8(AppendArgs a, AppendArgs q) {
-  __shared__ float2 turns[64][64];
+template <int DT, int DH, bool ROT>
+__global__ __launch_bounds__(256, ROT ? 4 : 5) void k_kv_append8(AppendArgs a) {
+  __shared__ float2 turns[ROT ? 64 : 1][64];
   const int w = blockIdx.x;
   if (w < a.qblocks) {
-    const int part = w % q.parts, t = w / q.parts;
-    append_rows<DT, 1>(q, t / q.tiles, t % q.tiles, part, turns);
+    const int part = w % a.parts, t = w / a.parts;
+    append_row<DT, false>(a, t / a.kv.max_q, t % a.kv.max_q, part, turns[0]);
   } else {
-    const int v = w - a.qblocks, part = v % a.parts, t = v / a.parts;
-    append_page8<DT>(a, t / a.tiles, t % a.tiles, part, turns);
+    const int v = w - a.qblocks, part = v % a.groups, t = v / a.groups;
+    append_page8<DT, DH, ROT>(a, t / a.pages, t % a.pages, part, turns);
   }
 }
 
@@ -280,44 +297,47 @@ int zo_kv_append_launch(const KvArgs& kv, const void* Q, long long ldq, void* Q_
   a.ldk = ldk;
   a.ldv = ldv;
   a.k = rope_base > 0.f ? -2.0 * log2((double)rope_base) / (double)kv.dh : 0.0;
-  a.qblocks = 0;
-  const int cph = kv.dh / 16;
   const bool rot = a.k != 0.0;
-  long long wg = 0;
-  if (!kv.e8) {
-    const int items = (rot && Q ? kv.heads * cph : 0) + kv.kv_heads * cph * (rot ? 3 : 4);
-    // Few rows: one row per workgroup, an item per thread; many: one row per wave.
-    const bool few = (long long)kv.nseq * kv.max_q <= 1024;
-    a.tiles = few ? kv.max_q : (kv.max_q + 3) / 4;
-    a.parts = few ? (items + 255) / 256 : 1;
-    wg = (long long)kv.nseq * a.tiles * a.parts;
-    if (wg <= 0x7fffffffLL) {
-      const dim3 grid((unsigned)wg), block(256);
-      if (few) {
-        if (kv.dtype == ZO_BF16) hipLaunchKernelGGL((k_kv_append<ZO_BF16, 4>), grid, block, 0, stream, a);
-        else hipLaunchKernelGGL((k_kv_append<ZO_F16, 4>), grid, block, 0, stream, a);
-      } else {
-        if (kv.dtype == ZO_BF16) hipLaunchKernelGGL((k_kv_append<ZO_BF16, 1>), grid, block, 0, stream, a);
-        else hipLaunchKernelGGL((k_kv_append<ZO_F16, 1>), grid, block, 0, stream, a);
-      }
-      return zo_hip_status(hipGetLastError(), "k_kv_append");
+  const long long rows = (long long)kv.nseq * kv.max_q;
+  const int items = (Q ? kv.heads * (kv.dh / 16) : 0) + (kv.e8 ? 0 : kv.kv_heads * (kv.dh / 16) * (rot ? 3 : 4));
+  a.parts = (items + 255) / 256;
+  a.pages = a.groups = a.qblocks = 0;
+  long long wg = rows * a.parts;
+  const dim3 block(256);
+  int st = ZO_OK;
+  if (kv.e8) {
+    // Q's rows in the pages' launch, or, where they are many, in one of their own: its workgroups need an eighth of
+    // the registers and LDS.
+    const bool apart = rows > 1024;
+    const long long qb = apart ? 0 : wg;
+    a.pages = ((kv.max_q - 1 + (1 << kv.log2ps) - 1) >> kv.log2ps) + 1;
+    a.groups = (kv.kv_heads + 1) / 2;
+    const long long pages = qb + (long long)kv.nseq * a.pages * a.groups;
+    if (pages > 0x7fffffffLL || wg > 0x7fffffffLL) {
+      zo_set_error("kv_append: too many workgroups (%lld)", pages + wg);
+      return ZO_ERR_UNSUPPORTED;
     }
-  } else {
-    AppendArgs q = a;  // the queries' part: nothing is stored in the cache
-    q.kv.K = nullptr;
-    q.tiles = (kv.max_q + 3) / 4;
-    q.parts = 1;
-    const long long qb = Q ? (long long)kv.nseq * q.tiles : 0;
-    a.tiles = ((kv.max_q - 1 + (1 << kv.log2ps) - 1) >> kv.log2ps) + 1;  // pages that max_q positions touch at most
-    a.parts = (kv.kv_heads + 1) / 2;
-    wg = qb + (long long)kv.nseq * a.tiles * a.parts;
-    if (wg <= 0x7fffffffLL) {
-      a.qblocks = (int)qb;
-      const dim3 grid((unsigned)wg), block(256);
-      if (kv.dtype == ZO_BF16) hipLaunchKernelGGL(k_kv_append8<ZO_BF16>, grid, block, 0, stream, a, q);
-      else hipLaunchKernelGGL(k_kv_append8<ZO_F16>, grid, block, 0, stream, a, q);
-      return zo_hip_status(hipGetLastError(), "k_kv_append8");
+    a.qblocks = (int)qb;
+    const dim3 grid((unsigned)pages);
+#define ZO_APPEND8(D, R)                                                                                   \
+  if (kv.dtype == ZO_BF16) hipLaunchKernelGGL((k_kv_append8<ZO_BF16, D, R>), grid, block, 0, stream, a);   \
+  else hipLaunchKernelGGL((k_kv_append8<ZO_F16, D, R>), grid, block, 0, stream, a)
+    if (kv.dh == 64) {
+      if (rot) { ZO_APPEND8(64, true); } else { ZO_APPEND8(64, false); }
+    } else {
+      if (rot) { ZO_APPEND8(128, true); } else { ZO_APPEND8(128, false); }
     }
+#undef ZO_APPEND8
+    st = zo_hip_status(hipGetLastError(), "k_kv_append8");
+    if (st != ZO_OK || !apart || wg == 0) return st;
+    if (kv.dtype == ZO_BF16) hipLaunchKernelGGL((k_kv_append<ZO_BF16, false>), dim3((unsigned)wg), block, 0, stream, a);
+    else hipLaunchKernelGGL((k_kv_append<ZO_F16, false>), dim3((unsigned)wg), block, 0, stream, a);
+    return zo_hip_status(hipGetLastError(), "k_kv_append");
+  }
+  if (wg <= 0x7fffffffLL) {
+    if (kv.dtype == ZO_BF16) hipLaunchKernelGGL((k_kv_append<ZO_BF16, true>), dim3((unsigned)wg), block, 0, stream, a);
+    else hipLaunchKernelGGL((k_kv_append<ZO_F16, true>), dim3((unsigned)wg), block, 0, stream, a);
+    return zo_hip_status(hipGetLastError(), "k_kv_append");
   }
   zo_set_error("kv_append: too many workgroups (%lld)", wg);
   return ZO_ERR_UNSUPPORTED;

@@ -42,9 +42,9 @@ struct PagedArgs {
   float2* stat;                       // its (maximum, sum)
 };
 
-// The splits that a range of `keys` keys is cut into, in whole tiles of `tile` keys.
+// The splits that a range of `keys` keys is cut into.
 __device__ __forceinline__ int splits_of(const PagedArgs& a, int keys) {
-  return min(a.nsplit, max(1, (keys + a.min_keys - 1) / a.min_keys));
+  return keys <= 512 ? 1 : min(a.nsplit, max(1, (keys + a.min_keys - 1) / a.min_keys));
 }
 
 // The sequence that is i-th when every 64 consecutive ones are ordered by their lengths, the longest first
@@ -1062,9 +1062,10 @@ int zo_paged_attention_launch(const KvArgs& kv, const void* Q, long long ldq, vo
   const long long units = (long long)kv.nseq * kv.kv_heads * tiles;
   const long long keys = (long long)kv.max_pages << kv.log2ps;
   // Splits: as many as give 512 workgroups, two per CU (at least that where a split's rows are few).  With 128 units or more a split has 2048 keys at least, for
-  // it costs a partial result (32 sequences of 2000 keys, 8 key heads: 51 us, in halves 55); with fewer, 256.
+  // it costs a partial result (32 sequences of 2000 keys, 8 key heads: 51 us, in halves 55); with fewer, 256, but
+  // up to 512 keys stay whole (300 keys of one sequence: 7.8 us, in halves and a second launch 9.3).
   a.min_keys = units < 128 ? 256 : 2048;
-  const long long most = (keys + a.min_keys - 1) / a.min_keys;
+  const long long most = keys <= 512 ? 1 : (keys + a.min_keys - 1) / a.min_keys;
   long long split = ((many && tiles > 1 ? 0 : units - 1) + 512) / units;
   if (split > 64) split = 64;
   if (split > most) split = most;
