@@ -689,10 +689,13 @@ typedef struct {
  * larger than before, the page's earlier slots are rounded again to the new
  * scale (exact but for values under 2^-6 of it).  Then code = e4m3(x / scale),
  * to nearest even.  Values that are not finite are stored as NaN.
- * One call must not store into one page of one head from two sequences, and no
- * tensor of the call may overlap another but Q_out = Q.
- * Limits: dh = 64 or 128; page_size 16, 32, 64, 128 or 256; ld* % 8 == 0;
- * 16-byte aligned tensors. */
+ * One call must not store into one page from two sequences or through two
+ * entries of the table, and no tensor of the call may overlap another but
+ * Q_out = Q.
+ * Limits: dh = 64 or 128; page_size 16, 32, 64, 128 or 256; ld* % 8 == 0 and
+ * < 2^31; 16-byte aligned tensors; rows <= 2^30; heads, kv_heads <= 2^15;
+ * max_pages page_size <= 2^31 - 4096; num_pages kv_heads page_size / 16,
+ * nseq max_q and a call's workgroups < 2^31. */
 int zo_kv_append(const zo_kv_cache* cache, const zo_kv_batch* batch, int heads,
                  int dtype, const void* Q, long long ldq, void* Q_out,
                  long long ldqo, const void* K, long long ldk, const void* V,
@@ -715,7 +718,8 @@ int zo_kv_append(const zo_kv_cache* cache, const zo_kv_batch* batch, int heads,
  * The workspace holds partial results where a sequence's keys are split over
  * workgroups; its size depends on the host arguments only (0 where nothing is
  * split), and calls that may run at the same time need one each.
- * Limits: those of zo_kv_append; heads % kv_heads == 0. */
+ * Limits: those of zo_kv_append, but nseq kv_heads and max_q heads / kv_heads
+ * (< 2^31 - 4096) for nseq max_q; heads % kv_heads == 0. */
 size_t zo_paged_attention_workspace(const zo_kv_cache* cache,
                                     const zo_kv_batch* batch, int heads,
                                     int dtype);

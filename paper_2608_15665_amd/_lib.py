@@ -536,8 +536,8 @@ def _kv_tensor(t: torch.Tensor, name: str, dtype, here: int) -> int:
 
 
 def _kv_args(dt, rows: int, here: int, k_cache: torch.Tensor, v_cache: torch.Tensor, page_table: torch.Tensor,
-             kv_len: torch.Tensor, q_start: Optional[torch.Tensor], max_q: int, k_scale: Optional[torch.Tensor],
-             v_scale: Optional[torch.Tensor], bad_flag: Optional[torch.Tensor]):
+             kv_len: torch.Tensor, q_start: Optional[torch.Tensor], max_q: Optional[int],
+             k_scale: Optional[torch.Tensor], v_scale: Optional[torch.Tensor], bad_flag: Optional[torch.Tensor]):
     """The checked cache and batch descriptors of a call with `rows` rows of type dt."""
     shape = k_cache.shape
     if len(shape) != 4 or v_cache.shape != shape:
@@ -561,6 +561,10 @@ def _kv_args(dt, rows: int, here: int, k_cache: torch.Tensor, v_cache: torch.Ten
     nseq = kv_len.numel()
     if page_table.dim() != 2 or page_table.shape[0] != nseq:
         raise ValueError(f"page_table must be nseq x max_pages, with nseq = {nseq} of kv_len")
+    if max_q is None:
+        max_q = 1 if q_start is None else rows
+    if not 0 <= max_q < 1 << 31 or page_table.shape[1] >= 1 << 31:  # the descriptors' integers would wrap
+        raise ValueError(f"max_q = {max_q} or max_pages = {page_table.shape[1]} out of range")
     if q_start is not None:
         qs = _kv_tensor(q_start, "q_start", torch.int32, here)
         if q_start.numel() != nseq + 1:
@@ -593,13 +597,14 @@ def _row_tensor(t: torch.Tensor, name: str, dtype, rows: int, cols: int, here: i
 
 
 def kv_append(K: torch.Tensor, V: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor,
-              page_table: torch.Tensor, kv_len: torch.Tensor, q_start: Optional[torch.Tensor] = None, max_q: int = 1,
-              Q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
+              page_table: torch.Tensor, kv_len: torch.Tensor, q_start: Optional[torch.Tensor] = None,
+              max_q: Optional[int] = None, Q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
               rope_base: Optional[float] = None, k_scale: Optional[torch.Tensor] = None,
               v_scale: Optional[torch.Tensor] = None, bad_flag: Optional[torch.Tensor] = None):
     """Appends the rows of K and V (rows x kv_heads dh) to the paged cache (num_pages x kv_heads x page_size
     x dh; the rows' type, or torch.float8_e4m3fn with k_scale and v_scale, num_pages x kv_heads), keys rotated
-    to their positions where rope_base is given.  kv_len counts the new rows.  With Q (rows x heads dh) also
+    to their positions where rope_base is given.  kv_len counts the new rows; max_q is at least the rows of the
+    longest sequence (default: 1 without q_start, else all rows; the nearer, the fewer idle workgroups).  With Q (rows x heads dh) also
     returns the rotated queries (in q_out, or a new tensor).  See zo_kv_append."""
     dt, here = K.dtype, torch._C._cuda_getDevice()
     if dt not in _DT:
@@ -613,7 +618,7 @@ def kv_append(K: torch.Tensor, V: torch.Tensor, k_cache: torch.Tensor, v_cache: 
     ldq = ldqo = heads = 0
     if Q is not None:
         dq = Q.shape[-1]
-        heads = dq // dh
+        heads = dq // max(dh, 1)
         if heads * dh != dq:
             raise ValueError(f"Q must have a multiple of dh = {dh} columns (got {dq})")
         ldq = _row_tensor(Q, "Q", dt, rows, dq, here)
@@ -628,12 +633,12 @@ def kv_append(K: torch.Tensor, V: torch.Tensor, k_cache: torch.Tensor, v_cache: 
 
 
 def paged_attention(Q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, page_table: torch.Tensor,
-                    kv_len: torch.Tensor, q_start: Optional[torch.Tensor] = None, max_q: int = 1,
+                    kv_len: torch.Tensor, q_start: Optional[torch.Tensor] = None, max_q: Optional[int] = None,
                     k_scale: Optional[torch.Tensor] = None, v_scale: Optional[torch.Tensor] = None,
                     out: Optional[torch.Tensor] = None, bad_flag: Optional[torch.Tensor] = None,
                     workspace: Optional[torch.Tensor] = None):
     """Causal attention of the new rows' queries Q (rows x heads dh) over the paged cache that kv_append fills
-    (which holds their own keys and values already).  Rows of `out` behind the last sequence are left as they
+    (which holds their own keys and values already); max_q as for kv_append.  Rows of `out` behind the last sequence are left as they
     are.  The workspace is the stream's own, or under graph capture one of the graph's.  See
     zo_paged_attention."""
     dt, here = Q.dtype, torch._C._cuda_getDevice()

@@ -111,11 +111,17 @@ __device__ __forceinline__ void append_row(const AppendArgs& a, int s, int i, in
   const long long hstride = (long long)dh << a.kv.log2ps;
   if (turned) {
     const int h = x >> lcph, c = x & (cph - 1);
+    if (!isq && slot < 0) return;
+    if (p < 0) {  // padding: its queries are copied
+      uint16_t* dst = (uint16_t*)a.Qo + row * a.ldqo + h * dh + 8 * c;
+      *(u32x4*)dst = u;
+      *(u32x4*)(dst + half) = v;
+      return;
+    }
     float f[8], g[8];
     widen<DT>(u, f);
     widen<DT>(v, g);
     rotate8(f, g, &turns[8 * c]);
-    if (!isq && slot < 0) return;
     const size_t dst = isq ? (size_t)(row * a.ldqo) + (size_t)h * dh + 8 * c : (size_t)(slot + h * hstride) + 8 * c;
     store8<DT>(isq ? a.Qo : a.kv.K, dst, f);
     store8<DT>(isq ? a.Qo : a.kv.K, dst + half, g);
@@ -299,6 +305,10 @@ int zo_kv_append_launch(const KvArgs& kv, const void* Q, long long ldq, void* Q_
   a.k = rope_base > 0.f ? -2.0 * log2((double)rope_base) / (double)kv.dh : 0.0;
   const bool rot = a.k != 0.0;
   const long long rows = (long long)kv.nseq * kv.max_q;
+  if (rows > 0x7fffffffLL) {  // what follows of it stays within 64 bits
+    zo_set_error("kv_append: nseq x max_q = %lld too many", rows);
+    return ZO_ERR_UNSUPPORTED;
+  }
   const int items = (Q ? kv.heads * (kv.dh / 16) : 0) + (kv.e8 ? 0 : kv.kv_heads * (kv.dh / 16) * (rot ? 3 : 4));
   a.parts = (items + 255) / 256;
   a.pages = a.groups = a.qblocks = 0;

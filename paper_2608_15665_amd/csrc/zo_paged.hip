@@ -1058,7 +1058,11 @@ int zo_paged_attention_launch(const KvArgs& kv, const void* Q, long long ldq, vo
   a.group = kv.heads / kv.kv_heads;
   a.inv_group = a.group > 1 ? (uint32_t)((1ull << 32) / (unsigned)a.group) + 1 : 0;
   a.scale_log2 = 1.4426950408889634f / sqrtf((float)kv.dh);
-  const long long all_rows = (long long)kv.max_q * a.group;
+  const long long all_rows = (long long)kv.max_q * a.group, seqs = (long long)kv.nseq * kv.kv_heads;
+  if (all_rows > 0x7fffffffLL - 4096 || seqs > 0x7fffffffLL) {  // what follows of them stays within 64 bits
+    zo_set_error("paged_attention: max_q x heads / kv_heads = %lld or nseq x kv_heads = %lld too many", all_rows, seqs);
+    return ZO_ERR_UNSUPPORTED;
+  }
   // Few rows of a sequence and key head read its keys and little else; more share staged tiles.  From 17 to 32 rows
   // (61 sequences of up to 8192 keys, 20 rows) the staged tiles took 218 us in 16 bits where 32-row workgroups took
   // 290; in 8 bits, where a staged tile is half as many bytes under way, 202 against 131.
@@ -1067,7 +1071,7 @@ int zo_paged_attention_launch(const KvArgs& kv, const void* Q, long long ldq, vo
   a.rt_rows = many ? PT_Q : 16 * ng;
   a.prows = (int)(all_rows < a.rt_rows ? all_rows : a.rt_rows);
   const long long tiles = (all_rows + a.rt_rows - 1) / a.rt_rows;
-  const long long units = (long long)kv.nseq * kv.kv_heads * tiles;
+  const long long units = seqs * tiles;
   const long long keys = (long long)kv.max_pages << kv.log2ps;
   // Splits: as many as give 512 workgroups, two per CU (at least that where a split's rows are few).  With 128 units or more a split has 2048 keys at least, for
   // it costs a partial result (32 sequences of 2000 keys, 8 key heads: 51 us, in halves 55); with fewer, 256, but
@@ -1078,7 +1082,7 @@ int zo_paged_attention_launch(const KvArgs& kv, const void* Q, long long ldq, vo
   if (split > 64) split = 64;
   if (split > most) split = most;
   if (split < 1) split = 1;
-  if (tiles > 0x7fffffffLL || units * split > 0x7fffffffLL || (split > 1 && units * a.prows > 0x7fffffffLL)) {
+  if (units * split > 0x7fffffffLL || (split > 1 && units * a.prows > 0x7fffffffLL)) {
     zo_set_error("paged_attention: too many workgroups (%lld)", units * split);
     return ZO_ERR_UNSUPPORTED;
   }

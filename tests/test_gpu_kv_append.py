@@ -109,6 +109,54 @@ def test_matches_rope_of_a_whole_sequence():
     assert np.mean(d > 0) < 1e-3 and np.all(d <= 2.0 ** -7 * np.abs(mine) + 2.0 ** -20)
 
 
+@pytest.mark.parametrize("cache", ["same", "e4m3"])
+@pytest.mark.parametrize("inplace", [False, True])
+def test_padding_is_copied(cache, inplace):
+    """Queries before position 0 keep their bits (infinities, NaN and -0 among them), their keys are not stored."""
+    rng, dh, ps, kvh = np.random.default_rng(3), 128, 16, 2
+    news, lens = [6, 4, 3], [2, -3, 0]
+    a = rng.standard_normal((14, 4 * dh))
+    a[:, ::7], a[:, 3::11], a[:, 5::13], a[:, 1::17] = np.inf, np.nan, -0.0, -np.inf
+    Q, _ = rows16(a, "bf16")
+    was = bits(Q).copy()
+    K, _ = rows16(np.where(np.isfinite(a), a, 1.0)[:, :kvh * dh], "bf16")
+    table, q_start, kv_len, pages = batch(rng, lens, news, ps)
+    kc = torch.zeros((pages, kvh, ps, dh), device="cuda").to(E4M3 if cache == "e4m3" else torch.bfloat16)
+    vc = kc.clone()
+    ks, vs = ((torch.ones((pages, kvh), device="cuda") for _ in range(2)) if cache == "e4m3" else (None, None))
+    got = zo.kv_append(K, K, kc, vc, dev(table), dev(kv_len), q_start=dev(q_start), max_q=6, Q=Q,
+                       q_out=Q if inplace else torch.zeros_like(Q), rope_base=1e4, k_scale=ks, v_scale=vs)
+    pad = [r for r in range(13) if r not in (4, 5)]  # rows 4, 5 are positions 0, 1 of the first sequence
+    np.testing.assert_array_equal(bits(got)[pad], was[pad])
+    assert not np.array_equal(bits(got)[5], was[5])
+    stored = host64(vc).any((1, 3))
+    assert stored.sum() == 2 and stored[table[0, 0], :2].all()
+
+
+@pytest.mark.parametrize("cache", ["same", "e4m3"])
+def test_max_q_by_default(cache):
+    """Without max_q every row of a batch with q_start is taken, and one of each sequence without."""
+    rng, dh, ps, kvh = np.random.default_rng(4), 64, 32, 2
+    table, q_start, kv_len, pages = batch(rng, [40, 9, 70], [35, 0, 3], ps)
+    K, V, Q = (rows16(rng.standard_normal((38, n * dh)), "f16")[0] for n in (kvh, kvh, 4))
+    outs = []
+    for kw in (dict(max_q=35), dict()):
+        kc = torch.zeros((pages, kvh, ps, dh), device="cuda").to(E4M3 if cache == "e4m3" else torch.float16)
+        vc = kc.clone()
+        ks, vs = ((torch.ones((pages, kvh), device="cuda") for _ in range(2)) if cache == "e4m3" else (None, None))
+        flag = torch.zeros(1, dtype=torch.int32, device="cuda")
+        args = dict(q_start=dev(q_start), k_scale=ks, v_scale=vs, bad_flag=flag, **kw)
+        q = zo.kv_append(K, V, kc, vc, dev(table), dev(kv_len), Q=Q, rope_base=1e4, **args)
+        o = zo.paged_attention(q, kc, vc, dev(table), dev(kv_len), **args)
+        assert int(flag) == 0
+        outs.append([bits(t) for t in (q, kc, vc, o)])
+    for x, y in zip(*outs):
+        np.testing.assert_array_equal(x, y)
+    for bad in (-1, 1 << 31, (1 << 32) + 1):
+        with pytest.raises(ValueError, match="max_q"):
+            zo.paged_attention(q, kc, vc, dev(table), dev(kv_len), q_start=dev(q_start), max_q=bad, k_scale=ks, v_scale=vs)
+
+
 # ---------------------------------------------------------------- 8-bit cache
 def check8(kc, ks, ref, refs, src, what, rotated):
     """Scales as the reference's, but where the largest magnitude is within the rotation's error of a border;

@@ -98,6 +98,24 @@ def test_attention_refusals(kw, status, needle):
     assert _attend(**kw) == status and needle in _detail(), _detail()
 
 
+@pytest.mark.parametrize("nseq,rows,heads,kvh", [(1 << 26, 1 << 30, 1 << 15, 1), (1 << 30, 1 << 30, 1 << 15, 1 << 15),
+                                                 (3, 1 << 30, 1 << 15, 1), (1 << 17, 1 << 14, 1 << 15, 1 << 15)])
+def test_more_work_than_a_launch_holds(nseq, rows, heads, kvh):
+    """Numbers whose products leave 32 or 64 bits are refused; nothing wraps to a small launch, or to 0."""
+    kw = dict(nseq=nseq, rows=rows, max_q=rows, kv_heads=kvh)
+    ld = 1 << 22
+    for cache in (1, 3):
+        c, b = _descs(**kw)
+        c.dtype = cache
+        if cache == 3:
+            c.k_scale = c.v_scale = FAKE
+        assert zo.lib().zo_paged_attention_workspace(c, b, heads, 1) == 0
+        assert zo.lib().zo_paged_attention(c, b, heads, 1, FAKE, ld, FAKE, ld, FAKE, 1 << 62, None) == 2, _detail()
+        assert "too many" in _detail()
+        assert zo.lib().zo_kv_append(c, b, heads, 1, FAKE, ld, FAKE, ld, FAKE, ld, FAKE, ld, 1e4, None) == 2, _detail()
+        assert "too many" in _detail()
+
+
 def test_nothing_to_do():
     for kw in (dict(nseq=0), dict(rows=0), dict(max_q=0)):
         assert _append(**kw) == 0 and _attend(**kw) == 0
