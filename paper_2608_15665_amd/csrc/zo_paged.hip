@@ -3,15 +3,24 @@
 //
 // The queries of the heads that share a key/value head read the same keys, so a workgroup's rows are
 // (token, head of the group) pairs of one key/value head: row t G + j is head j of the group at the
-// sequence's new token t.
+// sequence's new token t.  Softmax in one pass over the keys: a running maximum m, P = 2^((s - m) scale),
+// a running sum of P and of P V, both scaled when m moves (by more than 2^3).
 //
-// k_paged_rows: a workgroup of 4 waves takes 16 NG rows and a range of the keys; its waves take the
-// range's tiles of 32 keys in turn, each with a softmax of its own (running maximum and sum), and
-// join their results in LDS at the end.  Ranges of one sequence (nsplit > 1) are joined by
-// k_paged_join.  Products as in the causal attention of whole sequences:
-//   S^T = K Q^T   (16 x 16 x 32 MFMA; A = K rows from global memory straight into the fragment)
-//   O^T += V^T P^T, V^T's fragments by transposed reads of a row-major V tile in LDS, private to
-//   the wave; P as a hi + lo 16-bit pair.
+// k_paged_rows, for rows that read their keys and little else (up to 16, of 8-bit caches 32): a workgroup of 4
+// waves takes 16 NG rows and a range of the keys; its waves take the range's tiles (as many bytes each: 32 keys of 16
+// bits, 64 of 8) in turn, each with a softmax of its own, and join their results in LDS at the end.  K goes from
+// global memory straight into the fragments, a tile ahead.  Ranges of one sequence (nsplit > 1) are joined by
+// k_paged_join.  Bound by HBM: 61 tokens with up to 8192 keys each, 40 query heads to 8, 196 us for 1.09 GB (5.5 TB/s,
+// where a kernel that only reads reaches 6.2); one token, 131072 keys, 99 us for 0.54 GB with its join; 8-bit,
+// 61 tokens, 111 us for 0.54 GB.
+// k_paged_tile, for more rows: 4 waves of 32 rows share tiles of 64 keys in LDS.  Bound by the MFMAs and the
+// exponentials between them: pieces of up to 1000 tokens of 4 sequences over up to 7000 keys, 255 us, 850 TFLOP/s of
+// visible pairs, where a large matrix product reaches 1211; 8-bit pieces by the vector instructions that widen the codes.
+//
+// Products as in the causal attention of whole sequences:
+//   S^T = K Q^T   (16 x 16 x 32 MFMA; A = K rows)
+//   O^T += V^T P^T, V^T's fragments by transposed reads of a row-major V tile in LDS; P as a hi + lo
+//   16-bit pair in k_paged_rows, where the MFMAs cost nothing, rounded once in k_paged_tile.
 // 8-bit caches: codes are exact in fp16 and in bf16, so K enters as Q's type, V as bf16; the page's
 // key scale multiplies S, its value scale P, in fp32.
 // A page boundary never lies inside 16 keys, so the 16 keys of an MFMA tile have one page: its
@@ -525,6 +534,10 @@ constexpr int PT_AHEAD = 2;               // LDS reads of a phase that go out be
 // and within a row the 16-byte chunks are permuted by an XOR with swz(row) in two bits, so that the 16 rows of a K
 // fragment, and the 8 (8-bit: 16) rows of a transposed read of V, lie on different banks.  A read's address is then
 // one of one (K) or four (V) per lane, the rest is an immediate offset.
+// 8-bit tiles take 480 vector instructions of a wave beside its 64 MFMAs where 16-bit ones take 240 (128 widen the
+// codes, which every wave does for itself, 64 apply the scales): 8 pieces of up to 256 tokens over up to 4096 keys,
+// 32 heads, 154 us (16 bits: 120).  Four buffers of each instead of two, with the loads three tiles ahead, changed
+// nothing (158), so it is not their latency.
 // P enters its product rounded once to 16 bits: each weight is off by at most 2^-8 (bf16) or 2^-11 (fp16) of
 // itself, as the output is by its own rounding, and the errors of many weights average out; the low parts
 // would cost half as many MFMAs again.
