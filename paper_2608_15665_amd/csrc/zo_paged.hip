@@ -536,8 +536,8 @@ constexpr int PT_AHEAD = 2;               // LDS reads of a phase that go out be
 // one of one (K) or four (V) per lane, the rest is an immediate offset.
 // 8-bit tiles take 480 vector instructions of a wave beside its 64 MFMAs where 16-bit ones take 240 (128 widen the
 // codes, which every wave does for itself, 64 apply the scales): 8 pieces of up to 256 tokens over up to 4096 keys,
-// 32 heads, 154 us (16 bits: 120).  Four buffers of each instead of two, with the loads three tiles ahead, changed
-// nothing (158), so it is not their latency.
+// 32 heads, 114 us (16 bits: 101).  Four buffers of each instead of two, with the loads three tiles ahead, gained
+// nothing (2 % slower), so it is not their latency.
 // P enters its product rounded once to 16 bits: each weight is off by at most 2^-8 (bf16) or 2^-11 (fp16) of
 // itself, as the output is by its own rounding, and the errors of many weights average out; the low parts
 // would cost half as many MFMAs again.
@@ -567,17 +567,20 @@ __global__ __launch_bounds__(64 * PG_W, 2) void k_paged_tile(PagedArgs a) {
       Vb1[NBLK * VBLK];
   __shared__ int bads[PG_W];
 
-  // Workgroups are dealt to the 8 XCDs in turn; each XCD gets a contiguous range, a part of the key heads of
-  // every sequence: the row tiles that read one sequence's keys share its L2, and sequences of different lengths
-  // load the XCDs alike.
-  int w = (int)(blockIdx.x & 7) * (int)(gridDim.x >> 3) + min((int)(blockIdx.x & 7), (int)(gridDim.x & 7)) +
-          (int)(blockIdx.x >> 3);
+  // Workgroups are dealt to the 8 XCDs in turn.  Where the key heads are a multiple of 8, each XCD takes as many of
+  // them, the longest sequence of all its heads first (8 sequences in pieces of up to 256 over up to 4096 keys, 32
+  // heads: 101 us, head after head 119; 8-bit 120 and 157); else a contiguous range of (head, sequence) pairs.  The
+  // row tiles that read one sequence's keys share its L2, and sequences of different lengths load the XCDs alike.
+  const int xcd = (int)(blockIdx.x & 7), hx = a.kv.kv_heads & 7 ? 0 : a.kv.kv_heads >> 3;
+  int w = (int)(blockIdx.x >> 3);
+  if (!hx) w += xcd * (int)(gridDim.x >> 3) + min(xcd, (int)(gridDim.x & 7));
   const int rt = a.tiles - 1 - w % a.tiles;  // the last rows see the most keys: they begin first
   w /= a.tiles;
   const int split = w % a.nsplit;
   w /= a.nsplit;
+  const int kvh = hx ? xcd * hx + w % hx : w / a.kv.nseq;
   KvSpan sp;
-  const int s = by_length(a.kv, w % a.kv.nseq, threadIdx.x & 63, sp), kvh = w / a.kv.nseq;
+  const int s = by_length(a.kv, hx ? w / hx : w % a.kv.nseq, threadIdx.x & 63, sp);
   const RowTile rtile = row_tile(a, sp, rt);
   if (rtile.nrows <= 0) return;
   const int nsp = splits_of(a, rtile.kend);

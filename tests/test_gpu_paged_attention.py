@@ -57,6 +57,19 @@ def test_long_contexts(heads, kvh, dh, news, lens, ps, width, cache):
         check_attention(got, ref, mag, dt, (lens, dt), many(news, heads, kvh, cache), cache)
 
 
+@pytest.mark.parametrize("cache", ["same", "e4m3"])
+@pytest.mark.parametrize("heads,kvh,dh", [(8, 8, 64), (16, 16, 128), (16, 8, 64)])
+@pytest.mark.parametrize("seqs", [1, 5, 70])
+def test_many_heads_and_sequences(seqs, heads, kvh, dh, cache):
+    """Every (sequence, head, row tile) is taken once, whatever order the workgroups go in."""
+    rng = np.random.default_rng(seqs + heads)
+    news = [int(x) for x in rng.integers(0, 40, seqs)]
+    news[0] = 150 if seqs < 70 else 35
+    lens = [n + int(c) for n, c in zip(news, rng.integers(0, 90, seqs))]
+    got, ref, mag = attend(rng, "bf16", lens, news, 32, heads, kvh, dh, cache=cache)
+    check_attention(got, ref, mag, "bf16", (seqs, heads, kvh), many=many(news, heads, kvh, cache), cache=cache)
+
+
 @pytest.mark.parametrize("shape", ["rise", "fall", "large"])
 @pytest.mark.parametrize("heads,kvh,dh,news,lens", [(4, 2, 128, [1, 1], [700, 90]), (2, 1, 64, [60, 9], [333, 200])])
 def test_moving_maximum(shape, heads, kvh, dh, news, lens):
