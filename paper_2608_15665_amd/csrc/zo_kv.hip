@@ -168,12 +168,14 @@ __device__ __forceinline__ u32x2 codes8(const float* v, float inv) {
   return (u32x2){codes4(x), codes4(x + 4)};
 }
 
-// One page of one sequence, heads 2 part and 2 part + 1: wave w takes tensor w & 1 (K, V) of head w >> 1.  Two passes
+// One page of one sequence, W waves for one head's K or V: wave w takes tensor w & 1 (K, V) of head 2 part + (w >> 1) or,
+// with W = 2, of head part, each wave every other item.  Two passes
 // over the page's new rows, the largest magnitude and then the codes (the second reads the rows from the caches: held
 // in registers, they left room for half as many waves, and 16 prompts of 512 rows, 8 heads of 128, took 94 us
 // where this takes 57), and one over its earlier slots where the scale grows.
-template <int DT, int DH, bool ROT>
-__device__ __forceinline__ void append_page8(const AppendArgs& a, int s, int jpage, int part, float2 (*turns)[64]) {
+template <int DT, int DH, bool ROT, int W>
+__device__ __forceinline__ void append_page8(const AppendArgs& a, int s, int jpage, int part, float2 (*turns)[64],
+                                             float* tops) {
   const KvArgs& kv = a.kv;
   constexpr int half = DH / 2, CPH = DH / 16, UN = 2;  // chunks of 8 pairs of a row; items of a lane loaded together
   const int ps = 1 << kv.log2ps;
@@ -187,7 +189,7 @@ __device__ __forceinline__ void append_page8(const AppendArgs& a, int s, int jpa
   if (lo >= hi) return;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const int nt = hi - lo, old = lo & (ps - 1);
-  const int h = 2 * part + (wave >> 1);
+  const int h = W == 1 ? 2 * part + (wave >> 1) : part, of = W == 1 ? 0 : wave >> 1;  // of: which of the W
   const bool isk = (wave & 1) == 0, mine = h < kv.kv_heads;
   const uint16_t* src = (const uint16_t*)(isk ? a.K : a.V) + (size_t)h * DH;
   const long long ld = isk ? a.ldk : a.ldv, row0 = sp.r0 + (lo - p0);
@@ -217,7 +219,8 @@ __device__ __forceinline__ void append_page8(const AppendArgs& a, int s, int jpa
             v[q] = *(const u32x4*)(p + half);
           }
       };
-      load(lane);
+      const int first = lane + 64 * UN * of;
+      load(first);
       if (ROT && (nt > 64 || pass == 0)) {
         __syncthreads();  // those before have been used
         for (int t = threadIdx.x / half; t < cn; t += 256 / half) {
@@ -227,7 +230,7 @@ __device__ __forceinline__ void append_page8(const AppendArgs& a, int s, int jpa
         }
         __syncthreads();
       }
-      for (int x0 = lane; x0 < items; x0 += 64 * UN) {
+      for (int x0 = first; x0 < items; x0 += 64 * UN * W) {
 #pragma unroll
         for (int q = 0; q < UN; ++q) {
           const int x = x0 + 64 * q;
@@ -246,18 +249,23 @@ __device__ __forceinline__ void append_page8(const AppendArgs& a, int s, int jpa
             }
           }
         }
-        load(x0 + 64 * UN);
+        load(x0 + 64 * UN * W);
       }
     }
     if (pass == 0 && mine) {
 #pragma unroll
       for (int off = 32; off > 0; off >>= 1) amax = fmaxf(amax, __shfl_xor(amax, off, 64));
+      if constexpr (W == 2) {  // mine is true of all waves
+        if (lane == 0) tops[wave] = amax;
+        __syncthreads();
+        amax = fmaxf(amax, tops[wave ^ 2]);
+      }
       float to = need_scale(amax);
       if (old > 0) {
         to = fmaxf(was, to);
         if (to > was) {
           const float ratio = was / to;
-          for (int x = lane; x < old * DH / 8; x += 64) {
+          for (int x = lane + 64 * of; x < old * DH / 8; x += 64 * W) {
             const u32x2 w = *(const u32x2*)(base + 8 * x);
             float v[8];
 #pragma unroll
@@ -271,22 +279,23 @@ __device__ __forceinline__ void append_page8(const AppendArgs& a, int s, int jpa
           }
         }
       }
-      if (lane == 0) *sc = to;
+      if (lane == 0 && of == 0) *sc = to;
       inv = 1.f / to;
     }
   }
 }
 
-template <int DT, int DH, bool ROT>
+template <int DT, int DH, bool ROT, int W>
 __global__ __launch_bounds__(256, ROT ? 4 : 5) void k_kv_append8(AppendArgs a) {
   __shared__ float2 turns[ROT ? 64 : 1][64];
+  __shared__ float tops[4];
   const int w = blockIdx.x;
   if (w < a.qblocks) {
     const int part = w % a.parts, t = w / a.parts;
     append_row<DT, false>(a, t / a.kv.max_q, t % a.kv.max_q, part, turns[0]);
   } else {
     const int v = w - a.qblocks, part = v % a.groups, t = v / a.groups;
-    append_page8<DT, DH, ROT>(a, t / a.pages, t % a.pages, part, turns);
+    append_page8<DT, DH, ROT, W>(a, t / a.pages, t % a.pages, part, turns, tops);
   }
 }
 
@@ -323,7 +332,11 @@ int zo_kv_append_launch(const KvArgs& kv, const void* Q, long long ldq, void* Q_
     const bool apart = rows > 1024;
     const long long qb = apart ? 0 : wg;
     a.pages = ((kv.max_q - 1 + (1 << kv.log2ps) - 1) >> kv.log2ps) + 1;
-    a.groups = (kv.kv_heads + 1) / 2;
+    // Two waves a page, head and tensor from 128 positions on, for there are few such pages (16 prompts of 512 rows, 8
+    // heads of 128: 128 positions 63.5 us, with one wave 68.6; 256 positions 77 and 89), one below (64 positions 56 and
+    // 54 with two, 16 positions 55 and 65); single tokens are the same with either.
+    const bool two = kv.log2ps >= 7;
+    a.groups = two ? kv.kv_heads : (kv.kv_heads + 1) / 2;
     const long long pages = qb + (long long)kv.nseq * a.pages * a.groups;
     if (pages > 0x7fffffffLL || wg > 0x7fffffffLL) {
       zo_set_error("kv_append: too many workgroups (%lld)", pages + wg);
@@ -331,15 +344,18 @@ int zo_kv_append_launch(const KvArgs& kv, const void* Q, long long ldq, void* Q_
     }
     a.qblocks = (int)qb;
     const dim3 grid((unsigned)pages);
-#define ZO_APPEND8(D, R)                                                                                   \
-  if (kv.dtype == ZO_BF16) hipLaunchKernelGGL((k_kv_append8<ZO_BF16, D, R>), grid, block, 0, stream, a);   \
-  else hipLaunchKernelGGL((k_kv_append8<ZO_F16, D, R>), grid, block, 0, stream, a)
+#define ZO_APPEND8_W(T, D, R)                                                                        \
+  if (two) hipLaunchKernelGGL((k_kv_append8<T, D, R, 2>), grid, block, 0, stream, a);                \
+  else hipLaunchKernelGGL((k_kv_append8<T, D, R, 1>), grid, block, 0, stream, a)
+#define ZO_APPEND8(D, R)                                                                             \
+  if (kv.dtype == ZO_BF16) { ZO_APPEND8_W(ZO_BF16, D, R); } else { ZO_APPEND8_W(ZO_F16, D, R); }
     if (kv.dh == 64) {
       if (rot) { ZO_APPEND8(64, true); } else { ZO_APPEND8(64, false); }
     } else {
       if (rot) { ZO_APPEND8(128, true); } else { ZO_APPEND8(128, false); }
     }
 #undef ZO_APPEND8
+#undef ZO_APPEND8_W
     st = zo_hip_status(hipGetLastError(), "k_kv_append8");
     if (st != ZO_OK || !apart || wg == 0) return st;
     if (kv.dtype == ZO_BF16) hipLaunchKernelGGL((k_kv_append<ZO_BF16, false>), dim3((unsigned)wg), block, 0, stream, a);

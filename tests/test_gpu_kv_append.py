@@ -176,7 +176,7 @@ def check8(kc, ks, ref, refs, src, what, rotated):
 
 @pytest.mark.parametrize("dt", ["bf16", "f16"])
 @pytest.mark.parametrize("base", [None, 1e4])
-@pytest.mark.parametrize("kvh,dh,ps", [(1, 128, 16), (3, 64, 32), (5, 128, 64), (2, 64, 256), (2, 128, 256)])
+@pytest.mark.parametrize("kvh,dh,ps", [(1, 128, 16), (3, 64, 32), (5, 128, 64), (2, 64, 256), (2, 128, 256), (3, 128, 128)])
 def test_append8_in_pieces(dt, base, kvh, dh, ps):
     """A sequence in pieces of several lengths, with values that grow and shrink, beside one that stands still
     and one of single rows: scales grow within a page, start again in the next, and junk slots stay."""
