@@ -20,7 +20,8 @@
 // Products as in the causal attention of whole sequences:
 //   S^T = K Q^T   (16 x 16 x 32 MFMA; A = K rows)
 //   O^T += V^T P^T, V^T's fragments by transposed reads of a row-major V tile in LDS; P as a hi + lo
-//   16-bit pair in k_paged_rows, where the MFMAs cost nothing, rounded once in k_paged_tile.
+//   16-bit pair in k_paged_rows, where the MFMAs cost nothing, rounded once in k_paged_tile (but for fp16 rows of
+//   8-bit caches, whose product is bf16's).
 // 8-bit caches: codes are exact in fp16 and in bf16, so K enters as Q's type, V as bf16; the page's
 // key scale multiplies S, its value scale P, in fp32.
 // A page boundary never lies inside 16 keys, so the 16 keys of an MFMA tile have one page: its
@@ -540,7 +541,9 @@ constexpr int PT_AHEAD = 2;               // LDS reads of a phase that go out be
 // nothing (2 % slower), so it is not their latency.
 // P enters its product rounded once to 16 bits: each weight is off by at most 2^-8 (bf16) or 2^-11 (fp16) of
 // itself, as the output is by its own rounding, and the errors of many weights average out; the low parts
-// would cost half as many MFMAs again.
+// would cost half as many MFMAs again.  fp16 rows of an 8-bit cache have them (LO): scales leave fp16's range, so P V is
+// bf16's, and one rounding of P there would be 8 times the output's (the pieces above: 145 us where bf16 rows take 113;
+// the output's error 2.1e-4 of its size, with one rounding 6.3e-4).
 template <int RB>
 __device__ __forceinline__ int swz(int r) {
   return RB == 256 ? r & 3 : RB == 128 ? (r >> 1) & 3 : (r >> 2) & 3;
@@ -558,6 +561,7 @@ __global__ __launch_bounds__(64 * PG_W, 2) void k_paged_tile(PagedArgs a) {
   constexpr int NBLK = PT_K / RPB;               // blocks of a tile
   constexpr int VX = E8 ? 1 : 2;                 // V's chunks are permuted one by one or in pairs
   constexpr bool PF16 = F16 && !E8;
+  constexpr bool LO = F16 && E8;  // P also as a low part
   constexpr float SHIFT = PF16 ? 12.f : 0.f;
   constexpr int OROW = DH + 8;  // LDS row of the finished rows (16-bit elements)
   static_assert(16 * OROW * 2 <= NBLK * 1024, "16 finished rows of a wave fit a buffer");
@@ -786,11 +790,11 @@ __global__ __launch_bounds__(64 * PG_W, 2) void k_paged_tile(PagedArgs a) {
 #pragma unroll
         for (int t = 0; t < 4; ++t) st[gq][t] -= mrow[gq];
     }
-    bf16x8 bh[2][PT_NG];
+    bf16x8 bh[2][PT_NG], bl[2][LO ? PT_NG : 1];
     auto probs = [&](int c) {
 #pragma unroll
       for (int gq = 0; gq < PT_NG; ++gq) {
-        u32x4 hp;
+        u32x4 hp, lp;
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
           const int t = 2 * c + (x >> 1), i = 2 * (x & 1);
@@ -802,9 +806,11 @@ __global__ __launch_bounds__(64 * PG_W, 2) void k_paged_tile(PagedArgs a) {
             q1 *= vsc[t];
           }
           hp[x] = cvt_pk<PF16>(q0, q1);
+          if constexpr (LO) lp[x] = cvt_pk<PF16>(q0 - unpk<PF16>(hp[x], 0), q1 - unpk<PF16>(hp[x], 1));
           if constexpr (!E8) lsum[gq] = add_pair<PF16>(hp[x], lsum[gq]);
         }
         bh[c][gq] = __builtin_bit_cast(bf16x8, hp);
+        if constexpr (LO) bl[c][gq] = __builtin_bit_cast(bf16x8, lp);
       }
     };
     // O^T += V^T P^T over keys 32 c ..: lane group g's k slots are keys 32 c + 4 g + (0..3) and
@@ -825,7 +831,10 @@ __global__ __launch_bounds__(64 * PG_W, 2) void k_paged_tile(PagedArgs a) {
           av = (u32x4){finite_pair<PF16>(av[0]), finite_pair<PF16>(av[1]), finite_pair<PF16>(av[2]), finite_pair<PF16>(av[3])};
         const bf16x8 af = __builtin_bit_cast(bf16x8, av);
 #pragma unroll
-        for (int gq = 0; gq < PT_NG; ++gq) o[gq][t] = mfma16<PF16>(af, bh[c][gq], o[gq][t]);
+        for (int gq = 0; gq < PT_NG; ++gq) {
+          o[gq][t] = mfma16<PF16>(af, bh[c][gq], o[gq][t]);
+          if constexpr (LO) o[gq][t] = mfma16<PF16>(af, bl[c][gq], o[gq][t]);
+        }
       }
     };
     // The first reads of a phase go out together; each later one while the MFMAs of an earlier one run.
@@ -864,7 +873,7 @@ __global__ __launch_bounds__(64 * PG_W, 2) void k_paged_tile(PagedArgs a) {
 #pragma unroll
     for (int x = 0; x < DT; ++x) {
       __builtin_amdgcn_sched_group_barrier(0x002, VV, 1);
-      __builtin_amdgcn_sched_group_barrier(0x008, PT_NG, 1);
+      __builtin_amdgcn_sched_group_barrier(0x008, PT_NG * (LO ? 2 : 1), 1);
       if (x + PT_AHEAD < DT) __builtin_amdgcn_sched_group_barrier(0x100, VR, 1);
     }
     __builtin_amdgcn_sched_barrier(0);
@@ -877,7 +886,7 @@ __global__ __launch_bounds__(64 * PG_W, 2) void k_paged_tile(PagedArgs a) {
 #pragma unroll
     for (int x = 0; x < DT; ++x) {
       __builtin_amdgcn_sched_group_barrier(0x002, (next ? 32 : 0) / DT, 2);
-      __builtin_amdgcn_sched_group_barrier(0x008, PT_NG, 2);
+      __builtin_amdgcn_sched_group_barrier(0x008, PT_NG * (LO ? 2 : 1), 2);
       if (x + PT_AHEAD < DT) __builtin_amdgcn_sched_group_barrier(0x100, VR, 2);
     }
     __builtin_amdgcn_sched_barrier(0);

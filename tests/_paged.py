@@ -106,9 +106,10 @@ def check_attention(got, ref, mag, dt, what, many=False, cache="same"):
     """Few rows: P enters the P V product as a hi + lo pair of 16-bit values (relative error <= 2^-16), and the
     fp32 logits carry an absolute error of a few 2^-24 |q| |k|, which moves P by under 2^-16 relative at logits
     of a few hundred; fp32 sums of up to some thousand terms add 2^-16.  So before its rounding (half an ulp of
-    the type) an output is within 2^-14 softmax(S) |V| of the exact one.  Many (see many()): P is rounded once, by 2^-8 of a weight (bf16, and 8-bit caches), or 2^-11 (fp16), at most."""
+    the type) an output is within 2^-14 softmax(S) |V| of the exact one.  Many (see many()): P is rounded once, by 2^-8 (bf16) or 2^-11
+    (fp16) of a weight at most, but a pair too for fp16 rows of 8-bit caches."""
     assert np.all(np.isfinite(got)), what
-    p = 2.0 ** -14 + (0.0 if not many else 2.0 ** -11 if dt == "f16" and cache == "same" else 2.0 ** -8)
+    p = 2.0 ** -14 + (0.0 if not many or (dt == "f16" and cache == "e4m3") else 2.0 ** -11 if dt == "f16" else 2.0 ** -8)
     bound = 0.5 * ulp16(ref, dt) * (1 + 2.0 ** -6) + p * mag
     err = np.abs(got - ref)
     assert np.all(err <= bound), (what, float(np.max(err / np.maximum(bound, 1e-300))))
