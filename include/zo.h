@@ -709,12 +709,10 @@ int zo_kv_append(const zo_kv_cache* cache, const zo_kv_batch* batch, int heads,
  *             cache has the same), ldq and ldo apart.  O may be Q (ldo = ldq).
  * Slots behind a sequence's last position may hold anything, NaN included.
  * Arithmetic: fp32 softmax; the products run on the MFMA (8-bit codes are
- * exact in 16 bits; their scales are applied in fp32).  Where max_q heads /
- * kv_heads <= 16 (8-bit caches: 32), and for fp16 rows of an 8-bit cache, P
- * enters its product as a hi + lo 16-bit pair, as for zo_causal_attention; else
- * it is rounded once, to the rows' type: a weight is off by at most 2^-8 (bf16)
- * or 2^-11 (fp16) of itself.  A value that is not finite reaches the rows that see its position,
- * and no others.
+ * exact in 16 bits; their scales are applied in fp32).  P enters its product as
+ * a hi + lo 16-bit pair, as for zo_causal_attention (a weight is within 2^-15
+ * of itself), for every row and any max_q.  A value that is not finite reaches
+ * the rows that see its position, and no others.
  * The workspace holds partial results where a sequence's keys are split over
  * workgroups; its size depends on the host arguments only (0 where nothing is
  * split), and calls that may run at the same time need one each.

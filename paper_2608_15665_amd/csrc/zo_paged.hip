@@ -14,14 +14,13 @@
 // where a kernel that only reads reaches 6.2); one token, 131072 keys, 99 us for 0.54 GB with its join; 8-bit,
 // 61 tokens, 111 us for 0.54 GB.
 // k_paged_tile, for more rows: 4 waves of 32 rows share tiles of 64 keys in LDS.  Bound by the MFMAs and the
-// exponentials between them: pieces of up to 1000 tokens of 4 sequences over up to 7000 keys, 255 us, 850 TFLOP/s of
-// visible pairs, where a large matrix product reaches 1211; 8-bit pieces by the vector instructions that widen the codes.
+// exponentials between them: pieces of up to 1000 tokens of 4 sequences over up to 7000 keys, 333 us, 650 TFLOP/s of
+// visible pairs; 8-bit pieces by the vector instructions that widen the codes.
 //
 // Products as in the causal attention of whole sequences:
 //   S^T = K Q^T   (16 x 16 x 32 MFMA; A = K rows)
 //   O^T += V^T P^T, V^T's fragments by transposed reads of a row-major V tile in LDS; P as a hi + lo
-//   16-bit pair in k_paged_rows, where the MFMAs cost nothing, rounded once in k_paged_tile (but for fp16 rows of
-//   8-bit caches, whose product is bf16's).
+//   16-bit pair.
 // 8-bit caches: codes are exact in fp16 and in bf16, so K enters as Q's type, V as bf16; the page's
 // key scale multiplies S, its value scale P, in fp32.
 // A page boundary never lies inside 16 keys, so the 16 keys of an MFMA tile have one page: its
@@ -211,13 +210,13 @@ __device__ __forceinline__ u32x2 ds_read_tr8(const char* p) {
   return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) i32x2_t*)p));
 }
 
-// The sum of a pair of 16-bit values and an fp32 one, in one instruction (fp32 products with 1).
+// Two fp32 values (0 or more) rounded down into a packed pair of 16-bit values.
 template <bool F16>
-__device__ __forceinline__ float add_pair(uint32_t pk, float x) {
+__device__ __forceinline__ uint32_t cvt_down(float x, float y) {
   if constexpr (F16)
-    return __builtin_amdgcn_fdot2(__builtin_bit_cast(f16x2_t, pk), (f16x2_t){(_Float16)1.f, (_Float16)1.f}, x, false);
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(x, y));
   else
-    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, pk), (bf16x2_t){(__bf16)1.f, (__bf16)1.f}, x, false);
+    return __builtin_amdgcn_perm(__float_as_uint(y), __float_as_uint(x), 0x07060302u);
 }
 
 // A result o / l of a row at position p, from unnormalised sums: 0 where it has no keys, NaN where it
@@ -537,13 +536,11 @@ constexpr int PT_AHEAD = 2;               // LDS reads of a phase that go out be
 // one of one (K) or four (V) per lane, the rest is an immediate offset.
 // 8-bit tiles take 480 vector instructions of a wave beside its 64 MFMAs where 16-bit ones take 240 (128 widen the
 // codes, which every wave does for itself, 64 apply the scales): 8 pieces of up to 256 tokens over up to 4096 keys,
-// 32 heads, 114 us (16 bits: 101).  Four buffers of each instead of two, with the loads three tiles ahead, gained
+// 32 heads, 142 us (16 bits: 120).  Four buffers of each instead of two, with the loads three tiles ahead, gained
 // nothing (2 % slower), so it is not their latency.
-// P enters its product rounded once to 16 bits: each weight is off by at most 2^-8 (bf16) or 2^-11 (fp16) of
-// itself, as the output is by its own rounding, and the errors of many weights average out; the low parts
-// would cost half as many MFMAs again.  fp16 rows of an 8-bit cache have them (LO): scales leave fp16's range, so P V is
-// bf16's, and one rounding of P there would be 8 times the output's (the pieces above: 145 us where bf16 rows take 113;
-// the output's error 2.1e-4 of its size, with one rounding 6.3e-4).
+// P enters its product as a hi + lo pair, as in k_paged_rows, so a row is as exact here as it is alone.  That is half as
+// many MFMAs again: the pieces above took 114 us (8 bits) and 100 (16 bits) with P rounded once, which put an
+// output off by up to 2^-8 (bf16) or 2^-11 (fp16) of the values it averages.
 template <int RB>
 __device__ __forceinline__ int swz(int r) {
   return RB == 256 ? r & 3 : RB == 128 ? (r >> 1) & 3 : (r >> 2) & 3;
@@ -561,7 +558,7 @@ __global__ __launch_bounds__(64 * PG_W, 2) void k_paged_tile(PagedArgs a) {
   constexpr int NBLK = PT_K / RPB;               // blocks of a tile
   constexpr int VX = E8 ? 1 : 2;                 // V's chunks are permuted one by one or in pairs
   constexpr bool PF16 = F16 && !E8;
-  constexpr bool LO = F16 && E8;  // P also as a low part
+  constexpr float PULL = F16 || E8 ? 1.f : 1.f + 0x1p-18f;  // P's factor (see probs)
   constexpr float SHIFT = PF16 ? 12.f : 0.f;
   constexpr int OROW = DH + 8;  // LDS row of the finished rows (16-bit elements)
   static_assert(16 * OROW * 2 <= NBLK * 1024, "16 finished rows of a wave fit a buffer");
@@ -738,15 +735,17 @@ __global__ __launch_bounds__(64 * PG_W, 2) void k_paged_tile(PagedArgs a) {
     float vsc[4];
     if constexpr (E8) scales(n, pg.vs, vsp, vsc);
     if constexpr (!next) scale_s(n, st);
-    bool clean = false;  // V of the tile is not finite, and rows see only a part of it
-    if (!next && k0 + PT_K > wfirst + 1) {
+    bool clean = false;  // V of the tile is not finite
+    if (!next) {
+      if (k0 + PT_K > wfirst + 1) {
 #pragma unroll
-      for (int gq = 0; gq < PT_NG; ++gq)
+        for (int gq = 0; gq < PT_NG; ++gq)
 #pragma unroll
-        for (int t = 0; t < 4; ++t)
+          for (int t = 0; t < 4; ++t)
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (k0 + 16 * t + 4 * g + i > pos[gq]) st[gq][t][i] = -INFINITY;
+            for (int i = 0; i < 4; ++i)
+              if (k0 + 16 * t + 4 * g + i > pos[gq]) st[gq][t][i] = -INFINITY;
+      }
       uint32_t odd = 0;
 #pragma unroll 4
       for (int x = 0; x < NBLK; ++x) odd |= odd_bits<PF16, E8>(*(const u32x4*)(vt + VBLK * x + 16 * lane));
@@ -790,7 +789,11 @@ __global__ __launch_bounds__(64 * PG_W, 2) void k_paged_tile(PagedArgs a) {
 #pragma unroll
         for (int t = 0; t < 4; ++t) st[gq][t] -= mrow[gq];
     }
-    bf16x8 bh[2][PT_NG], bl[2][LO ? PT_NG : 1];
+    // P as a hi + lo pair.  An infinity of V (8-bit codes have none) times such a pair is NaN unless lo is positive
+    // as well.  Where rows see all of a tile, which is not searched for infinities, it is: hi is rounded down, and
+    // lo then holds PULL times P less hi (bf16; the sum of P gets the same factor), or its last bit is set (fp16,
+    // at most 2^-20 of P or 2^-24).
+    bf16x8 bh[2][PT_NG], bl[2][PT_NG];
     auto probs = [&](int c) {
 #pragma unroll
       for (int gq = 0; gq < PT_NG; ++gq) {
@@ -800,17 +803,17 @@ __global__ __launch_bounds__(64 * PG_W, 2) void k_paged_tile(PagedArgs a) {
           const int t = 2 * c + (x >> 1), i = 2 * (x & 1);
           float q0 = __builtin_amdgcn_exp2f(fmaf(st[gq][t][i], a.scale_log2, brow[gq]));
           float q1 = __builtin_amdgcn_exp2f(fmaf(st[gq][t][i + 1], a.scale_log2, brow[gq]));
+          lsum[gq] += q0 + q1;
           if constexpr (E8) {
-            lsum[gq] += q0 + q1;
             q0 *= vsc[t];
             q1 *= vsc[t];
           }
-          hp[x] = cvt_pk<PF16>(q0, q1);
-          if constexpr (LO) lp[x] = cvt_pk<PF16>(q0 - unpk<PF16>(hp[x], 0), q1 - unpk<PF16>(hp[x], 1));
-          if constexpr (!E8) lsum[gq] = add_pair<PF16>(hp[x], lsum[gq]);
+          hp[x] = E8 ? cvt_pk<PF16>(q0, q1) : cvt_down<PF16>(q0, q1);
+          lp[x] = cvt_pk<PF16>(fmaf(q0, PULL, -unpk<PF16>(hp[x], 0)), fmaf(q1, PULL, -unpk<PF16>(hp[x], 1)));
+          if constexpr (PF16 && next) lp[x] |= 0x00010001u;
         }
         bh[c][gq] = __builtin_bit_cast(bf16x8, hp);
-        if constexpr (LO) bl[c][gq] = __builtin_bit_cast(bf16x8, lp);
+        bl[c][gq] = __builtin_bit_cast(bf16x8, lp);
       }
     };
     // O^T += V^T P^T over keys 32 c ..: lane group g's k slots are keys 32 c + 4 g + (0..3) and
@@ -833,7 +836,7 @@ __global__ __launch_bounds__(64 * PG_W, 2) void k_paged_tile(PagedArgs a) {
 #pragma unroll
         for (int gq = 0; gq < PT_NG; ++gq) {
           o[gq][t] = mfma16<PF16>(af, bh[c][gq], o[gq][t]);
-          if constexpr (LO) o[gq][t] = mfma16<PF16>(af, bl[c][gq], o[gq][t]);
+          o[gq][t] = mfma16<PF16>(af, bl[c][gq], o[gq][t]);
         }
       }
     };
@@ -873,7 +876,7 @@ __global__ __launch_bounds__(64 * PG_W, 2) void k_paged_tile(PagedArgs a) {
 #pragma unroll
     for (int x = 0; x < DT; ++x) {
       __builtin_amdgcn_sched_group_barrier(0x002, VV, 1);
-      __builtin_amdgcn_sched_group_barrier(0x008, PT_NG * (LO ? 2 : 1), 1);
+      __builtin_amdgcn_sched_group_barrier(0x008, PT_NG * 2, 1);
       if (x + PT_AHEAD < DT) __builtin_amdgcn_sched_group_barrier(0x100, VR, 1);
     }
     __builtin_amdgcn_sched_barrier(0);
@@ -886,7 +889,7 @@ __global__ __launch_bounds__(64 * PG_W, 2) void k_paged_tile(PagedArgs a) {
 #pragma unroll
     for (int x = 0; x < DT; ++x) {
       __builtin_amdgcn_sched_group_barrier(0x002, (next ? 32 : 0) / DT, 2);
-      __builtin_amdgcn_sched_group_barrier(0x008, PT_NG * (LO ? 2 : 1), 2);
+      __builtin_amdgcn_sched_group_barrier(0x008, PT_NG * 2, 2);
       if (x + PT_AHEAD < DT) __builtin_amdgcn_sched_group_barrier(0x100, VR, 2);
     }
     __builtin_amdgcn_sched_barrier(0);
@@ -973,7 +976,7 @@ __global__ __launch_bounds__(64 * PG_W, 2) void k_paged_tile(PagedArgs a) {
 #pragma unroll
   for (int gq = 0; gq < PT_NG; ++gq) {
     float l = lsum[gq] + __shfl_xor(lsum[gq], 16, 64);
-    l += __shfl_xor(l, 32, 64);
+    l = (l + __shfl_xor(l, 32, 64)) * PULL;
     const int row = wr0 + 16 * gq + l16;
     if (nsp > 1) {
       if (row >= rtile.nrows) continue;
