@@ -178,11 +178,13 @@ __device__ __forceinline__ uint32_t finite_pair(uint32_t x) {
 // V of a staged tile of `keys` keys is not finite somewhere.  0 times such a value is NaN, so a product with
 // P = 0 would take it to rows that do not see the key (and a hi + lo pair may meet an infinity with opposite
 // signs).  P V then runs on V without such values, and here they are added to the rows that do see them.
-// at(key, d): where values d .. d + 3 of a key lie.
+// at(key, d): where values d .. d + 3 of a key lie.  Of the keys the first is looked at in any case (a loop that may
+// have no turn costs the caller registers).
 template <bool F16, bool E8, int DT, int NG, class At>
 __device__ __forceinline__ void add_odd_values(At at, int k0, int keys, int g, const int* pos, f32x4 (*o)[DT]) {
+  int key = 0;
 #pragma unroll 1
-  for (int key = 0; key < keys; ++key)
+  do {
 #pragma unroll
     for (int d = 0; d < DT; ++d) {
       u32x2 v;
@@ -200,6 +202,7 @@ __device__ __forceinline__ void add_odd_values(At at, int k0, int keys, int g, c
           if (k0 + key <= pos[gq] && !(fabsf(x) < INFINITY)) o[gq][d][e] += x;
       }
     }
+  } while (++key < keys);
 }
 
 typedef int i32x2_t __attribute__((ext_vector_type(2)));
@@ -736,6 +739,7 @@ __global__ __launch_bounds__(64 * PG_W, 2) void k_paged_tile(PagedArgs a) {
     if constexpr (E8) scales(n, pg.vs, vsp, vsc);
     if constexpr (!next) scale_s(n, st);
     bool clean = false;  // V of the tile is not finite
+    int odds = 1;  // keys to look for such values in
     if (!next) {
       if (k0 + PT_K > wfirst + 1) {
 #pragma unroll
@@ -746,9 +750,17 @@ __global__ __launch_bounds__(64 * PG_W, 2) void k_paged_tile(PagedArgs a) {
             for (int i = 0; i < 4; ++i)
               if (k0 + 16 * t + 4 * g + i > pos[gq]) st[gq][t][i] = -INFINITY;
       }
-      uint32_t odd = 0;
+      // What is behind the wave's last row (slots behind the sequence among it, which may hold anything) only has to
+      // be kept out of the product.
+      const int keys = min(PT_K, wlast + 1 - k0);
+      uint32_t odd = 0, seen = 0;
 #pragma unroll 4
-      for (int x = 0; x < NBLK; ++x) odd |= odd_bits<PF16, E8>(*(const u32x4*)(vt + VBLK * x + 16 * lane));
+      for (int x = 0; x < NBLK; ++x) {
+        const uint32_t b = odd_bits<PF16, E8>(*(const u32x4*)(vt + VBLK * x + 16 * lane));
+        odd |= b;
+        seen |= RPB * x + lane / CPR < keys ? b : 0;
+      }
+      if (__ballot(seen != 0) != 0) odds = keys;
       clean = __ballot(odd != 0) != 0;
     }
     if constexpr (!next) top_of(st, tmax);
@@ -862,11 +874,12 @@ __global__ __launch_bounds__(64 * PG_W, 2) void k_paged_tile(PagedArgs a) {
     if constexpr (!next) {
       if (__builtin_expect(clean, 0)) {
         probs(1);
+        asm volatile("" : "+v"(lsum[0]), "+v"(lsum[1]));  // summed here: P is not kept in registers until after the loop below
         pv(0, std::true_type{});
         pv(1, std::true_type{});
         add_odd_values<PF16, E8, DT, PT_NG>(
             [&](int key, int d) { return vt + key / RPB * VBLK + key % RPB * RB + 16 * ((d * EB / 16) ^ (VX * swz<RB>(key))) + (d * EB) % 16; },
-            k0, PT_K, g, pos, o);
+            k0, odds, g, pos, o);
         return;
       }
     }
