@@ -639,8 +639,8 @@ def paged_attention(Q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tenso
                     workspace: Optional[torch.Tensor] = None):
     """Causal attention of the new rows' queries Q (rows x heads dh) over the paged cache that kv_append fills
     (which holds their own keys and values already); max_q as for kv_append.  Rows of `out` behind the last sequence are left as they
-    are.  The workspace is the stream's own, or under graph capture one of the graph's.  See
-    zo_paged_attention."""
+    are.  Without a workspace (uint8; calls that may run at the same time, from two threads on one stream too, need
+    one each) the call allocates its own.  See zo_paged_attention."""
     dt, here = Q.dtype, torch._C._cuda_getDevice()
     if dt not in _DT:
         raise TypeError(f"unsupported dtype {dt}")
@@ -661,11 +661,10 @@ def paged_attention(Q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tenso
     if workspace is not None:
         ws, ws_n = _need(workspace, "workspace", torch.uint8).data_ptr(), workspace.numel()
     elif need:
-        # A graph that is replayed on another stream, or after the stream's buffer has grown, needs memory
-        # of its own.
-        buf = (torch.empty(need, dtype=torch.uint8, device=Q.device) if torch.cuda.is_current_stream_capturing()
-               else Workspace.get(need))
-        ws, ws_n = buf.data_ptr(), buf.numel()
+        # Of the call's own, not the stream's buffer: the call is two launches, between which another thread's call on
+        # the same stream may come, and a graph may be replayed on another stream.
+        buf = torch.empty(need, dtype=torch.uint8, device=Q.device)
+        ws, ws_n = buf.data_ptr(), need
     _check(L.zo_paged_attention(cache, batch, heads, _DT[dt], Q.data_ptr(), ldq, out.data_ptr(), ldo, ws, ws_n,
                                 _stream_handle()))
     return out
