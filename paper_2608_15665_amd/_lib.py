@@ -11,6 +11,7 @@ from __future__ import annotations
 import ctypes
 import os
 import threading
+import weakref
 from typing import Optional, Sequence
 
 import torch
@@ -260,22 +261,38 @@ def _need(t: torch.Tensor, name: str, dtype=None, numel=None) -> torch.Tensor:
 _DT = {torch.float32: ZO_F32, torch.bfloat16: ZO_BF16, torch.float16: ZO_F16}
 
 
-class Workspace:
-    """Grow-only device scratch buffer, one per (device, stream).
+class _ThreadKey:
+    """What a thread's buffers are kept by: it ends with the thread, and they with it."""
+    __slots__ = ("__weakref__",)
 
-    Calls enqueued on one stream run in order, so reusing one buffer between
-    them is safe; calls on different streams get different buffers.
+
+_thread = threading.local()
+
+
+class Workspace:
+    """Grow-only device scratch buffer, one per (thread, device, stream).
+
+    Calls that one thread enqueues on one stream run in order, so reusing one
+    buffer between them is safe; calls on different streams get different
+    buffers, and so do calls of different threads on one stream: a call may be
+    several launches, between which another thread's may come.
     """
-    _bufs: dict = {}
+    _bufs: "weakref.WeakKeyDictionary" = weakref.WeakKeyDictionary()
 
     @classmethod
     def get(cls, nbytes: int) -> torch.Tensor:
+        me = getattr(_thread, "key", None)
+        if me is None:
+            me = _thread.key = _ThreadKey()
+        bufs = cls._bufs.get(me)
+        if bufs is None:
+            bufs = cls._bufs[me] = {}
         dev = torch.cuda.current_device()
         key = (dev, _stream_handle())
-        buf = cls._bufs.get(key)
+        buf = bufs.get(key)
         if buf is None or buf.numel() < nbytes:
             buf = torch.empty(max(int(nbytes), 256), dtype=torch.uint8, device=f"cuda:{dev}")
-            cls._bufs[key] = buf
+            bufs[key] = buf
         return buf
 
     @classmethod

@@ -1,6 +1,8 @@
 """Scratch memory of the binding where two threads call on one stream (torch's default stream is every thread's): a call
 may be several launches, and those of two calls may be enqueued in turn, so no two threads share a buffer."""
+import gc
 import threading
+import weakref
 
 import pytest
 import torch
@@ -52,3 +54,44 @@ def test_two_attention_calls_at_once_have_a_workspace_each(host, monkeypatch):
     (a, na), (b, nb) = fake.seen
     assert na >= 4096 and nb >= 4096
     assert a + na <= b or b + nb <= a
+
+
+def test_a_thread_has_its_own_buffers(host, monkeypatch):
+    """The buffers that every other call takes: one for a thread and stream, grown when it is too small, given up when
+    the thread ends or on clear()."""
+    empty = torch.empty
+    monkeypatch.setattr(torch, "empty", lambda n, dtype, device: empty(n, dtype=dtype))
+    get = _lib.Workspace.get
+    _lib.Workspace.clear()
+    mine = get(1000)
+    assert get(900) is mine and get(1000) is mine and mine.numel() >= 1000
+    monkeypatch.setattr(_lib, "_stream_handle", lambda: 8)
+    assert get(1000) is not mine
+    monkeypatch.setattr(_lib, "_stream_handle", lambda: 7)
+    others, kept = [], []
+    up, down = threading.Barrier(3, timeout=30), threading.Barrier(3, timeout=30)
+
+    def work():
+        buf = get(500)
+        assert get(400) is buf
+        others.append(buf.data_ptr())
+        kept.append(weakref.ref(buf))
+        up.wait()
+        down.wait()
+
+    threads = [threading.Thread(target=work) for _ in range(2)]
+    for t in threads:
+        t.start()
+    up.wait()
+    assert len({mine.data_ptr(), *others}) == 3
+    down.wait()
+    for t in threads:
+        t.join()
+    gc.collect()
+    assert [r() for r in kept] == [None, None]
+    assert get(1000) is mine
+    grown = get(5000)
+    assert grown.numel() >= 5000 and get(1000) is grown
+    _lib.Workspace.clear()
+    assert get(5000) is not grown
+    _lib.Workspace.clear()
