@@ -676,7 +676,7 @@ def paged_attention(Q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tenso
     need = L.zo_paged_attention_workspace(cache, batch, heads, _DT[dt])
     ws, ws_n = None, 0
     if workspace is not None:
-        ws, ws_n = _need(workspace, "workspace", torch.uint8).data_ptr(), workspace.numel()
+        ws, ws_n = _kv_tensor(workspace, "workspace", torch.uint8, here), workspace.numel()
     elif need:
         # Of the call's own, not the stream's buffer: the call is two launches, between which another thread's call on
         # the same stream may come, and a graph may be replayed on another stream.
