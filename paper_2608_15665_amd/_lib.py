@@ -610,7 +610,7 @@ def _row_tensor(t: torch.Tensor, name: str, dtype, rows: int, cols: int, here: i
     ld, one = t.stride()
     if one != 1 and cols > 1:
         raise ValueError(f"{name}'s rows must be dense")
-    return ld if rows > 1 else max(ld, cols)  # one row has no distance
+    return ld if rows > 1 else cols  # one row has no distance
 
 
 def kv_append(K: torch.Tensor, V: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor,

@@ -55,3 +55,19 @@ def test_a_workspace_of_another_device_is_refused(fake):
     with pytest.raises(ValueError, match="workspace must live on the current device"):
         _lib.paged_attention(torch.zeros(1, 128, dtype=torch.bfloat16), **_cache(), workspace=ws)
     assert not fake.calls
+
+
+@pytest.mark.parametrize("wide", [128, 130, 133, 136])
+def test_one_row_has_no_distance(fake, wide):
+    """A single row may come from a tensor of any width (its start on 16 bytes): the library's multiple of 8 between
+    rows has nothing to be between."""
+    row = torch.zeros(1, wide, dtype=torch.bfloat16)[:, :128]
+    _lib.kv_append(row, row.clone(), **_cache(), Q=row, q_out=row, rope_base=1e4)
+    ldq, ldqo, ldk, ldv = (fake.calls[-1][i] for i in (5, 7, 9, 11))
+    assert ldq == ldqo and all(x % 8 == 0 and x >= 128 for x in (ldq, ldk, ldv))
+    fake.need = 0
+    _lib.paged_attention(row, **_cache(), out=row)
+    assert fake.calls[-1][5] == fake.calls[-1][7] and fake.calls[-1][5] % 8 == 0
+    two = torch.zeros(2, wide, dtype=torch.bfloat16)[:, :128]
+    _lib.kv_append(two, two, **_cache(), max_q=1)
+    assert fake.calls[-1][9] == wide  # refused by the library where it is no multiple of 8
