@@ -6,6 +6,14 @@
 
 namespace {
 
+// The grid of a launch of n < 2^31 workgroups of 256 threads: the x dimension holds fewer than 2^32 threads, so from 2^24
+// workgroups on they go in rows of 2^22, of which the last may be longer than n.
+inline dim3 kv_grid(long long n) {
+  if (n < (1LL << 24)) return dim3((unsigned)n);
+  return dim3(1u << 22, (unsigned)((n + (1LL << 22) - 1) >> 22));
+}
+__device__ __forceinline__ unsigned kv_block() { return blockIdx.x + (blockIdx.y << 22); }
+
 // A sequence's first row, its rows and its length with them.
 struct KvSpan {
   int r0, n, len;

@@ -24,6 +24,7 @@ struct AppendArgs {
   int parts;    // workgroups per row
   int pages, groups;  // 8-bit: pages that max_q positions touch at most, workgroups (pairs of heads) per page
   int qblocks;  // 8-bit: workgroups that rotate Q, before those of the pages
+  unsigned wgs;  // workgroups of the launch
 };
 
 // Sine and cosine of `turns` full turns: the nearest quarter turn is taken off in fp64, the rest
@@ -136,7 +137,8 @@ __device__ __forceinline__ void append_row(const AppendArgs& a, int s, int i, in
 template <int DT, bool KV>
 __global__ __launch_bounds__(256) void k_kv_append(AppendArgs a) {
   __shared__ float2 turns[64];
-  const int w = blockIdx.x, part = w % a.parts, t = w / a.parts;
+  if (kv_block() >= a.wgs) return;
+  const int w = kv_block(), part = w % a.parts, t = w / a.parts;
   append_row<DT, KV>(a, t / a.kv.max_q, t % a.kv.max_q, part, turns);
 }
 
@@ -289,7 +291,8 @@ template <int DT, int DH, bool ROT, int W>
 __global__ __launch_bounds__(256, ROT ? 4 : 5) void k_kv_append8(AppendArgs a) {
   __shared__ float2 turns[ROT ? 64 : 1][64];
   __shared__ float tops[4];
-  const int w = blockIdx.x;
+  if (kv_block() >= a.wgs) return;
+  const int w = kv_block();
   if (w < a.qblocks) {
     const int part = w % a.parts, t = w / a.parts;
     append_row<DT, false>(a, t / a.kv.max_q, t % a.kv.max_q, part, turns[0]);
@@ -343,7 +346,8 @@ int zo_kv_append_launch(const KvArgs& kv, const void* Q, long long ldq, void* Q_
       return ZO_ERR_UNSUPPORTED;
     }
     a.qblocks = (int)qb;
-    const dim3 grid((unsigned)pages);
+    const dim3 grid = kv_grid(pages);
+    a.wgs = (unsigned)pages;
 #define ZO_APPEND8_W(T, D, R)                                                                        \
   if (two) hipLaunchKernelGGL((k_kv_append8<T, D, R, 2>), grid, block, 0, stream, a);                \
   else hipLaunchKernelGGL((k_kv_append8<T, D, R, 1>), grid, block, 0, stream, a)
@@ -358,13 +362,15 @@ int zo_kv_append_launch(const KvArgs& kv, const void* Q, long long ldq, void* Q_
 #undef ZO_APPEND8_W
     st = zo_hip_status(hipGetLastError(), "k_kv_append8");
     if (st != ZO_OK || !apart || wg == 0) return st;
-    if (kv.dtype == ZO_BF16) hipLaunchKernelGGL((k_kv_append<ZO_BF16, false>), dim3((unsigned)wg), block, 0, stream, a);
-    else hipLaunchKernelGGL((k_kv_append<ZO_F16, false>), dim3((unsigned)wg), block, 0, stream, a);
+    a.wgs = (unsigned)wg;
+    if (kv.dtype == ZO_BF16) hipLaunchKernelGGL((k_kv_append<ZO_BF16, false>), kv_grid(wg), block, 0, stream, a);
+    else hipLaunchKernelGGL((k_kv_append<ZO_F16, false>), kv_grid(wg), block, 0, stream, a);
     return zo_hip_status(hipGetLastError(), "k_kv_append");
   }
   if (wg <= 0x7fffffffLL) {
-    if (kv.dtype == ZO_BF16) hipLaunchKernelGGL((k_kv_append<ZO_BF16, true>), dim3((unsigned)wg), block, 0, stream, a);
-    else hipLaunchKernelGGL((k_kv_append<ZO_F16, true>), dim3((unsigned)wg), block, 0, stream, a);
+    a.wgs = (unsigned)wg;
+    if (kv.dtype == ZO_BF16) hipLaunchKernelGGL((k_kv_append<ZO_BF16, true>), kv_grid(wg), block, 0, stream, a);
+    else hipLaunchKernelGGL((k_kv_append<ZO_F16, true>), kv_grid(wg), block, 0, stream, a);
     return zo_hip_status(hipGetLastError(), "k_kv_append");
   }
   zo_set_error("kv_append: too many workgroups (%lld)", wg);

@@ -45,6 +45,7 @@ struct PagedArgs {
   int group, nsplit, tiles;           // heads per K/V head; splits; row tiles per (sequence, K/V head)
   int rt_rows, prows;                 // rows of a tile; those of them that partial results have room for
   int min_keys;                       // a split's keys at the least
+  unsigned wgs;                       // workgroups of the launch
   uint32_t inv_group;                 // 2^32 / group, rounded up past a whole one; 0: group is 1
   float scale_log2;                   // log2(e) / sqrt(dh)
   float* part;                        // nsplit > 1: O of a split, unnormalised, per row
@@ -251,7 +252,8 @@ __global__ __launch_bounds__(64 * PG_W, 2) void k_paged_rows(PagedArgs a) {
   __shared__ float2 stats[PG_W][16 * NG];
   __shared__ int bads[PG_W];
 
-  int w = blockIdx.x;
+  if (kv_block() >= a.wgs) return;
+  int w = kv_block();
   const int split = w % a.nsplit;
   w /= a.nsplit;
   const int rt = w % a.tiles;
@@ -575,9 +577,11 @@ __global__ __launch_bounds__(64 * PG_W, 2) void k_paged_tile(PagedArgs a) {
   // them, the longest sequence of all its heads first (8 sequences in pieces of up to 256 over up to 4096 keys, 32
   // heads: 101 us, head after head 119; 8-bit 120 and 157); else a contiguous range of (head, sequence) pairs.  The
   // row tiles that read one sequence's keys share its L2, and sequences of different lengths load the XCDs alike.
-  const int xcd = (int)(blockIdx.x & 7), hx = a.kv.kv_heads & 7 ? 0 : a.kv.kv_heads >> 3;
-  int w = (int)(blockIdx.x >> 3);
-  if (!hx) w += xcd * (int)(gridDim.x >> 3) + min(xcd, (int)(gridDim.x & 7));
+  const unsigned block = kv_block();
+  if (block >= a.wgs) return;
+  const int xcd = (int)(block & 7), hx = a.kv.kv_heads & 7 ? 0 : a.kv.kv_heads >> 3;
+  int w = (int)(block >> 3);
+  if (!hx) w += xcd * (int)(a.wgs >> 3) + min(xcd, (int)(a.wgs & 7));
   const int rt = a.tiles - 1 - w % a.tiles;  // the last rows see the most keys: they begin first
   w /= a.tiles;
   const int split = w % a.nsplit;
@@ -1123,7 +1127,7 @@ int zo_paged_attention_launch(const KvArgs& kv, const void* Q, long long ldq, vo
   if (split > 64) split = 64;
   if (split > most) split = most;
   if (split < 1) split = 1;
-  if (units * split > 0x7fffffffLL || (split > 1 && units * a.prows > 0x7fffffffLL)) {
+  if (units * split > 0x7fffffffLL) {
     zo_set_error("paged_attention: too many workgroups (%lld)", units * split);
     return ZO_ERR_UNSUPPORTED;
   }
@@ -1137,7 +1141,8 @@ int zo_paged_attention_launch(const KvArgs& kv, const void* Q, long long ldq, vo
     *ws_needed = c.off;
     return ZO_OK;
   }
-  const dim3 grid((unsigned)(units * split)), block(64 * PG_W);
+  const dim3 grid = kv_grid(units * split), block(64 * PG_W);
+  a.wgs = (unsigned)(units * split);
   const bool f16 = kv.dtype == ZO_F16;
 #define ZO_ROWS(F, E, D)                                                                                    \
   if (many) hipLaunchKernelGGL((k_paged_tile<F, E, D>), grid, block, 0, stream, a);                        \
@@ -1158,7 +1163,7 @@ int zo_paged_attention_launch(const KvArgs& kv, const void* Q, long long ldq, vo
   // One team of lanes per row, but for many splits of few rows.
   const int teams = 256 / (kv.dh / 4);
   const bool wide = split > 4 && units * a.prows <= 4096;
-  const dim3 jgrid((unsigned)(units * (wide ? a.prows : (a.prows + teams - 1) / teams)));
+  const dim3 jgrid((unsigned)(units * (wide ? a.prows : (a.prows + teams - 1) / teams)));  // at most 511 units here
 #define ZO_JOIN(F, D)                                                                                       \
   if (wide) hipLaunchKernelGGL((k_paged_join<F, D, 256 / (D / 4)>), jgrid, dim3(256), 0, stream, a);       \
   else hipLaunchKernelGGL((k_paged_join<F, D, 1>), jgrid, dim3(256), 0, stream, a)
