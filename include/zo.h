@@ -687,8 +687,10 @@ typedef struct {
  * a <= 448 need (within [2^-126, 2^120]).  If the call stores the page's first
  * slot, the scale becomes need; else max(scale, need), and where that is
  * larger than before, the page's earlier slots are rounded again to the new
- * scale (exact but for values under 2^-6 of it).  Then code = e4m3(x / scale),
- * to nearest even.  Values that are not finite are stored as NaN.
+ * scale (exact but for values under 2^-6 of it, where the scale was a power of
+ * two as well).  Then code = e4m3(x / scale), the quotient in fp32, both to
+ * nearest even; a page that the caller filled may have any positive scale.
+ * Values that are not finite are stored as NaN.
  * One call must not store into one page from two sequences or through two
  * entries of the table, and no tensor of the call may overlap another but
  * Q_out = Q.

@@ -163,10 +163,15 @@ __device__ __forceinline__ uint32_t codes4(const float* v) {
   w = __builtin_amdgcn_cvt_pk_fp8_f32(v[2], v[3], w, true);
   return (uint32_t)w;
 }
-__device__ __forceinline__ u32x2 codes8(const float* v, float inv) {
+// inv = 1 / to: v inv is v / to where to is a power of two, as all scales are that this file forms; with another one's
+// scale it is made so by what is left of v.
+__device__ __forceinline__ u32x2 codes8(const float* v, float to, float inv) {
   float x[8];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) x[e] = fabsf(v[e]) < INFINITY ? v[e] * inv : __builtin_nanf("");
+  for (int e = 0; e < 8; ++e) {
+    const float q = v[e] * inv;
+    x[e] = fabsf(v[e]) < INFINITY ? fmaf(fmaf(-q, to, v[e]), inv, q) : __builtin_nanf("");
+  }
   return (u32x2){codes4(x), codes4(x + 4)};
 }
 
@@ -205,7 +210,7 @@ __device__ __forceinline__ void append_page8(const AppendArgs& a, int s, int jpa
   uint8_t* const base = (uint8_t*)(isk ? kv.K : kv.V) + ((head << kv.log2ps) * DH);
   const float was = old > 0 ? *sc : 0.f;
   const double theta = ROT ? exp2((double)(threadIdx.x & (half - 1)) * a.k) * kInv2Pi : 0.0;
-  float amax = 0.f, inv = 0.f;
+  float amax = 0.f, to = 0.f, inv = 0.f;
 #pragma unroll 1
   for (int pass = 0; pass < 2; ++pass) {
     // 64 rows at a time: their turns fit LDS (and serve both passes where they are all).
@@ -246,8 +251,8 @@ __device__ __forceinline__ void append_page8(const AppendArgs& a, int s, int jpa
               for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fmaxf(finite_abs(f[e]), finite_abs(g[e])));
             } else {
               uint8_t* dst = base + (size_t)(old + c0 + x / CPH) * DH + 8 * (x % CPH);
-              *(u32x2*)dst = codes8(f, inv);
-              *(u32x2*)(dst + half) = codes8(g, inv);
+              *(u32x2*)dst = codes8(f, to, inv);
+              *(u32x2*)(dst + half) = codes8(g, to, inv);
             }
           }
         }
@@ -262,7 +267,7 @@ __device__ __forceinline__ void append_page8(const AppendArgs& a, int s, int jpa
         __syncthreads();
         amax = fmaxf(amax, tops[wave ^ 2]);
       }
-      float to = need_scale(amax);
+      to = need_scale(amax);
       if (old > 0) {
         to = fmaxf(was, to);
         if (to > was) {
