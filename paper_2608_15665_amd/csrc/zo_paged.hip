@@ -6,7 +6,7 @@
 // sequence's new token t.  Softmax in one pass over the keys: a running maximum m, P = 2^((s - m) scale),
 // a running sum of P and of P V, both scaled when m moves (by more than 2^3).
 //
-// k_paged_rows, for rows that read their keys and little else (up to 16, of 8-bit caches 32): a workgroup of 4
+// k_paged_rows, for rows that read their keys and little else (up to 32): a workgroup of 4
 // waves takes 16 NG rows and a range of the keys; its waves take the range's tiles (as many bytes each: 32 keys of 16
 // bits, 64 of 8) in turn, each with a softmax of its own, and join their results in LDS at the end.  K goes from
 // global memory straight into the fragments, a tile ahead.  Ranges of one sequence (nsplit > 1) are joined by
@@ -1108,10 +1108,10 @@ int zo_paged_attention_launch(const KvArgs& kv, const void* Q, long long ldq, vo
     zo_set_error("paged_attention: max_q x heads / kv_heads = %lld or nseq x kv_heads = %lld too many", all_rows, seqs);
     return ZO_ERR_UNSUPPORTED;
   }
-  // Few rows of a sequence and key head read its keys and little else; more share staged tiles.  From 17 to 32 rows
-  // (61 sequences of up to 8192 keys, 20 rows) the staged tiles took 218 us in 16 bits where 32-row workgroups took
-  // 290; in 8 bits, where a staged tile is half as many bytes under way, 202 against 131.
-  const bool many = all_rows > (kv.e8 ? 32 : 16);
+  // Few rows of a sequence and key head read its keys and little else; more share staged tiles.  With 20 rows (40 heads
+  // to 8 of 128), 61 sequences of up to 8192 keys took 209 us here where staged tiles took 220, in 8 bits 124 and 190
+  // (heads of 64: 115 and 122, 80 and 134); 16 sequences of up to 1000 keys 22 and 34, in 8 bits 22 and 40.
+  const bool many = all_rows > 32;
   const int ng = many || all_rows > 16 ? 2 : 1;
   a.rt_rows = many ? PT_Q : 16 * ng;
   a.prows = (int)(all_rows < a.rt_rows ? all_rows : a.rt_rows);
@@ -1146,7 +1146,7 @@ int zo_paged_attention_launch(const KvArgs& kv, const void* Q, long long ldq, vo
   const bool f16 = kv.dtype == ZO_F16;
 #define ZO_ROWS(F, E, D)                                                                                    \
   if (many) hipLaunchKernelGGL((k_paged_tile<F, E, D>), grid, block, 0, stream, a);                        \
-  else if (E && ng == 2) hipLaunchKernelGGL((k_paged_rows<F, E, D, E ? 2 : 1>), grid, block, 0, stream, a); \
+  else if (ng == 2) hipLaunchKernelGGL((k_paged_rows<F, E, D, 2>), grid, block, 0, stream, a);             \
   else hipLaunchKernelGGL((k_paged_rows<F, E, D, 1>), grid, block, 0, stream, a)
 #define ZO_ROWS_D(F, E) \
   if (kv.dh == 64) { ZO_ROWS(F, E, 64); } \
