@@ -5,11 +5,12 @@
 // Bound by the bytes of Q, K and V in and out, or by the latency of a few dependent loads (a length, a page, the
 // row).  A row's angles are the same for all its heads, so a workgroup takes (a part of) one row: 256 items of
 // 16 bytes copied or 32 turned, one per thread, loaded before its first waves form the row's dh / 2 sines and
-// cosines in LDS.  One row per wave instead, eight items after one another, took 37 us where this takes 29 (16 prompts
-// of up to 512 rows, 40 query and 8 key heads of 128: 5.1 TB/s), and a workgroup per whole row 38.
-// A token alone is a launch's latency (3.2 us of the GPU, 61 tokens 4).
-// The 8-bit form: a wave takes one page of one head and tensor, for which it needs the largest magnitude first (61
-// tokens 5 us, 16 prompts of up to 512 rows, 32 heads of 64 unrotated, 17 us: 3.8 TB/s).
+// cosines in LDS.  16 prompts of up to 512 rows, 40 query and 8 key heads of 128: 33 us for 145 MB where the tensors
+// change from call to call (4.4 TB/s), 27 over the same ones again.  One row per wave instead, eight items after one
+// another, took 37 us where this took 29, and a workgroup per whole row 38.
+// A token alone is a launch's latency (3.3 us of the GPU, 61 tokens 3.9).
+// The 8-bit form: one wave or two take one page of one head and tensor, for which they need the largest magnitude first
+// (61 tokens 5.4 us, 16 prompts of up to 512 rows, 32 heads of 64 unrotated, 17.5 us: 3.6 TB/s).
 #include "zo_attn.h"
 #include "zo_kv.h"
 
@@ -178,8 +179,8 @@ __device__ __forceinline__ u32x2 codes8(const float* v, float to, float inv) {
 // One page of one sequence, W waves for one head's K or V: wave w takes tensor w & 1 (K, V) of head 2 part + (w >> 1) or,
 // with W = 2, of head part, each wave every other item.  Two passes
 // over the page's new rows, the largest magnitude and then the codes (the second reads the rows from the caches: held
-// in registers, they left room for half as many waves, and 16 prompts of 512 rows, 8 heads of 128, took 94 us
-// where this takes 57), and one over its earlier slots where the scale grows.
+// in registers, they left room for half as many waves, and 16 prompts of 512 rows, 8 key heads of 128 and 40
+// query heads, took 94 us where this took 57), and one over its earlier slots where the scale grows.
 template <int DT, int DH, bool ROT, int W>
 __device__ __forceinline__ void append_page8(const AppendArgs& a, int s, int jpage, int part, float2 (*turns)[64],
                                              float* tops) {
@@ -335,15 +336,17 @@ int zo_kv_append_launch(const KvArgs& kv, const void* Q, long long ldq, void* Q_
   const dim3 block(256);
   int st = ZO_OK;
   if (kv.e8) {
-    // Q's rows in the pages' launch, or, where they are many, in one of their own: its workgroups need an eighth of
-    // the registers and LDS.
+    // Q's rows in the pages' launch, or, where they are many, in one of their own: its workgroups need half of the
+    // registers and no tables of turns (the prompts above, 64 positions, 40 query heads: 52 us, in one launch 55).
     const bool apart = rows > 1024;
     const long long qb = apart ? 0 : wg;
     a.pages = ((kv.max_q - 1 + (1 << kv.log2ps) - 1) >> kv.log2ps) + 1;
-    // Two waves a page, head and tensor from 128 positions on, for there are few such pages (16 prompts of 512 rows, 8
-    // heads of 128: 128 positions 63.5 us, with one wave 68.6; 256 positions 77 and 89), one below (64 positions 56 and
-    // 54 with two, 16 positions 55 and 65); single tokens are the same with either.
-    const bool two = kv.log2ps >= 7;
+    // Two waves a page, head and tensor from 64 positions on, for there is more to a page and there are fewer of them; one
+    // below.  16 prompts of 512 rows, 8 key heads of 128, without and (in brackets) with 40 rotated query heads, us with
+    // two waves and with one: 256 positions 26 and 36 (73, 84), 128 positions 20 and 24 (61, 65), 64 positions 17 and 19
+    // (49, 52), 32 positions 17.3 and 16.8 (50, 48), 16 positions 22 and 17 (58, 49).  64 prompts of 1024 rows, 32 key
+    // heads: 256 positions 459 and 530, 64 positions 378 and 385.  Single tokens are the same with either.
+    const bool two = kv.log2ps >= 6;
     a.groups = two ? kv.kv_heads : (kv.kv_heads + 1) / 2;
     const long long pages = qb + (long long)kv.nseq * a.pages * a.groups;
     if (pages > 0x7fffffffLL || wg > 0x7fffffffLL) {

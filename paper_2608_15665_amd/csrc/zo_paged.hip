@@ -10,12 +10,12 @@
 // waves takes 16 NG rows and a range of the keys; its waves take the range's tiles (as many bytes each: 32 keys of 16
 // bits, 64 of 8) in turn, each with a softmax of its own, and join their results in LDS at the end.  K goes from
 // global memory straight into the fragments, a tile ahead.  Ranges of one sequence (nsplit > 1) are joined by
-// k_paged_join.  Bound by HBM: 61 tokens with up to 8192 keys each, 40 query heads to 8, 196 us for 1.09 GB (5.5 TB/s,
-// where a kernel that only reads reaches 6.2); one token, 131072 keys, 99 us for 0.54 GB with its join; 8-bit,
-// 61 tokens, 111 us for 0.54 GB.
+// k_paged_join.  Bound by HBM: 61 tokens with up to 8192 keys each, 40 query heads to 8, 198 us for 1.09 GB (5.5 TB/s,
+// where a kernel that only reads reaches 6.0); one token, 131072 keys, 100 us for 0.54 GB with its join; 8-bit,
+// 61 tokens, 112 us for 0.54 GB.
 // k_paged_tile, for more rows: 4 waves of 32 rows share tiles of 64 keys in LDS.  Bound by the MFMAs and the
-// exponentials between them: pieces of up to 1000 tokens of 4 sequences over up to 7000 keys, 333 us, 650 TFLOP/s of
-// visible pairs; 8-bit pieces by the vector instructions that widen the codes.
+// exponentials between them: pieces of up to 1000 tokens of 4 sequences over up to 7000 keys, 330 us, 657 TFLOP/s of
+// visible pairs (986 with the low parts), where a large matrix product reaches 1567; 8-bit pieces by the vector instructions that widen the codes.
 //
 // Products as in the causal attention of whole sequences:
 //   S^T = K Q^T   (16 x 16 x 32 MFMA; A = K rows)
@@ -539,7 +539,7 @@ constexpr int PT_AHEAD = 2;               // LDS reads of a phase that go out be
 // and within a row the 16-byte chunks are permuted by an XOR with swz(row) in two bits, so that the 16 rows of a K
 // fragment, and the 8 (8-bit: 16) rows of a transposed read of V, lie on different banks.  A read's address is then
 // one of one (K) or four (V) per lane, the rest is an immediate offset.
-// 8-bit tiles take 480 vector instructions of a wave beside its 64 MFMAs where 16-bit ones take 240 (128 widen the
+// 8-bit tiles take 600 vector instructions of a wave beside its 96 MFMAs where 16-bit ones take 370 (128 widen the
 // codes, which every wave does for itself, 64 apply the scales): 8 pieces of up to 256 tokens over up to 4096 keys,
 // 32 heads, 142 us (16 bits: 120).  Four buffers of each instead of two, with the loads three tiles ahead, gained
 // nothing (2 % slower), so it is not their latency.
@@ -575,7 +575,7 @@ __global__ __launch_bounds__(64 * PG_W, 2) void k_paged_tile(PagedArgs a) {
 
   // Workgroups are dealt to the 8 XCDs in turn.  Where the key heads are a multiple of 8, each XCD takes as many of
   // them, the longest sequence of all its heads first (8 sequences in pieces of up to 256 over up to 4096 keys, 32
-  // heads: 101 us, head after head 119; 8-bit 120 and 157); else a contiguous range of (head, sequence) pairs.  The
+  // heads: 120 us, head after head 152; 8-bit 142 and 192); else a contiguous range of (head, sequence) pairs.  The
   // row tiles that read one sequence's keys share its L2, and sequences of different lengths load the XCDs alike.
   const unsigned block = kv_block();
   if (block >= a.wgs) return;
@@ -949,7 +949,7 @@ __global__ __launch_bounds__(64 * PG_W, 2) void k_paged_tile(PagedArgs a) {
     ++n;
   };
   // A wave without rows only loads its part of the tiles (32 sequences of up to 4096 keys, 8 new tokens each, 40
-  // query heads to 8: 71.6 us, where it worked on for nothing 73.9; from an 8-bit cache 82.7 and 86.4).
+  // query heads to 8: 84 us, where it worked on for nothing 91; from an 8-bit cache 103 and 110).
   auto wholes = [&](auto ROWS) {
     f32x4 sa[PT_NG][4], sb[PT_NG][4];
     landed();
@@ -1118,7 +1118,11 @@ int zo_paged_attention_launch(const KvArgs& kv, const void* Q, long long ldq, vo
   const long long tiles = (all_rows + a.rt_rows - 1) / a.rt_rows;
   const long long units = seqs * tiles;
   const long long keys = (long long)kv.max_pages << kv.log2ps;
-  // Splits: as many as give 512 workgroups, two per CU (at least that where a split's rows are few).  With 128 units or more a split has 2048 keys at least, for
+  // Splits: as many as give 512 workgroups, two per CU (at least that where a split's rows are few), but 64 at most: with
+  // three key heads and more 64 fill the CUs, and with one or two more of them gained only for the longest of
+  // contexts (one token, 64 and 128 splits: two key heads, 32768 keys 16.3 and 17.3 us, 131072 keys 31.8 and 31.5; four,
+  // 30 and 32, 48.5 and 51 us at 65536 and 131072; one key head 15.1 and 15.2, 31 and 24; with 256 and 512 no better).
+  // With 128 units or more a split has 2048 keys at least, for
   // it costs a partial result (32 sequences of 2000 keys, 8 key heads: 51 us, in halves 55); with fewer, 256, but
   // up to 512 keys stay whole (300 keys of one sequence: 7.8 us, in halves and a second launch 9.3).
   a.min_keys = units < 128 ? 256 : 2048;
