@@ -341,12 +341,13 @@ int zo_kv_append_launch(const KvArgs& kv, const void* Q, long long ldq, void* Q_
     const bool apart = rows > 1024;
     const long long qb = apart ? 0 : wg;
     a.pages = ((kv.max_q - 1 + (1 << kv.log2ps) - 1) >> kv.log2ps) + 1;
-    // Two waves a page, head and tensor from 64 positions on, for there is more to a page and there are fewer of them; one
-    // below.  16 prompts of 512 rows, 8 key heads of 128, without and (in brackets) with 40 rotated query heads, us with
-    // two waves and with one: 256 positions 26 and 36 (73, 84), 128 positions 20 and 24 (61, 65), 64 positions 17 and 19
-    // (49, 52), 32 positions 17.3 and 16.8 (50, 48), 16 positions 22 and 17 (58, 49).  64 prompts of 1024 rows, 32 key
-    // heads: 256 positions 459 and 530, 64 positions 378 and 385.  Single tokens are the same with either.
-    const bool two = kv.log2ps >= 6;
+    // Two waves a page, head and tensor where a page of 64 positions or more may get more rows than one wave loads at
+    // once (128 pairs of 8 values): there is more to such a page, and there are fewer of them.  16 prompts of 512 rows, 8 key
+    // heads of 128, without and (in brackets) with 40 rotated query heads, us with two waves and with one: 256 positions
+    // 26 and 36 (73, 84), 128 positions 20 and 24 (61, 65), 64 positions 17 and 19 (49, 52), 32 positions 17.3 and 16.8
+    // (50, 48), 16 positions 22 and 17 (58, 49).  Single tokens of 61 sequences 5.0 and 4.6 (5.7, 5.2), of 200 7.7 and 6.3
+    // (9.8, 7.6), of one 4.2 and 4.7 (4.7, 5.2), with pages of any size, in a graph.
+    const bool two = kv.log2ps >= 6 && (long long)kv.max_q * (kv.dh / 16) > 128;
     a.groups = two ? kv.kv_heads : (kv.kv_heads + 1) / 2;
     const long long pages = qb + (long long)kv.nseq * a.pages * a.groups;
     if (pages > 0x7fffffffLL || wg > 0x7fffffffLL) {
