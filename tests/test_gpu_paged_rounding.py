@@ -8,7 +8,8 @@ import pytest
 import torch
 
 import paper_2608_15665_amd as zo
-from _paged import DT, attend, batch, bits, check_attention, dev, rows16
+from _paged import DT, attend, batch, bits, check_attention, dev, host64, rows16
+from oracle import paged as op
 
 pytestmark = pytest.mark.gpu
 
@@ -57,3 +58,31 @@ def test_equal_calls_give_equal_bits(news, lens, width, cache):
     first = call()
     for _ in range(5):
         np.testing.assert_array_equal(call(), first)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f16"])
+@pytest.mark.parametrize("news,heads,n", [([70], 1, 500), ([40], 3, 1000), ([200], 2, 3000), ([3], 2, 500)])
+def test_an_infinity_among_earlier_values(news, heads, n, dt):
+    """In a tile that every row sees, and with a weight that has no low part (equal logits: all weights are powers of
+    two where 2^i keys tie, and 1 of the running maximum): the pair's product is the infinity, of its sign, not a NaN."""
+    rng = np.random.default_rng(n)
+    dh = 64
+    for q, where in ((rng.standard_normal((news[0], heads * dh)), 100), (np.zeros((news[0], heads * dh)), 3)):
+        v = rng.standard_normal((1, n, dh))
+        table, q_start, kv_len, pages = batch(rng, [n], news, 16)
+        Q, Qv = rows16(q, dt)
+        pool = [np.zeros((pages, 1, 16, dh)) for _ in range(2)]
+        k = rng.standard_normal((1, n, dh))
+        k[0, where] *= 2.0
+        v[0, where, 5], v[0, where + 1, 9], v[0, where + 64, 20], v[0, where + 65, 21] = np.inf, -np.inf, np.nan, np.inf
+        for t in range(n):
+            pool[0][table[0, t // 16], :, t % 16] = k[:, t]
+            pool[1][table[0, t // 16], :, t % 16] = v[:, t]
+        kd, vd = (dev(x, DT[dt]) for x in pool)
+        got = host64(zo.paged_attention(Q, kd, vd, dev(table), dev(kv_len), q_start=dev(q_start), max_q=news[0]))
+        got = got.reshape(news[0], heads, dh)
+        held = [np.where(np.isfinite(host64(x)), host64(x), 0.0) for x in (kd, vd)]
+        ref, mag = op.paged_attention(Qv.reshape(news[0], heads, dh), held, table, q_start, kv_len)
+        assert np.all(got[..., [5, 21]] == np.inf) and np.all(got[..., 9] == -np.inf) and np.all(np.isnan(got[..., 20]))
+        rest = [d for d in range(dh) if d not in (5, 9, 20, 21)]
+        check_attention(got[..., rest], ref[..., rest], mag[..., rest], dt, (n, where))
