@@ -728,6 +728,150 @@ int zo_paged_attention(const zo_kv_cache* cache, const zo_kv_batch* batch,
                        void* O, long long ldo, void* workspace,
                        size_t ws_bytes, void* stream);
 
+/* ------------------------------------------------------------------------
+ * The two ends of a language model -- tokens in, log-probabilities and losses
+ * out, with the gradients that train what no subspace covers (the embedding
+ * and the head).  The losses take every query block's log-probabilities at
+ * once and give one float64 loss each, for zo_combine_central / _forward.
+ * Tokens, labels and sequence starts are device int32.
+ * ------------------------------------------------------------------------ */
+
+/* Embedding: H[t] = round(scale E[ids[t]]) for t < rows.
+ *   ids       device int32 [rows].  Below 0: padding, a row of zeros.
+ *   E, H      device, vocab x d and rows x d, both of dtype (ZO_F32, ZO_BF16
+ *             or ZO_F16).  H overlaps neither E nor ids.
+ *   bad_flag  device int, nullable: set to 1 (never cleared here) when a token
+ *             is >= vocab; its row of H is NaN.
+ * The product is taken in fp32 and rounded once.  rows = 0 launches nothing.
+ * Limits: 0 <= rows <= 2^30; vocab >= 1; d % 8 == 0, d <= 2^20; 16-byte
+ * aligned E and H; scale finite. */
+int zo_embedding(long long rows, int vocab, int d, int dtype, const int* ids,
+                 const void* E, float scale, void* H, int* bad_flag,
+                 void* stream);
+
+/* The table's gradient from the gradient dH of H:
+ *   G[v] = scale sum_{t: ids[t] = v} dH[t];
+ *   dE = round(G) for every v (zeros for a token that does not occur), or with
+ *   accumulate != 0: dE[v] = round(dE[v] + G[v]) for the tokens that occur,
+ *   other rows untouched.
+ * Tokens are sorted (a stable radix sort) and each token's rows summed in fp32
+ * in an order fixed by ids alone, so equal calls give equal bits.
+ * accumulate == 0 writes dE twice where it writes zeros first: nothing else may
+ * read it while the call runs.  Negative tokens are left out, and so are those
+ * >= vocab, which set bad_flag.
+ *   dH   device, rows x d of dtype.      dE   device, vocab x d of out_dtype:
+ *        dtype or ZO_F32.  It overlaps no other tensor of the call.
+ * Limits: 0 <= rows <= 2^24; vocab < 2^30; the rest as for zo_embedding; the
+ * workspace is not shared with a call that may run at the same time. */
+size_t zo_embedding_backward_workspace(long long rows, int vocab, int d);
+int zo_embedding_backward(long long rows, int vocab, int d, int dtype,
+                          const int* ids, const void* dH, float scale,
+                          int out_dtype, void* dE, int accumulate,
+                          int* bad_flag, void* workspace, size_t ws_bytes,
+                          void* stream);
+
+/* Log-probabilities of labelled tokens, for nblk blocks of T rows of logits X:
+ * row i = b T + t of block b, with label y = labels[t],
+ *   lse[i] = log sum_{j < vocab} exp(scale X[i][j]),
+ *   logp[i] = scale X[i][y] - lse[i].
+ * y < 0: the row does not count; it is not read, logp[i] = lse[i] = 0.
+ * y >= vocab: logp[i] = NaN and bad_flag (device int, nullable) is set to 1.
+ *   X      device, nblk T rows of vocab elements of dtype (ZO_F32, ZO_BF16 or
+ *          ZO_F16), ld elements apart (ld >= vocab: a padded head's columns
+ *          behind the vocabulary are not read).
+ *   logp   device fp32 [nblk T].          lse   the same, nullable.
+ * A logit may be -infinity or the type's lowest value (a masked token); a row
+ * with a NaN or +infinity, or with nothing but -infinity, gives NaN in logp.
+ * Sums are taken in fp32 relative to the row's largest logit, logarithm and
+ * differences in fp64, one rounding at the end: logp does not lose where lse
+ * is large.
+ * Limits: nblk >= 1, T >= 0, nblk T < 2^31; 1 <= vocab <= ld < 2^31; scale finite
+ * and > 0; tensors aligned to their elements. */
+int zo_token_logprob(int nblk, int T, int vocab, int dtype, const void* X,
+                     long long ld, const int* labels, float scale, float* logp,
+                     float* lse, int* bad_flag, void* stream);
+
+/* The logits' gradient from the gradient g of logp (device fp32 [nblk T]):
+ *   dX[i][j] = round(scale g[i] ([j = y] - exp(scale X[i][j] - lse[i])))
+ * with lse as zo_token_logprob gave it (fp32: where |lse| is large, so is its
+ * rounding, and exp() is |lse| 2^-24 off).  y < 0: zeros (X and g not read);
+ * y >= vocab: NaN and bad_flag.  dX has X's layout and dtype, rows ldo apart;
+ * it may be X itself (ldo = ld).  Columns behind the vocabulary stay as they
+ * are.  fp32 arithmetic, one rounding.  Limits as for zo_token_logprob. */
+int zo_token_logprob_backward(int nblk, int T, int vocab, int dtype,
+                              const void* X, long long ld, const int* labels,
+                              float scale, const float* lse, const float* g,
+                              void* dX, long long ldo, int* bad_flag,
+                              void* stream);
+
+/* Sequences of a loss: row t of sequence s for seq_start[s] <= t <
+ * seq_start[s + 1] (device int32 [nseq + 1], not decreasing, within [0, rows]);
+ * rows in no sequence are neither read nor written.  A row counts if
+ * labels is NULL or labels[t] >= 0 (device int32 [rows]); what does not count
+ * may hold anything, NaN included, and gets a gradient of 0.  A seq_start that
+ * breaks the rule sets bad_flag (device int, nullable, never cleared here) and
+ * is taken as clamped to it.  Tensors of a block are `rows` apart; what is not
+ * per block is shared by all blocks.
+ *
+ * Preference loss: sequence 2p is the chosen, 2p + 1 the rejected one of pair
+ * p < pairs.  With the sums over the rows that count
+ *   R_s = w_s sum (logp - ref_logp),   w_s = 1, or 1 / their number (average),
+ *   z = R_2p - R_2p+1 - margin,   h = beta z,
+ * the pair's loss l is
+ *   ZO_PREF_SIGMOID  -(1 - smoothing) log sigma(h) - smoothing log sigma(-h)
+ *   ZO_PREF_HINGE    max(0, 1 - h)
+ *   ZO_PREF_IPO      (z - 1 / (2 beta))^2
+ * and loss[b] = weight / pairs sum_p l.  A pair one of whose sequences has no
+ * row that counts adds 0 and has no gradient.
+ *   logp      device fp32 [nblk x rows]; ref_logp device fp32 [rows], NULL: 0.
+ *   loss      device float64 [nblk].
+ *   rewards   device fp32 [nblk x 2 pairs], nullable: beta R_s (0 for a
+ *             sequence without rows that count).
+ *   dlogp     device fp32 [nblk x rows], nullable: the gradient of loss[b].
+ * float64 arithmetic throughout; sums in a fixed order.
+ * Limits: 1 <= nblk <= 65535, 1 <= pairs <= 2^22, rows >= 0, nblk rows and
+ * nblk pairs < 2^31;
+ * beta finite and > 0, margin and weight finite, 0 <= smoothing <= 0.5 (0 but for
+ * ZO_PREF_SIGMOID). */
+typedef enum { ZO_PREF_SIGMOID = 0, ZO_PREF_HINGE = 1, ZO_PREF_IPO = 2 } zo_preference;
+size_t zo_preference_loss_workspace(int nblk, int rows, int pairs);
+int zo_preference_loss(int nblk, int rows, int pairs, int kind, int average,
+                       double beta, double margin, double smoothing,
+                       double weight,
+                       const float* logp, const float* ref_logp,
+                       const int* labels, const int* seq_start, double* loss,
+                       float* rewards, float* dlogp, int* bad_flag,
+                       void* workspace, size_t ws_bytes, void* stream);
+
+/* Clipped policy loss with a KL term over the same kind of sequences: for a row
+ * that counts, with its advantage A,
+ *   r = exp(logp - old_logp),   c = min(max(r, 1 - clip_low), 1 + clip_high),
+ *   l = -min(r A, c A) + kl_coef k,   k = exp(d) - d - 1,   d = ref_logp - logp,
+ *   loss[b] = weight sum over sequences and rows of l times
+ *     ZO_AGG_TOKEN     1 / N, N the rows that count in all sequences
+ *     ZO_AGG_SEQUENCE  1 / (nseq n_s), n_s those of its sequence
+ *     ZO_AGG_SUM       1
+ *   (a sum over no rows is 0).  The gradient of l is [r A <= c A] (-r A) +
+ *   kl_coef (1 - exp(d)).
+ *   old_logp    device fp32 [rows].
+ *   ref_logp    device fp32 [rows]; NULL: no KL term (kl_coef is then 0).
+ *   advantage   device fp32, [rows] with per_token != 0, else [nseq].
+ *   stats       device float64 [nblk x 2], nullable: the mean of k and the share
+ *               of rows with r A > c A, over the N rows.
+ *   logp, loss, dlogp, and the arithmetic as for zo_preference_loss.
+ * Limits: those of zo_preference_loss with nseq for pairs; clip_low in [0, 1],
+ * clip_high finite and >= 0, kl_coef finite and >= 0, weight finite. */
+typedef enum { ZO_AGG_TOKEN = 0, ZO_AGG_SEQUENCE = 1, ZO_AGG_SUM = 2 } zo_aggregate;
+size_t zo_policy_loss_workspace(int nblk, int rows, int nseq);
+int zo_policy_loss(int nblk, int rows, int nseq, int aggregate, int per_token,
+                   double clip_low, double clip_high, double kl_coef,
+                   double weight,
+                   const float* logp, const float* old_logp,
+                   const float* ref_logp, const float* advantage,
+                   const int* labels, const int* seq_start, double* loss,
+                   double* stats, float* dlogp, int* bad_flag, void* workspace,
+                   size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

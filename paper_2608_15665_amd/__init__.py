@@ -23,6 +23,15 @@ of include/zo.h); this package only binds it.  Entry points:
                            answering with a tuned model: a layer's paged key/value cache
                            (16-bit, or e4m3 with a scale per page and head), appended to with
                            the rotation on the way, and the causal attention that reads it
+    embedding, embedding_backward
+                           a model's first step, rows of a table by token, and the table's gradient
+                           by sorted tokens
+    token_logprob, token_logprob_backward
+                           its last: the labels' log-probabilities over the vocabulary for all query
+                           blocks, and the logits' gradient
+    preference_loss, policy_loss
+                           losses over sequences of token log-probabilities, one per query block
+                           (float64, for the estimates below), with their gradients
     subspace_adam_update   subspace Adam and W <- W - lr U S V^T (Eqs. 6-10)
     subspace_sgd_update    plain subspace SGD, W <- W - lr U Zbar V^T
     sq_loss, combine_central, combine_forward   loss and estimate helpers (central
@@ -31,12 +40,13 @@ of include/zo.h); this package only binds it.  Entry points:
 from ._lib import (ZO_BF16, ZO_E4M3, ZO_EPI_NONE, ZO_EPI_RELU, ZO_EPI_RESIDUAL, ZO_EPI_SILU_MUL, ZO_F16, ZO_F32, ZO_MAX_BLOCKS,
                    ZO_MAX_QR_RANK, ZO_MAX_RANK, ZO_NOALLOC_SCRATCH_BYTES, ABI_SYMBOLS, LIB_PATH, DecoderLayer, LlamaLayer,
                    LlamaLoraLayer, LoraPerturbedLinear, PerturbedLinear, Workspace, ZoError, abi_version, causal_attention, combine_central,
-                   combine_forward, kv_append, layernorm, lib, lora_perturbed_linear, paged_attention, perturbed_linear, prepare_group, rmsnorm, rope,
-                   sq_loss, subspace_adam_update, subspace_refresh, subspace_refresh_noalloc,
-                   subspace_sgd_update)
+                   combine_forward, embedding, embedding_backward, kv_append, layernorm, lib, lora_perturbed_linear,
+                   paged_attention, perturbed_linear, policy_loss, preference_loss, prepare_group, rmsnorm, rope, sq_loss, subspace_adam_update, subspace_refresh, subspace_refresh_noalloc,
+                   subspace_sgd_update, token_logprob, token_logprob_backward)
 
 __all__ = ["ZO_BF16", "ZO_E4M3", "ZO_EPI_NONE", "ZO_EPI_RELU", "ZO_EPI_RESIDUAL", "ZO_EPI_SILU_MUL", "ZO_F16", "ZO_F32", "ZO_MAX_BLOCKS",
            "ZO_MAX_QR_RANK", "ZO_MAX_RANK", "ZO_NOALLOC_SCRATCH_BYTES", "ABI_SYMBOLS", "LIB_PATH", "DecoderLayer", "LlamaLayer", "LlamaLoraLayer", "LoraPerturbedLinear",
            "PerturbedLinear", "Workspace", "ZoError", "abi_version", "causal_attention", "combine_central",
-           "combine_forward", "kv_append", "layernorm", "lib", "lora_perturbed_linear", "paged_attention", "perturbed_linear", "prepare_group", "rmsnorm", "rope", "sq_loss",
-           "subspace_adam_update", "subspace_refresh", "subspace_refresh_noalloc", "subspace_sgd_update"]
+           "combine_forward", "embedding", "embedding_backward", "kv_append", "layernorm", "lib", "lora_perturbed_linear", "paged_attention", "perturbed_linear",
+           "policy_loss", "preference_loss", "prepare_group", "rmsnorm", "rope", "sq_loss",
+           "subspace_adam_update", "subspace_refresh", "subspace_refresh_noalloc", "subspace_sgd_update", "token_logprob", "token_logprob_backward"]

@@ -43,9 +43,14 @@ ABI_SYMBOLS = (
     "zo_perturbed_linear_group_workspace", "zo_perturbed_linear_prepare_group",
     "zo_subspace_refresh_noalloc",
     "zo_kv_append", "zo_paged_attention_workspace", "zo_paged_attention",
+    "zo_embedding", "zo_embedding_backward_workspace", "zo_embedding_backward",
+    "zo_token_logprob", "zo_token_logprob_backward",
+    "zo_preference_loss_workspace", "zo_preference_loss", "zo_policy_loss_workspace", "zo_policy_loss",
 )
 ZO_NOALLOC_SCRATCH_BYTES = 64 << 20
 ZO_EPI_NONE, ZO_EPI_RELU, ZO_EPI_RESIDUAL, ZO_EPI_SILU_MUL = 0, 1, 2, 3
+PREFERENCES = {"sigmoid": 0, "hinge": 1, "ipo": 2}
+AGGREGATES = {"token": 0, "sequence": 1, "sum": 2}
 
 
 class Matrix(ctypes.Structure):
@@ -226,6 +231,26 @@ def lib() -> ctypes.CDLL:
             L.zo_paged_attention_workspace.argtypes = [cache_p, batch_p, c_int, c_int]
             L.zo_paged_attention.restype = c_int
             L.zo_paged_attention.argtypes = [cache_p, batch_p, c_int, c_int, c_vp, c_ll, c_vp, c_ll, c_vp, c_sz, c_vp]
+            c_d = ctypes.c_double
+            L.zo_embedding.restype = c_int
+            L.zo_embedding.argtypes = [c_ll, c_int, c_int, c_int, c_vp, c_vp, c_f, c_vp, c_vp, c_vp]
+            L.zo_embedding_backward_workspace.restype = c_sz
+            L.zo_embedding_backward_workspace.argtypes = [c_ll, c_int, c_int]
+            L.zo_embedding_backward.restype = c_int
+            L.zo_embedding_backward.argtypes = [c_ll, c_int, c_int, c_int, c_vp, c_vp, c_f, c_int, c_vp, c_int, c_vp, c_vp,
+                                                c_sz, c_vp]
+            L.zo_token_logprob.restype = c_int
+            L.zo_token_logprob.argtypes = [c_int] * 4 + [c_vp, c_ll, c_vp, c_f, c_vp, c_vp, c_vp, c_vp]
+            L.zo_token_logprob_backward.restype = c_int
+            L.zo_token_logprob_backward.argtypes = [c_int] * 4 + [c_vp, c_ll, c_vp, c_f, c_vp, c_vp, c_vp, c_ll, c_vp, c_vp]
+            L.zo_preference_loss_workspace.restype = c_sz
+            L.zo_preference_loss_workspace.argtypes = [c_int] * 3
+            L.zo_preference_loss.restype = c_int
+            L.zo_preference_loss.argtypes = [c_int] * 5 + [c_d] * 4 + [c_vp] * 9 + [c_sz, c_vp]
+            L.zo_policy_loss_workspace.restype = c_sz
+            L.zo_policy_loss_workspace.argtypes = [c_int] * 3
+            L.zo_policy_loss.restype = c_int
+            L.zo_policy_loss.argtypes = [c_int] * 5 + [c_d] * 4 + [c_vp] * 11 + [c_sz, c_vp]
             _lib = L
     return _lib
 
@@ -1099,3 +1124,211 @@ def combine_forward(L: torch.Tensor, eps: float, out: Optional[torch.Tensor] = N
     _need(out, "g", torch.float32, q)
     _check(lib().zo_combine_forward(q, L.data_ptr(), float(eps), out.data_ptr(), _stream_handle()))
     return out
+
+
+# ---------------------------------------------------------------------------
+def _here(t: torch.Tensor, name: str, dtype, here: int, numel: int) -> int:
+    """The address of a dense tensor of `numel` elements of the type on the current device."""
+    p = _kv_tensor(t, name, dtype, here)
+    if t.numel() != numel:
+        raise ValueError(f"{name} must hold {numel} elements (got {t.numel()})")
+    return p
+
+
+def _flag(bad_flag: Optional[torch.Tensor], here: int) -> Optional[int]:
+    return None if bad_flag is None else _here(bad_flag, "bad_flag", torch.int32, here, 1)
+
+
+def _fits(n: int, what: str) -> None:
+    if not 0 <= n < 1 << 31:  # an int of the call would wrap
+        raise ValueError(f"{what}: {n} out of range")
+
+
+def _own_ws(workspace: Optional[torch.Tensor], need: int, here: int):
+    """(tensor to keep, address, bytes) of a call's workspace: the caller's, or one of the call's own (calls are several
+    launches, and a graph may be replayed beside another)."""
+    if workspace is not None:
+        return workspace, _kv_tensor(workspace, "workspace", torch.uint8, here), workspace.numel()
+    buf = torch.empty(need, dtype=torch.uint8, device=f"cuda:{here}")
+    return buf, buf.data_ptr(), need
+
+
+def embedding(ids: torch.Tensor, table: torch.Tensor, scale: float = 1.0, out: Optional[torch.Tensor] = None,
+              bad_flag: Optional[torch.Tensor] = None):
+    """Rows of table (vocab x d) by token, scaled: ids.shape x d in the table's type.  ids: int32, below 0 for padding (a
+    row of zeros); bad_flag (one int32) is set where a token is not below vocab, whose row is NaN.  See zo_embedding."""
+    here = torch._C._cuda_getDevice()
+    if table.dtype not in _DT:
+        raise TypeError(f"unsupported dtype {table.dtype}")
+    if table.dim() != 2:
+        raise ValueError("table must be vocab x d")
+    vocab, d = table.shape
+    _fits(vocab, "vocab")
+    rows = ids.numel()
+    if out is None:
+        out = torch.empty((*ids.shape, d), dtype=table.dtype, device=table.device)
+    _check(lib().zo_embedding(rows, vocab, d, _DT[table.dtype], _kv_tensor(ids, "ids", torch.int32, here),
+                              _kv_tensor(table, "table", table.dtype, here), scale,
+                              _here(out, "out", table.dtype, here, rows * d), _flag(bad_flag, here), _stream_handle()))
+    return out
+
+
+def embedding_backward(ids: torch.Tensor, grad: torch.Tensor, vocab: int, scale: float = 1.0,
+                       out: Optional[torch.Tensor] = None, accumulate: bool = False,
+                       bad_flag: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
+    """The gradient (vocab x d; fp32 if no out is given, else out's type: fp32 or grad's) of embedding's table from grad, the
+    gradient of its result: scaled sums of each token's rows, zeros elsewhere; with accumulate, added to out, whose other
+    rows are not touched.  Without a workspace (uint8) the call allocates its own.  See zo_embedding_backward."""
+    here = torch._C._cuda_getDevice()
+    dt = grad.dtype
+    if dt not in _DT:
+        raise TypeError(f"unsupported dtype {dt}")
+    rows, d = ids.numel(), grad.shape[-1]
+    _fits(vocab, "vocab")
+    if out is None:
+        if accumulate:
+            raise ValueError("accumulate needs out")
+        out = torch.empty((vocab, d), dtype=torch.float32, device=grad.device)
+    if out.dtype not in _DT:
+        raise TypeError(f"unsupported dtype {out.dtype}")
+    L = lib()
+    ids_p, grad_p = _kv_tensor(ids, "ids", torch.int32, here), _here(grad, "grad", dt, here, rows * d)
+    out_p, flag = _here(out, "out", out.dtype, here, vocab * d), _flag(bad_flag, here)
+    _keep, ws, ws_n = _own_ws(workspace, L.zo_embedding_backward_workspace(rows, vocab, d), here)
+    _check(L.zo_embedding_backward(rows, vocab, d, _DT[dt], ids_p, grad_p, scale, _DT[out.dtype], out_p, int(accumulate), flag,
+                                   ws, ws_n, _stream_handle()))
+    return out
+
+
+def _logits(X: torch.Tensor, labels: torch.Tensor, vocab: Optional[int], here: int):
+    """(nblk, T, vocab, row distance, labels' address) of rows of logits for T labels."""
+    if X.dtype not in _DT:
+        raise TypeError(f"unsupported dtype {X.dtype}")
+    if X.dim() != 2:
+        raise ValueError("logits must be rows x columns")
+    n, cols = X.shape
+    vocab = cols if vocab is None else int(vocab)
+    T = labels.numel()
+    if vocab > cols:
+        raise ValueError(f"logits of {cols} columns for a vocabulary of {vocab}")
+    if n != 0 if T == 0 else n % T != 0 or n == 0:
+        raise ValueError(f"logits must hold blocks of T = {T} rows, one for each label (got {n} rows)")
+    _fits(max(n, cols), "rows or columns of logits")
+    ld = _row_tensor(X, "logits", X.dtype, n, cols, here)
+    return (n // T if T else 1), T, vocab, ld, _kv_tensor(labels, "labels", torch.int32, here)
+
+
+def token_logprob(logits: torch.Tensor, labels: torch.Tensor, vocab: Optional[int] = None, scale: float = 1.0,
+                  logp: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                  bad_flag: Optional[torch.Tensor] = None):
+    """(logp, lse), fp32, of logits (nblk T rows; the first `vocab` columns, default all) scaled by `scale`: each row's
+    log-probability of its label (labels: int32, T of them shared by the blocks; below 0: not counted, 0) and its
+    log-sum-exp.  bad_flag (one int32) is set where a label is not below vocab.  See zo_token_logprob."""
+    here = torch._C._cuda_getDevice()
+    nblk, T, vocab, ld, lab = _logits(logits, labels, vocab, here)
+    n = nblk * T
+    if logp is None:
+        logp = torch.empty(n, dtype=torch.float32, device=logits.device)
+    if lse is None:
+        lse = torch.empty(n, dtype=torch.float32, device=logits.device)
+    _check(lib().zo_token_logprob(nblk, T, vocab, _DT[logits.dtype], logits.data_ptr(), ld, lab, scale,
+                                  _here(logp, "logp", torch.float32, here, n), _here(lse, "lse", torch.float32, here, n),
+                                  _flag(bad_flag, here), _stream_handle()))
+    return logp, lse
+
+
+def token_logprob_backward(logits: torch.Tensor, labels: torch.Tensor, lse: torch.Tensor, grad: torch.Tensor,
+                           vocab: Optional[int] = None, scale: float = 1.0, out: Optional[torch.Tensor] = None,
+                           bad_flag: Optional[torch.Tensor] = None):
+    """The logits' gradient from grad, the gradient of token_logprob's logp, with its lse: in out (the logits' shape and
+    type; it may be the logits themselves; columns behind `vocab` are left as they are) or a new tensor, zeros there.
+    See zo_token_logprob_backward."""
+    here = torch._C._cuda_getDevice()
+    nblk, T, vocab, ld, lab = _logits(logits, labels, vocab, here)
+    n, cols = logits.shape
+    if out is None:
+        out = (torch.empty if vocab == cols else torch.zeros)((n, cols), dtype=logits.dtype, device=logits.device)
+    ldo = _row_tensor(out, "out", logits.dtype, n, cols, here)
+    _check(lib().zo_token_logprob_backward(nblk, T, vocab, _DT[logits.dtype], logits.data_ptr(), ld, lab, scale,
+                                           _here(lse, "lse", torch.float32, here, n),
+                                           _here(grad, "grad", torch.float32, here, n), out.data_ptr(), ldo,
+                                           _flag(bad_flag, here), _stream_handle()))
+    return out
+
+
+def _blocks(logp: torch.Tensor):
+    """(nblk, rows) of log-probabilities: nblk x rows, or the rows of one block."""
+    if logp.dim() not in (1, 2):
+        raise ValueError("logp must be nblk x rows, or rows")
+    _fits(max(logp.numel(), *logp.shape), "log-probabilities")
+    return (1, logp.shape[0]) if logp.dim() == 1 else logp.shape
+
+
+def _optional(t: Optional[torch.Tensor], name: str, dtype, here: int, numel: int) -> Optional[int]:
+    return None if t is None else _here(t, name, dtype, here, numel)
+
+
+def _loss_out(loss: Optional[torch.Tensor], nblk: int, like: torch.Tensor) -> torch.Tensor:
+    return torch.empty(nblk, dtype=torch.float64, device=like.device) if loss is None else loss
+
+
+def preference_loss(logp: torch.Tensor, seq_start: torch.Tensor, beta: float, ref_logp: Optional[torch.Tensor] = None,
+                    labels: Optional[torch.Tensor] = None, kind: str = "sigmoid", average: bool = False, margin: float = 0.0,
+                    label_smoothing: float = 0.0, weight: float = 1.0, loss: Optional[torch.Tensor] = None,
+                    rewards: Optional[torch.Tensor] = None, dlogp: Optional[torch.Tensor] = None,
+                    bad_flag: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
+    """The preference loss (float64, one per block) of pairs of sequences from their tokens' log-probabilities logp (fp32,
+    nblk x rows): sequence 2p is the chosen, 2p + 1 the rejected one, rows seq_start[s] .. seq_start[s + 1] - 1 (int32,
+    2 pairs + 1).  ref_logp: the reference's (rows, shared by the blocks); labels (int32, rows): rows below 0 do not count;
+    kind: "sigmoid", "hinge" or "ipo".  rewards (fp32, nblk x 2 pairs) and dlogp (fp32, as logp: the gradient, times
+    weight as the loss) are filled where given.  Returns loss.  See zo_preference_loss."""
+    here = torch._C._cuda_getDevice()
+    if kind not in PREFERENCES:
+        raise ValueError(f"kind must be one of {sorted(PREFERENCES)} (got {kind!r})")
+    nblk, rows = _blocks(logp)
+    pairs = (seq_start.numel() - 1) // 2
+    if seq_start.numel() != 2 * pairs + 1 or pairs < 1:
+        raise ValueError(f"seq_start must hold 2 pairs + 1 elements (got {seq_start.numel()})")
+    loss = _loss_out(loss, nblk, logp)
+    L = lib()
+    tensors = (_kv_tensor(logp, "logp", torch.float32, here), _optional(ref_logp, "ref_logp", torch.float32, here, rows),
+               _optional(labels, "labels", torch.int32, here, rows), _kv_tensor(seq_start, "seq_start", torch.int32, here),
+               _here(loss, "loss", torch.float64, here, nblk),
+               _optional(rewards, "rewards", torch.float32, here, 2 * nblk * pairs),
+               _optional(dlogp, "dlogp", torch.float32, here, nblk * rows), _flag(bad_flag, here))
+    _keep, ws, ws_n = _own_ws(workspace, L.zo_preference_loss_workspace(nblk, rows, pairs), here)
+    _check(L.zo_preference_loss(nblk, rows, pairs, PREFERENCES[kind], int(average), beta, margin, label_smoothing, weight,
+                                *tensors, ws, ws_n, _stream_handle()))
+    return loss
+
+
+def policy_loss(logp: torch.Tensor, old_logp: torch.Tensor, advantage: torch.Tensor, seq_start: torch.Tensor,
+                labels: Optional[torch.Tensor] = None, ref_logp: Optional[torch.Tensor] = None, per_token: bool = False,
+                clip_low: float = 0.2, clip_high: float = 0.2, kl_coef: float = 0.0, aggregate: str = "token",
+                weight: float = 1.0, loss: Optional[torch.Tensor] = None, stats: Optional[torch.Tensor] = None,
+                dlogp: Optional[torch.Tensor] = None, bad_flag: Optional[torch.Tensor] = None,
+                workspace: Optional[torch.Tensor] = None):
+    """The clipped policy loss with a KL term (float64, one per block) of sequences of sampled tokens from their
+    log-probabilities logp (fp32, nblk x rows) and those at the time of sampling, old_logp (rows); advantage: fp32, one per
+    sequence, or per row with per_token; seq_start (int32, nseq + 1), labels and ref_logp as for preference_loss;
+    aggregate: "token", "sequence" or "sum".  stats (float64, nblk x 2: the mean KL term, the share of clipped rows) and
+    dlogp (fp32, as logp: the gradient) are filled where given.  Returns loss.  See zo_policy_loss."""
+    here = torch._C._cuda_getDevice()
+    if aggregate not in AGGREGATES:
+        raise ValueError(f"aggregate must be one of {sorted(AGGREGATES)} (got {aggregate!r})")
+    nblk, rows = _blocks(logp)
+    nseq = seq_start.numel() - 1
+    if nseq < 1:
+        raise ValueError(f"seq_start must hold nseq + 1 elements, nseq >= 1 (got {seq_start.numel()})")
+    loss = _loss_out(loss, nblk, logp)
+    L = lib()
+    tensors = (_kv_tensor(logp, "logp", torch.float32, here), _here(old_logp, "old_logp", torch.float32, here, rows),
+               _optional(ref_logp, "ref_logp", torch.float32, here, rows),
+               _here(advantage, "advantage", torch.float32, here, rows if per_token else nseq),
+               _optional(labels, "labels", torch.int32, here, rows), _kv_tensor(seq_start, "seq_start", torch.int32, here),
+               _here(loss, "loss", torch.float64, here, nblk), _optional(stats, "stats", torch.float64, here, 2 * nblk),
+               _optional(dlogp, "dlogp", torch.float32, here, nblk * rows), _flag(bad_flag, here))
+    _keep, ws, ws_n = _own_ws(workspace, L.zo_policy_loss_workspace(nblk, rows, nseq), here)
+    _check(L.zo_policy_loss(nblk, rows, nseq, AGGREGATES[aggregate], int(per_token), clip_low, clip_high, kl_coef, weight,
+                            *tensors, ws, ws_n, _stream_handle()))
+    return loss

@@ -1123,4 +1123,175 @@ int zo_paged_attention(const zo_kv_cache* cache, const zo_kv_batch* batch, int h
   return zo_paged_attention_launch(a, Q, ldq, O, ldo, workspace, (hipStream_t)stream, nullptr);
 }
 
+// ------------------------------------------------------------------ embedding
+static int check_embedding(const char* what, long long rows, long long most, int vocab, int d, int dtype, const int* ids,
+                           float scale, const int* bad_flag) {
+  ZO_CHECK(rows >= 0 && rows <= most, "%s: rows = %lld outside [0, %lld]", what, rows, most);
+  ZO_CHECK(vocab >= 1 && vocab < (1 << 30), "%s: vocab = %d outside [1, 2^30)", what, vocab);
+  ZO_CHECK(d >= 8 && d % 8 == 0 && d <= (1 << 20), "%s: d = %d (need a multiple of 8, at most 2^20)", what, d);
+  ZO_CHECK(rows * d < (1LL << 40), "%s: rows x d = %lld x %d too large", what, rows, d);
+  ZO_CHECK(dtype == ZO_F32 || dtype == ZO_BF16 || dtype == ZO_F16, "%s: bad dtype %d", what, dtype);
+  ZO_CHECK(isfinite(scale), "%s: scale is not finite", what);
+  ZO_CHECK(rows == 0 || ids, "%s: ids is NULL", what);
+  ZO_CHECK(aligned(ids, 4) && aligned(bad_flag, 4), "%s: ids and bad_flag must be 4-byte aligned", what);
+  return ZO_OK;
+}
+
+int zo_embedding(long long rows, int vocab, int d, int dtype, const int* ids, const void* E, float scale, void* H, int* bad_flag,
+                 void* stream) {
+  const int st = check_embedding("embedding", rows, 1LL << 30, vocab, d, dtype, ids, scale, bad_flag);
+  if (st != ZO_OK || rows == 0) return st;
+  ZO_CHECK(E && H && aligned(E, 16) && aligned(H, 16), "embedding: E or H is NULL or not 16-byte aligned");
+  return zo_embedding_launch(rows, vocab, d, dtype, ids, E, scale, H, bad_flag, (hipStream_t)stream);
+}
+
+size_t zo_embedding_backward_workspace(long long rows, int vocab, int d) {
+  if (check_embedding("embedding_backward", rows, 1LL << 24, vocab, d, ZO_F32, (const int*)16, 1.f, nullptr) != ZO_OK) return 0;
+  size_t need = 0;
+  zo_embedding_backward_launch(rows, vocab, d, ZO_F32, nullptr, nullptr, 1.f, ZO_F32, nullptr, 0, nullptr, nullptr, nullptr,
+                               &need);
+  return need;
+}
+
+// A workspace of at least `need` bytes.
+static int check_ws(const char* what, size_t need, const void* workspace, size_t ws_bytes) {
+  if (need && (ws_bytes < need || !workspace)) {
+    zo_set_error("%s: workspace %zu bytes < required %zu", what, workspace ? ws_bytes : (size_t)0, need);
+    return ZO_ERR_WORKSPACE;
+  }
+  ZO_CHECK(!need || aligned(workspace, 256), "%s: workspace not 256-byte aligned", what);
+  return ZO_OK;
+}
+
+int zo_embedding_backward(long long rows, int vocab, int d, int dtype, const int* ids, const void* dH, float scale, int out_dtype,
+                          void* dE, int accumulate, int* bad_flag, void* workspace, size_t ws_bytes, void* stream) {
+  const char* what = "embedding_backward";
+  int st = check_embedding(what, rows, 1LL << 24, vocab, d, dtype, ids, scale, bad_flag);
+  if (st != ZO_OK) return st;
+  ZO_CHECK(out_dtype == dtype || out_dtype == ZO_F32, "%s: out_dtype %d with rows of dtype %d (the same, or fp32)", what,
+           out_dtype, dtype);
+  if (rows == 0 && accumulate) return ZO_OK;
+  ZO_CHECK(dE && aligned(dE, 16), "%s: dE is NULL or not 16-byte aligned", what);
+  ZO_CHECK(rows == 0 || (dH && aligned(dH, 16)), "%s: dH is NULL or not 16-byte aligned", what);
+  size_t need = 0;
+  zo_embedding_backward_launch(rows, vocab, d, dtype, nullptr, nullptr, 1.f, out_dtype, nullptr, 0, nullptr, nullptr, nullptr,
+                               &need);
+  if ((st = check_ws(what, need, workspace, ws_bytes)) != ZO_OK) return st;
+  return zo_embedding_backward_launch(rows, vocab, d, dtype, ids, dH, scale, out_dtype, dE, accumulate, bad_flag, workspace,
+                                      (hipStream_t)stream, nullptr);
+}
+
+// ------------------------------------------------------------------ token log-probabilities
+static int check_logprob(const char* what, int nblk, int T, int vocab, int dtype, const void* X, long long ld, const int* labels,
+                         float scale, const int* bad_flag) {
+  ZO_CHECK(nblk >= 1 && T >= 0 && (long long)nblk * T < (1LL << 31),
+           "%s: nblk = %d, T = %d (need nblk >= 1, T >= 0, nblk T < 2^31)", what, nblk, T);
+  ZO_CHECK(vocab >= 1 && ld >= vocab && ld < (1LL << 31), "%s: vocab = %d in rows %lld elements apart", what, vocab, ld);
+  ZO_CHECK(dtype == ZO_F32 || dtype == ZO_BF16 || dtype == ZO_F16, "%s: bad dtype %d", what, dtype);
+  ZO_CHECK(isfinite(scale) && scale > 0.f, "%s: scale must be finite and > 0", what);
+  ZO_CHECK(T == 0 || (X && labels), "%s: X or labels is NULL", what);
+  ZO_CHECK(aligned(X, dtype == ZO_F32 ? 4 : 2) && aligned(labels, 4) && aligned(bad_flag, 4), "%s: a tensor is not aligned", what);
+  return ZO_OK;
+}
+
+int zo_token_logprob(int nblk, int T, int vocab, int dtype, const void* X, long long ld, const int* labels, float scale,
+                     float* logp, float* lse, int* bad_flag, void* stream) {
+  const char* what = "token_logprob";
+  const int st = check_logprob(what, nblk, T, vocab, dtype, X, ld, labels, scale, bad_flag);
+  if (st != ZO_OK) return st;
+  if (T == 0) return ZO_OK;
+  ZO_CHECK(logp && aligned(logp, 4) && aligned(lse, 4), "%s: logp is NULL, or logp or lse not 4-byte aligned", what);
+  return zo_token_logprob_launch(nblk, T, vocab, dtype, X, ld, labels, scale, logp, lse, bad_flag, (hipStream_t)stream);
+}
+
+int zo_token_logprob_backward(int nblk, int T, int vocab, int dtype, const void* X, long long ld, const int* labels, float scale,
+                              const float* lse, const float* g, void* dX, long long ldo, int* bad_flag, void* stream) {
+  const char* what = "token_logprob_backward";
+  const int st = check_logprob(what, nblk, T, vocab, dtype, X, ld, labels, scale, bad_flag);
+  if (st != ZO_OK) return st;
+  if (T == 0) return ZO_OK;
+  ZO_CHECK(lse && g && aligned(lse, 4) && aligned(g, 4), "%s: lse or g is NULL or not 4-byte aligned", what);
+  ZO_CHECK(dX && aligned(dX, dtype == ZO_F32 ? 4 : 2), "%s: dX is NULL or not aligned", what);
+  ZO_CHECK(ldo >= vocab && ldo < (1LL << 31), "%s: rows of dX are %lld elements apart (vocab = %d)", what, ldo, vocab);
+  ZO_CHECK(dX != X || ldo == ld, "%s: dX is X, with another row distance", what);
+  return zo_token_logprob_backward_launch(nblk, T, vocab, dtype, X, ld, labels, scale, lse, g, dX, ldo, bad_flag,
+                                          (hipStream_t)stream);
+}
+
+// ------------------------------------------------------------------ losses over sequences
+static int check_seqs(const char* what, int nblk, int rows, int nseq, int most, const char* unit) {
+  ZO_CHECK(nblk >= 1 && nblk <= 65535, "%s: nblk = %d outside [1, 65535]", what, nblk);
+  ZO_CHECK(nseq >= 1 && nseq <= most, "%s: %s = %d outside [1, %d]", what, unit, nseq, most);
+  ZO_CHECK(rows >= 0 && (long long)nblk * rows < (1LL << 31), "%s: rows = %d of %d blocks (need nblk rows < 2^31)", what, rows,
+           nblk);
+  ZO_CHECK((long long)nblk * nseq < (1LL << 31), "%s: %d blocks of %d %s too many", what, nblk, nseq, unit);
+  return ZO_OK;
+}
+
+static int check_seq_tensors(const char* what, int rows, const float* logp, const float* ref, const int* labels,
+                             const int* seq_start, const double* loss, const float* dlogp, const int* bad_flag) {
+  ZO_CHECK(seq_start && loss && (rows == 0 || logp), "%s: logp, seq_start or loss is NULL", what);
+  ZO_CHECK(aligned(logp, 4) && aligned(ref, 4) && aligned(labels, 4) && aligned(seq_start, 4) && aligned(dlogp, 4) &&
+               aligned(bad_flag, 4) && aligned(loss, 8), "%s: a tensor is not aligned to its elements", what);
+  return ZO_OK;
+}
+
+size_t zo_preference_loss_workspace(int nblk, int rows, int pairs) {
+  if (check_seqs("preference_loss", nblk, rows, pairs, 1 << 22, "pairs") != ZO_OK) return 0;
+  size_t need = 0;
+  zo_preference_loss_launch(nblk, rows, pairs, 0, 0, 1.0, 0.0, 0.0, 1.0, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr,
+                            nullptr, nullptr, nullptr, nullptr, &need);
+  return need;
+}
+
+int zo_preference_loss(int nblk, int rows, int pairs, int kind, int average, double beta, double margin, double smoothing,
+                       double weight, const float* logp, const float* ref_logp, const int* labels, const int* seq_start,
+                       double* loss, float* rewards, float* dlogp, int* bad_flag, void* workspace, size_t ws_bytes,
+                       void* stream) {
+  const char* what = "preference_loss";
+  int st = check_seqs(what, nblk, rows, pairs, 1 << 22, "pairs");
+  if (st != ZO_OK) return st;
+  ZO_CHECK(kind == ZO_PREF_SIGMOID || kind == ZO_PREF_HINGE || kind == ZO_PREF_IPO, "%s: bad kind %d", what, kind);
+  ZO_CHECK(isfinite(beta) && beta > 0.0, "%s: beta must be finite and > 0", what);
+  ZO_CHECK(isfinite(margin) && isfinite(weight), "%s: margin or weight is not finite", what);
+  ZO_CHECK(smoothing >= 0.0 && smoothing <= 0.5 && (smoothing == 0.0 || kind == ZO_PREF_SIGMOID),
+           "%s: smoothing = %g (0 to 0.5, and 0 for other kinds than sigmoid)", what, smoothing);
+  if ((st = check_seq_tensors(what, rows, logp, ref_logp, labels, seq_start, loss, dlogp, bad_flag)) != ZO_OK) return st;
+  ZO_CHECK(aligned(rewards, 4), "%s: rewards not 4-byte aligned", what);
+  if ((st = check_ws(what, zo_preference_loss_workspace(nblk, rows, pairs), workspace, ws_bytes)) != ZO_OK) return st;
+  return zo_preference_loss_launch(nblk, rows, pairs, kind, average, beta, margin, smoothing, weight, logp, ref_logp, labels,
+                                   seq_start, loss, rewards, dlogp, bad_flag, workspace, (hipStream_t)stream, nullptr);
+}
+
+size_t zo_policy_loss_workspace(int nblk, int rows, int nseq) {
+  if (check_seqs("policy_loss", nblk, rows, nseq, 1 << 23, "nseq") != ZO_OK) return 0;
+  size_t need = 0;
+  zo_policy_loss_launch(nblk, rows, nseq, 0, 0, 0.0, 0.0, 0.0, 1.0, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr,
+                        nullptr, nullptr, nullptr, nullptr, nullptr, &need);
+  return need;
+}
+
+int zo_policy_loss(int nblk, int rows, int nseq, int aggregate, int per_token, double clip_low, double clip_high, double kl_coef,
+                   double weight, const float* logp, const float* old_logp, const float* ref_logp, const float* advantage,
+                   const int* labels, const int* seq_start, double* loss, double* stats, float* dlogp, int* bad_flag,
+                   void* workspace, size_t ws_bytes, void* stream) {
+  const char* what = "policy_loss";
+  int st = check_seqs(what, nblk, rows, nseq, 1 << 23, "nseq");
+  if (st != ZO_OK) return st;
+  ZO_CHECK(aggregate == ZO_AGG_TOKEN || aggregate == ZO_AGG_SEQUENCE || aggregate == ZO_AGG_SUM, "%s: bad aggregate %d", what,
+           aggregate);
+  ZO_CHECK(clip_low >= 0.0 && clip_low <= 1.0 && clip_high >= 0.0 && isfinite(clip_high),
+           "%s: clip_low = %g outside [0, 1] or clip_high = %g not finite and >= 0", what, clip_low, clip_high);
+  ZO_CHECK(kl_coef >= 0.0 && isfinite(kl_coef), "%s: kl_coef must be finite and >= 0", what);
+  ZO_CHECK(ref_logp || kl_coef == 0.0, "%s: kl_coef = %g without ref_logp", what, kl_coef);
+  ZO_CHECK(isfinite(weight), "%s: weight is not finite", what);
+  if ((st = check_seq_tensors(what, rows, logp, ref_logp, labels, seq_start, loss, dlogp, bad_flag)) != ZO_OK) return st;
+  ZO_CHECK((rows == 0 || old_logp) && (advantage || (per_token && rows == 0)), "%s: old_logp or advantage is NULL", what);
+  ZO_CHECK(aligned(old_logp, 4) && aligned(advantage, 4) && aligned(stats, 8), "%s: a tensor is not aligned to its elements", what);
+  if ((st = check_ws(what, zo_policy_loss_workspace(nblk, rows, nseq), workspace, ws_bytes)) != ZO_OK) return st;
+  return zo_policy_loss_launch(nblk, rows, nseq, aggregate, per_token, clip_low, clip_high, kl_coef, weight, logp, old_logp,
+                               ref_logp, advantage, labels, seq_start, loss, stats, dlogp, bad_flag, workspace,
+                               (hipStream_t)stream, nullptr);
+}
+
 }  // extern "C"

@@ -229,3 +229,25 @@ int zo_sq_loss_launch(int nblk, int T, int m, int dtype, const void* Y, const vo
 int zo_combine_central_launch(int q, const double* L, float eps, float* g,
                               hipStream_t stream);
 int zo_combine_forward_launch(int q, const double* L, float eps, float* g, hipStream_t stream);
+
+// Embedding and its gradient (zo_embed.hip).  ws_needed: only the workspace size is computed.
+int zo_embedding_launch(long long rows, int vocab, int d, int dtype, const int* ids, const void* E, float scale, void* H,
+                        int* bad_flag, hipStream_t stream);
+int zo_embedding_backward_launch(long long rows, int vocab, int d, int dtype, const int* ids, const void* dH, float scale,
+                                 int out_dtype, void* dE, int accumulate, int* bad_flag, void* ws, hipStream_t stream,
+                                 size_t* ws_needed);
+// Log-probabilities of labels over the vocabulary (zo_logprob.hip).
+int zo_token_logprob_launch(int nblk, int T, int vocab, int dtype, const void* X, long long ld, const int* labels, float scale,
+                            float* logp, float* lse, int* bad_flag, hipStream_t stream);
+int zo_token_logprob_backward_launch(int nblk, int T, int vocab, int dtype, const void* X, long long ld, const int* labels,
+                                     float scale, const float* lse, const float* g, void* dX, long long ldo, int* bad_flag,
+                                     hipStream_t stream);
+// Losses over sequences (zo_seqloss.hip).
+int zo_preference_loss_launch(int nblk, int rows, int pairs, int kind, int average, double beta, double margin, double smoothing,
+                              double weight, const float* logp, const float* ref_logp, const int* labels, const int* seq_start,
+                              double* loss, float* rewards, float* dlogp, int* bad_flag, void* ws, hipStream_t stream,
+                              size_t* ws_needed);
+int zo_policy_loss_launch(int nblk, int rows, int nseq, int aggregate, int per_token, double clip_low, double clip_high,
+                          double kl_coef, double weight, const float* logp, const float* old_logp, const float* ref_logp,
+                          const float* advantage, const int* labels, const int* seq_start, double* loss, double* stats,
+                          float* dlogp, int* bad_flag, void* ws, hipStream_t stream, size_t* ws_needed);
