@@ -784,12 +784,16 @@ int zo_embedding_backward(long long rows, int vocab, int d, int dtype,
  * with a NaN or +infinity, or with nothing but -infinity, gives NaN in logp.
  * Sums are taken in fp32 relative to the row's largest logit, logarithm and
  * differences in fp64, one rounding at the end: logp does not lose where lse
- * is large.
- * Limits: nblk >= 1, T >= 0, nblk T < 2^31; 1 <= vocab <= ld < 2^31; scale finite
- * and > 0; tensors aligned to their elements. */
+ * is large.  The workspace holds partial sums where few long rows are split over
+ * workgroups (0 bytes where none is); calls that may run at the same time need
+ * one each.
+ * Limits: nblk >= 1, T >= 0, nblk T < 2^31; 1 <= vocab <= ld < 2^31; scale in
+ * [2^-60, 2^60]; tensors aligned to their elements. */
+size_t zo_token_logprob_workspace(int nblk, int T, int vocab, int dtype);
 int zo_token_logprob(int nblk, int T, int vocab, int dtype, const void* X,
                      long long ld, const int* labels, float scale, float* logp,
-                     float* lse, int* bad_flag, void* stream);
+                     float* lse, int* bad_flag, void* workspace,
+                     size_t ws_bytes, void* stream);
 
 /* The logits' gradient from the gradient g of logp (device fp32 [nblk T]):
  *   dX[i][j] = round(scale g[i] ([j = y] - exp(scale X[i][j] - lse[i])))

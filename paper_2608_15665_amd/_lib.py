@@ -44,7 +44,7 @@ ABI_SYMBOLS = (
     "zo_subspace_refresh_noalloc",
     "zo_kv_append", "zo_paged_attention_workspace", "zo_paged_attention",
     "zo_embedding", "zo_embedding_backward_workspace", "zo_embedding_backward",
-    "zo_token_logprob", "zo_token_logprob_backward",
+    "zo_token_logprob_workspace", "zo_token_logprob", "zo_token_logprob_backward",
     "zo_preference_loss_workspace", "zo_preference_loss", "zo_policy_loss_workspace", "zo_policy_loss",
 )
 ZO_NOALLOC_SCRATCH_BYTES = 64 << 20
@@ -240,7 +240,9 @@ def lib() -> ctypes.CDLL:
             L.zo_embedding_backward.argtypes = [c_ll, c_int, c_int, c_int, c_vp, c_vp, c_f, c_int, c_vp, c_int, c_vp, c_vp,
                                                 c_sz, c_vp]
             L.zo_token_logprob.restype = c_int
-            L.zo_token_logprob.argtypes = [c_int] * 4 + [c_vp, c_ll, c_vp, c_f, c_vp, c_vp, c_vp, c_vp]
+            L.zo_token_logprob.argtypes = [c_int] * 4 + [c_vp, c_ll, c_vp, c_f, c_vp, c_vp, c_vp, c_vp, c_sz, c_vp]
+            L.zo_token_logprob_workspace.restype = c_sz
+            L.zo_token_logprob_workspace.argtypes = [c_int] * 4
             L.zo_token_logprob_backward.restype = c_int
             L.zo_token_logprob_backward.argtypes = [c_int] * 4 + [c_vp, c_ll, c_vp, c_f, c_vp, c_vp, c_vp, c_ll, c_vp, c_vp]
             L.zo_preference_loss_workspace.restype = c_sz
@@ -1149,6 +1151,8 @@ def _own_ws(workspace: Optional[torch.Tensor], need: int, here: int):
     launches, and a graph may be replayed beside another)."""
     if workspace is not None:
         return workspace, _kv_tensor(workspace, "workspace", torch.uint8, here), workspace.numel()
+    if need == 0:
+        return None, None, 0
     buf = torch.empty(need, dtype=torch.uint8, device=f"cuda:{here}")
     return buf, buf.data_ptr(), need
 
@@ -1220,10 +1224,11 @@ def _logits(X: torch.Tensor, labels: torch.Tensor, vocab: Optional[int], here: i
 
 def token_logprob(logits: torch.Tensor, labels: torch.Tensor, vocab: Optional[int] = None, scale: float = 1.0,
                   logp: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
-                  bad_flag: Optional[torch.Tensor] = None):
+                  bad_flag: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
     """(logp, lse), fp32, of logits (nblk T rows; the first `vocab` columns, default all) scaled by `scale`: each row's
     log-probability of its label (labels: int32, T of them shared by the blocks; below 0: not counted, 0) and its
-    log-sum-exp.  bad_flag (one int32) is set where a label is not below vocab.  See zo_token_logprob."""
+    log-sum-exp.  bad_flag (one int32) is set where a label is not below vocab.  Without a workspace (uint8) the call
+    allocates what it needs.  See zo_token_logprob."""
     here = torch._C._cuda_getDevice()
     nblk, T, vocab, ld, lab = _logits(logits, labels, vocab, here)
     n = nblk * T
@@ -1231,9 +1236,10 @@ def token_logprob(logits: torch.Tensor, labels: torch.Tensor, vocab: Optional[in
         logp = torch.empty(n, dtype=torch.float32, device=logits.device)
     if lse is None:
         lse = torch.empty(n, dtype=torch.float32, device=logits.device)
-    _check(lib().zo_token_logprob(nblk, T, vocab, _DT[logits.dtype], logits.data_ptr(), ld, lab, scale,
-                                  _here(logp, "logp", torch.float32, here, n), _here(lse, "lse", torch.float32, here, n),
-                                  _flag(bad_flag, here), _stream_handle()))
+    L, dt = lib(), _DT[logits.dtype]
+    tensors = (_here(logp, "logp", torch.float32, here, n), _here(lse, "lse", torch.float32, here, n), _flag(bad_flag, here))
+    _keep, ws, ws_n = _own_ws(workspace, L.zo_token_logprob_workspace(nblk, T, vocab, dt), here)
+    _check(L.zo_token_logprob(nblk, T, vocab, dt, logits.data_ptr(), ld, lab, scale, *tensors, ws, ws_n, _stream_handle()))
     return logp, lse
 
 

@@ -1188,20 +1188,29 @@ static int check_logprob(const char* what, int nblk, int T, int vocab, int dtype
            "%s: nblk = %d, T = %d (need nblk >= 1, T >= 0, nblk T < 2^31)", what, nblk, T);
   ZO_CHECK(vocab >= 1 && ld >= vocab && ld < (1LL << 31), "%s: vocab = %d in rows %lld elements apart", what, vocab, ld);
   ZO_CHECK(dtype == ZO_F32 || dtype == ZO_BF16 || dtype == ZO_F16, "%s: bad dtype %d", what, dtype);
-  ZO_CHECK(isfinite(scale) && scale > 0.f, "%s: scale must be finite and > 0", what);
+  ZO_CHECK(scale >= 0x1p-60f && scale <= 0x1p60f, "%s: scale = %g outside [2^-60, 2^60]", what, scale);
   ZO_CHECK(T == 0 || (X && labels), "%s: X or labels is NULL", what);
   ZO_CHECK(aligned(X, dtype == ZO_F32 ? 4 : 2) && aligned(labels, 4) && aligned(bad_flag, 4), "%s: a tensor is not aligned", what);
   return ZO_OK;
 }
 
+size_t zo_token_logprob_workspace(int nblk, int T, int vocab, int dtype) {
+  if (check_logprob("token_logprob", nblk, T, vocab, dtype, (void*)16, vocab, (const int*)16, 1.f, nullptr) != ZO_OK || T == 0)
+    return 0;
+  size_t need = 0;
+  zo_token_logprob_launch(nblk, T, vocab, dtype, nullptr, vocab, nullptr, 1.f, nullptr, nullptr, nullptr, nullptr, nullptr, &need);
+  return need;
+}
+
 int zo_token_logprob(int nblk, int T, int vocab, int dtype, const void* X, long long ld, const int* labels, float scale,
-                     float* logp, float* lse, int* bad_flag, void* stream) {
+                     float* logp, float* lse, int* bad_flag, void* workspace, size_t ws_bytes, void* stream) {
   const char* what = "token_logprob";
-  const int st = check_logprob(what, nblk, T, vocab, dtype, X, ld, labels, scale, bad_flag);
-  if (st != ZO_OK) return st;
-  if (T == 0) return ZO_OK;
+  int st = check_logprob(what, nblk, T, vocab, dtype, X, ld, labels, scale, bad_flag);
+  if (st != ZO_OK || T == 0) return st;
   ZO_CHECK(logp && aligned(logp, 4) && aligned(lse, 4), "%s: logp is NULL, or logp or lse not 4-byte aligned", what);
-  return zo_token_logprob_launch(nblk, T, vocab, dtype, X, ld, labels, scale, logp, lse, bad_flag, (hipStream_t)stream);
+  if ((st = check_ws(what, zo_token_logprob_workspace(nblk, T, vocab, dtype), workspace, ws_bytes)) != ZO_OK) return st;
+  return zo_token_logprob_launch(nblk, T, vocab, dtype, X, ld, labels, scale, logp, lse, bad_flag, workspace,
+                                 (hipStream_t)stream, nullptr);
 }
 
 int zo_token_logprob_backward(int nblk, int T, int vocab, int dtype, const void* X, long long ld, const int* labels, float scale,

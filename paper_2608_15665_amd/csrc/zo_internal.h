@@ -238,7 +238,7 @@ int zo_embedding_backward_launch(long long rows, int vocab, int d, int dtype, co
                                  size_t* ws_needed);
 // Log-probabilities of labels over the vocabulary (zo_logprob.hip).
 int zo_token_logprob_launch(int nblk, int T, int vocab, int dtype, const void* X, long long ld, const int* labels, float scale,
-                            float* logp, float* lse, int* bad_flag, hipStream_t stream);
+                            float* logp, float* lse, int* bad_flag, void* ws, hipStream_t stream, size_t* ws_needed);
 int zo_token_logprob_backward_launch(int nblk, int T, int vocab, int dtype, const void* X, long long ld, const int* labels,
                                      float scale, const float* lse, const float* g, void* dX, long long ldo, int* bad_flag,
                                      hipStream_t stream);

@@ -21,8 +21,9 @@ def _backward(rows=4, vocab=10, d=16, dtype=1, ids=FAKE, E=FAKE, scale=1.0, odt=
     return zo.lib().zo_embedding_backward(rows, vocab, d, dtype, ids, E, scale, odt, H, acc, flag, ws, n, None)
 
 
-def _logprob(nblk=1, T=4, vocab=10, dtype=1, X=FAKE, ld=16, labels=FAKE, scale=1.0, logp=FAKE, lse=FAKE, flag=None):
-    return zo.lib().zo_token_logprob(nblk, T, vocab, dtype, X, ld, labels, scale, logp, lse, flag, None)
+def _logprob(nblk=1, T=4, vocab=10, dtype=1, X=FAKE, ld=16, labels=FAKE, scale=1.0, logp=FAKE, lse=FAKE, flag=None,
+             ws=FAKE, n=1 << 40):
+    return zo.lib().zo_token_logprob(nblk, T, vocab, dtype, X, ld, labels, scale, logp, lse, flag, ws, n, None)
 
 
 def _logprob_grad(nblk=1, T=4, vocab=10, dtype=1, X=FAKE, ld=16, labels=FAKE, scale=1.0, lse=FAKE, g=FAKE, dX=2 * FAKE, ldo=16,
@@ -82,6 +83,14 @@ def test_logits(call, kw, needle):
 def test_logits_gradient(kw, needle):
     assert _logprob_grad(**kw) == 1 and needle in _detail(), _detail()
     assert _logprob(logp=None) == 1 and "logp is NULL" in _detail()
+
+
+def test_logits_workspace():
+    assert zo.lib().zo_token_logprob_workspace(1, 4, 10, 1) == 0 and zo.lib().zo_token_logprob_workspace(1, 0, 10, 1) == 0
+    assert zo.lib().zo_token_logprob_workspace(1, 2, 200000, 1) >= 2 * 2 * 8  # few long rows are split
+    long = dict(T=2, vocab=200000, ld=200000)
+    assert _logprob(**long, n=8) == 6 and "workspace 8" in _detail()
+    assert _logprob(**long, ws=None) == 6 and _logprob(**long, ws=FAKE + 16) == 1 and "256-byte" in _detail()
 
 
 BOTH = [(dict(nblk=0), "nblk"), (dict(nblk=65536), "nblk"), (dict(rows=-1), "rows"), (dict(nblk=1 << 15, rows=1 << 16), "rows"),
