@@ -117,40 +117,51 @@ __device__ __forceinline__ float group_total(float v) {
   return v;
 }
 
-// The sum over words lo .. hi - 1 of a row, and with `edges` over its elements before and behind the words.  The next
-// words are on their way while these are added.
+// The sum over words lo .. hi - 1 of a row, and with `edges` over its elements before and behind the words.  Whole steps of
+// U NT words need no checks, so the next step's loads stay on their way while this one's are added.
 template <int DT, int NT>
 __device__ __forceinline__ Sum row_sum(const char* x, const RowWords& r, int vocab, int lo, int hi, bool edges, float c) {
   using EL = Elem<DT>;
   constexpr int U = 2;
-  const int tid = threadIdx.x & (NT - 1);
-  const u32x4* words = (const u32x4*)(x + r.head * EL::SIZE);
+  const int tid = threadIdx.x & (NT - 1), steps = (hi - lo) / (U * NT);
+  const u32x4* words = (const u32x4*)(x + r.head * EL::SIZE) + lo + tid;
+  const int rest = hi - lo - tid;  // words from this thread's first on
   Sum sum = {LEAST, 0.f};
-  auto fetch = [&](int i, u32x4* w) {
+  u32x4 last[U], w[U], next[U];
+  float edge[2] = {-__builtin_inff(), -__builtin_inff()};
+  if (edges && tid < r.head) edge[0] = EL::load(x + tid * EL::SIZE);
+  if (edges && tid < r.tail) edge[1] = EL::load(x + ((size_t)vocab - 1 - tid) * EL::SIZE);
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int k = i + u * NT;
-      w[u] = (u32x4){EL::MINUS_INF, EL::MINUS_INF, EL::MINUS_INF, EL::MINUS_INF};
-      if (k < hi) w[u] = words[k];
-    }
+  for (int u = 0; u < U; ++u)
+    if (steps * U * NT + u * NT < rest) last[u] = words[steps * U * NT + u * NT];
+  auto load = [&](int s, u32x4* to) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) to[u] = words[s * (U * NT) + u * NT];
   };
-  u32x4 w[2][U];
-  fetch(lo + tid, w[0]);
-  if (edges && tid < 16) {
-    float e[2] = {-__builtin_inff(), -__builtin_inff()};
-    if (tid < r.head) e[0] = EL::load(x + tid * EL::SIZE);
-    if (tid < r.tail) e[1] = EL::load(x + ((size_t)vocab - 1 - tid) * EL::SIZE);
-    sum.add<2>(e, c);
+  auto add = [&](const u32x4* from) {
+    float e[U * EL::N];
+#pragma unroll
+    for (int u = 0; u < U; ++u) EL::widen(from[u], e + u * EL::N);
+    sum.add<U * EL::N>(e, c);
+  };
+  if (steps > 0) {
+    load(0, w);
+#pragma unroll 2
+    for (int s = 1; s < steps; ++s) {
+      load(s, next);
+      add(w);
+#pragma unroll
+      for (int u = 0; u < U; ++u) w[u] = next[u];
+    }
+    add(w);
   }
-  for (int i = lo + tid; i < hi; i += 2 * U * NT) {
+  if (edges && tid < 16) sum.add<2>(edge, c);
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      if (h && i + U * NT >= hi) break;  // a wave without words leaves: 2048 words a step are many beside a row's
-      fetch(i + (h + 1) * U * NT, w[1 - h]);
-      float e[U * EL::N];
-#pragma unroll
-      for (int u = 0; u < U; ++u) EL::widen(w[h][u], e + u * EL::N);
-      sum.add<U * EL::N>(e, c);
+  for (int u = 0; u < U; ++u) {
+    if (steps * U * NT + u * NT < rest) {
+      float e[EL::N];
+      EL::widen(last[u], e);
+      sum.add<EL::N>(e, c);
     }
   }
   const float R = group_max<NT>(sum.R);

@@ -59,8 +59,8 @@ def test_tables(call, kw, needle):
     (_embedding, dict(rows=(1 << 30) + 1), 1, "rows"), (_backward, dict(rows=(1 << 24) + 1), 1, "rows"),
     (_embedding, dict(rows=1 << 30, d=1 << 20), 1, "too large"),
     (_backward, dict(odt=2), 1, "out_dtype"), (_backward, dict(dtype=0, odt=1), 1, "out_dtype"),
-    (_backward, dict(odt=3), 1, "out_dtype"), (_backward, dict(n=100), 6, "workspace 100"),
-    (_backward, dict(ws=None), 6, "workspace 0"), (_backward, dict(ws=FAKE + 128), 1, "256-byte"),
+    (_backward, dict(odt=3), 1, "out_dtype"), (_backward, dict(rows=4000, n=100), 6, "workspace 100"),
+    (_backward, dict(rows=4000, ws=None), 6, "workspace 0"), (_backward, dict(rows=4000, ws=FAKE + 128), 1, "256-byte"),
 ])
 def test_tables_more(call, kw, status, needle):
     assert call(**kw) == status and needle in _detail(), _detail()

@@ -70,7 +70,7 @@ def _tokens(rng, form, rows, vocab):
 
 SIZES = [(1, 1, 8), (1, 40000, 512), (31, 3, 24), (32, 40, 72), (33, 40, 520), (63, 2, 8), (64, 1000, 1024), (65, 511, 8),
          (200, 512, 136), (257, 600, 8), (700, 50000, 264), (1024, 7, 64), (2047, 513, 24), (2049, 5000, 512),
-         (5000, 262143, 8), (4097, 262144, 16), (9000, 300, 1032)]
+         (5000, 262143, 8), (4097, 262144, 16), (8192, 3000, 8), (8193, 3000, 8), (9000, 300, 1032)]
 
 
 @pytest.mark.parametrize("dt,out", [("f32", "f32"), ("bf16", "bf16"), ("bf16", "f32"), ("f16", "f16"), ("f16", "f32")])
