@@ -833,8 +833,8 @@ int zo_token_logprob_backward(int nblk, int T, int vocab, int dtype,
  *             sequence without rows that count).
  *   dlogp     device fp32 [nblk x rows], nullable: the gradient of loss[b].
  * float64 arithmetic throughout; sums in a fixed order.
- * Limits: 1 <= nblk <= 65535, 1 <= pairs <= 2^22, rows >= 0, nblk rows and
- * nblk pairs < 2^31;
+ * Limits: 1 <= nblk <= 65535, 1 <= pairs <= 2^22, 0 <= rows <= 2^29, nblk rows
+ * and nblk pairs < 2^31;
  * beta finite and > 0, margin and weight finite, 0 <= smoothing <= 0.5 (0 but for
  * ZO_PREF_SIGMOID). */
 typedef enum { ZO_PREF_SIGMOID = 0, ZO_PREF_HINGE = 1, ZO_PREF_IPO = 2 } zo_preference;

@@ -9,6 +9,7 @@ libzo.so is missing or a call fails, an exception is raised.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 import threading
 import weakref
@@ -1131,10 +1132,13 @@ def combine_forward(L: torch.Tensor, eps: float, out: Optional[torch.Tensor] = N
 # ---------------------------------------------------------------------------
 def _here(t: torch.Tensor, name: str, dtype, here: int, numel: int) -> int:
     """The address of a dense tensor of `numel` elements of the type on the current device."""
-    p = _kv_tensor(t, name, dtype, here)
-    if t.numel() != numel:
-        raise ValueError(f"{name} must hold {numel} elements (got {t.numel()})")
-    return p
+    try:
+        if t.dtype is dtype and t.numel() == numel and t.get_device() == here and t.is_contiguous():
+            return t.data_ptr()
+    except AttributeError:
+        pass
+    _kv_tensor(t, name, dtype, here)  # raises, but for the number of elements
+    raise ValueError(f"{name} must hold {numel} elements (got {t.numel()})")
 
 
 def _flag(bad_flag: Optional[torch.Tensor], here: int) -> Optional[int]:
@@ -1146,14 +1150,20 @@ def _fits(n: int, what: str) -> None:
         raise ValueError(f"{what}: {n} out of range")
 
 
-def _own_ws(workspace: Optional[torch.Tensor], need: int, here: int):
+@functools.lru_cache(maxsize=1024)
+def _ws_bytes(name: str, *sizes: int) -> int:
+    """A workspace query's answer: a function of the sizes alone."""
+    return getattr(lib(), name)(*sizes)
+
+
+def _own_ws(workspace: Optional[torch.Tensor], need: int, like: torch.Tensor, here: int):
     """(tensor to keep, address, bytes) of a call's workspace: the caller's, or one of the call's own (calls are several
     launches, and a graph may be replayed beside another)."""
     if workspace is not None:
         return workspace, _kv_tensor(workspace, "workspace", torch.uint8, here), workspace.numel()
     if need == 0:
         return None, None, 0
-    buf = torch.empty(need, dtype=torch.uint8, device=f"cuda:{here}")
+    buf = torch.empty(need, dtype=torch.uint8, device=like.device)
     return buf, buf.data_ptr(), need
 
 
@@ -1171,8 +1181,8 @@ def embedding(ids: torch.Tensor, table: torch.Tensor, scale: float = 1.0, out: O
     rows = ids.numel()
     if out is None:
         out = torch.empty((*ids.shape, d), dtype=table.dtype, device=table.device)
-    _check(lib().zo_embedding(rows, vocab, d, _DT[table.dtype], _kv_tensor(ids, "ids", torch.int32, here),
-                              _kv_tensor(table, "table", table.dtype, here), scale,
+    _check(lib().zo_embedding(rows, vocab, d, _DT[table.dtype], _here(ids, "ids", torch.int32, here, rows),
+                              _here(table, "table", table.dtype, here, vocab * d), scale,
                               _here(out, "out", table.dtype, here, rows * d), _flag(bad_flag, here), _stream_handle()))
     return out
 
@@ -1195,12 +1205,11 @@ def embedding_backward(ids: torch.Tensor, grad: torch.Tensor, vocab: int, scale:
         out = torch.empty((vocab, d), dtype=torch.float32, device=grad.device)
     if out.dtype not in _DT:
         raise TypeError(f"unsupported dtype {out.dtype}")
-    L = lib()
     ids_p, grad_p = _kv_tensor(ids, "ids", torch.int32, here), _here(grad, "grad", dt, here, rows * d)
     out_p, flag = _here(out, "out", out.dtype, here, vocab * d), _flag(bad_flag, here)
-    _keep, ws, ws_n = _own_ws(workspace, L.zo_embedding_backward_workspace(rows, vocab, d), here)
-    _check(L.zo_embedding_backward(rows, vocab, d, _DT[dt], ids_p, grad_p, scale, _DT[out.dtype], out_p, int(accumulate), flag,
-                                   ws, ws_n, _stream_handle()))
+    _keep, ws, ws_n = _own_ws(workspace, _ws_bytes("zo_embedding_backward_workspace", rows, vocab, d), grad, here)
+    _check(lib().zo_embedding_backward(rows, vocab, d, _DT[dt], ids_p, grad_p, scale, _DT[out.dtype], out_p, int(accumulate),
+                                       flag, ws, ws_n, _stream_handle()))
     return out
 
 
@@ -1236,10 +1245,10 @@ def token_logprob(logits: torch.Tensor, labels: torch.Tensor, vocab: Optional[in
         logp = torch.empty(n, dtype=torch.float32, device=logits.device)
     if lse is None:
         lse = torch.empty(n, dtype=torch.float32, device=logits.device)
-    L, dt = lib(), _DT[logits.dtype]
+    dt = _DT[logits.dtype]
     tensors = (_here(logp, "logp", torch.float32, here, n), _here(lse, "lse", torch.float32, here, n), _flag(bad_flag, here))
-    _keep, ws, ws_n = _own_ws(workspace, L.zo_token_logprob_workspace(nblk, T, vocab, dt), here)
-    _check(L.zo_token_logprob(nblk, T, vocab, dt, logits.data_ptr(), ld, lab, scale, *tensors, ws, ws_n, _stream_handle()))
+    _keep, ws, ws_n = _own_ws(workspace, _ws_bytes("zo_token_logprob_workspace", nblk, T, vocab, dt), logits, here)
+    _check(lib().zo_token_logprob(nblk, T, vocab, dt, logits.data_ptr(), ld, lab, scale, *tensors, ws, ws_n, _stream_handle()))
     return logp, lse
 
 
@@ -1264,10 +1273,16 @@ def token_logprob_backward(logits: torch.Tensor, labels: torch.Tensor, lse: torc
 
 def _blocks(logp: torch.Tensor):
     """(nblk, rows) of log-probabilities: nblk x rows, or the rows of one block."""
-    if logp.dim() not in (1, 2):
+    shape = logp.shape
+    if len(shape) == 2:
+        nblk, rows = shape
+    elif len(shape) == 1:
+        nblk, rows = 1, shape[0]
+    else:
         raise ValueError("logp must be nblk x rows, or rows")
-    _fits(max(logp.numel(), *logp.shape), "log-probabilities")
-    return (1, logp.shape[0]) if logp.dim() == 1 else logp.shape
+    if nblk >= 1 << 31 or rows >= 1 << 31:
+        _fits(max(nblk, rows), "blocks or rows of logp")
+    return nblk, rows
 
 
 def _optional(t: Optional[torch.Tensor], name: str, dtype, here: int, numel: int) -> Optional[int]:
@@ -1289,21 +1304,22 @@ def preference_loss(logp: torch.Tensor, seq_start: torch.Tensor, beta: float, re
     kind: "sigmoid", "hinge" or "ipo".  rewards (fp32, nblk x 2 pairs) and dlogp (fp32, as logp: the gradient, times
     weight as the loss) are filled where given.  Returns loss.  See zo_preference_loss."""
     here = torch._C._cuda_getDevice()
-    if kind not in PREFERENCES:
+    code = PREFERENCES.get(kind)
+    if code is None:
         raise ValueError(f"kind must be one of {sorted(PREFERENCES)} (got {kind!r})")
     nblk, rows = _blocks(logp)
-    pairs = (seq_start.numel() - 1) // 2
-    if seq_start.numel() != 2 * pairs + 1 or pairs < 1:
-        raise ValueError(f"seq_start must hold 2 pairs + 1 elements (got {seq_start.numel()})")
+    starts = seq_start.numel()
+    pairs = (starts - 1) // 2
+    if starts != 2 * pairs + 1 or pairs < 1:
+        raise ValueError(f"seq_start must hold 2 pairs + 1 elements (got {starts})")
     loss = _loss_out(loss, nblk, logp)
-    L = lib()
-    tensors = (_kv_tensor(logp, "logp", torch.float32, here), _optional(ref_logp, "ref_logp", torch.float32, here, rows),
-               _optional(labels, "labels", torch.int32, here, rows), _kv_tensor(seq_start, "seq_start", torch.int32, here),
+    tensors = (_here(logp, "logp", torch.float32, here, nblk * rows), _optional(ref_logp, "ref_logp", torch.float32, here, rows),
+               _optional(labels, "labels", torch.int32, here, rows), _here(seq_start, "seq_start", torch.int32, here, starts),
                _here(loss, "loss", torch.float64, here, nblk),
                _optional(rewards, "rewards", torch.float32, here, 2 * nblk * pairs),
                _optional(dlogp, "dlogp", torch.float32, here, nblk * rows), _flag(bad_flag, here))
-    _keep, ws, ws_n = _own_ws(workspace, L.zo_preference_loss_workspace(nblk, rows, pairs), here)
-    _check(L.zo_preference_loss(nblk, rows, pairs, PREFERENCES[kind], int(average), beta, margin, label_smoothing, weight,
+    _keep, ws, ws_n = _own_ws(workspace, _ws_bytes("zo_preference_loss_workspace", nblk, rows, pairs), logp, here)
+    _check(lib().zo_preference_loss(nblk, rows, pairs, code, int(average), beta, margin, label_smoothing, weight,
                                 *tensors, ws, ws_n, _stream_handle()))
     return loss
 
@@ -1320,21 +1336,21 @@ def policy_loss(logp: torch.Tensor, old_logp: torch.Tensor, advantage: torch.Ten
     aggregate: "token", "sequence" or "sum".  stats (float64, nblk x 2: the mean KL term, the share of clipped rows) and
     dlogp (fp32, as logp: the gradient) are filled where given.  Returns loss.  See zo_policy_loss."""
     here = torch._C._cuda_getDevice()
-    if aggregate not in AGGREGATES:
+    code = AGGREGATES.get(aggregate)
+    if code is None:
         raise ValueError(f"aggregate must be one of {sorted(AGGREGATES)} (got {aggregate!r})")
     nblk, rows = _blocks(logp)
     nseq = seq_start.numel() - 1
     if nseq < 1:
         raise ValueError(f"seq_start must hold nseq + 1 elements, nseq >= 1 (got {seq_start.numel()})")
     loss = _loss_out(loss, nblk, logp)
-    L = lib()
-    tensors = (_kv_tensor(logp, "logp", torch.float32, here), _here(old_logp, "old_logp", torch.float32, here, rows),
+    tensors = (_here(logp, "logp", torch.float32, here, nblk * rows), _here(old_logp, "old_logp", torch.float32, here, rows),
                _optional(ref_logp, "ref_logp", torch.float32, here, rows),
                _here(advantage, "advantage", torch.float32, here, rows if per_token else nseq),
-               _optional(labels, "labels", torch.int32, here, rows), _kv_tensor(seq_start, "seq_start", torch.int32, here),
+               _optional(labels, "labels", torch.int32, here, rows), _here(seq_start, "seq_start", torch.int32, here, nseq + 1),
                _here(loss, "loss", torch.float64, here, nblk), _optional(stats, "stats", torch.float64, here, 2 * nblk),
                _optional(dlogp, "dlogp", torch.float32, here, nblk * rows), _flag(bad_flag, here))
-    _keep, ws, ws_n = _own_ws(workspace, L.zo_policy_loss_workspace(nblk, rows, nseq), here)
-    _check(L.zo_policy_loss(nblk, rows, nseq, AGGREGATES[aggregate], int(per_token), clip_low, clip_high, kl_coef, weight,
+    _keep, ws, ws_n = _own_ws(workspace, _ws_bytes("zo_policy_loss_workspace", nblk, rows, nseq), logp, here)
+    _check(lib().zo_policy_loss(nblk, rows, nseq, code, int(per_token), clip_low, clip_high, kl_coef, weight,
                             *tensors, ws, ws_n, _stream_handle()))
     return loss

@@ -1231,8 +1231,8 @@ int zo_token_logprob_backward(int nblk, int T, int vocab, int dtype, const void*
 static int check_seqs(const char* what, int nblk, int rows, int nseq, int most, const char* unit) {
   ZO_CHECK(nblk >= 1 && nblk <= 65535, "%s: nblk = %d outside [1, 65535]", what, nblk);
   ZO_CHECK(nseq >= 1 && nseq <= most, "%s: %s = %d outside [1, %d]", what, unit, nseq, most);
-  ZO_CHECK(rows >= 0 && (long long)nblk * rows < (1LL << 31), "%s: rows = %d of %d blocks (need nblk rows < 2^31)", what, rows,
-           nblk);
+  ZO_CHECK(rows >= 0 && rows <= (1 << 29) && (long long)nblk * rows < (1LL << 31),
+           "%s: rows = %d of %d blocks (need rows <= 2^29, nblk rows < 2^31)", what, rows, nblk);
   ZO_CHECK((long long)nblk * nseq < (1LL << 31), "%s: %d blocks of %d %s too many", what, nblk, nseq, unit);
   return ZO_OK;
 }

@@ -1,5 +1,6 @@
 // Losses over sequences of token log-probabilities: paired preferences and the clipped policy loss, with their
-// gradients.  float64 throughout; every sum in a fixed order.
+// gradients.  float64 throughout (the losses of two query blocks are subtracted, and their difference is small), every
+// sum in a fixed order.
 #include "zo_internal.h"
 
 namespace {
@@ -17,28 +18,51 @@ __device__ __forceinline__ Span span_of(const int* start, int s, int rows, int* 
   return r;
 }
 
-// Sums over a workgroup of 256, the same in every thread.
-template <int N>
-__device__ __forceinline__ void group_sum(double* v) {
-  __shared__ double red[N][4];
+// Sums over NT threads (a wave, or the workgroup), the same in every thread.
+template <int NT, int N, typename V>
+__device__ __forceinline__ void group_sum(V* v) {
 #pragma unroll
-  for (int k = 0; k < N; ++k) {
+  for (int k = 0; k < N; ++k)
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) v[k] += __shfl_xor(v[k], off, 64);
-    if ((threadIdx.x & 63) == 0) red[k][threadIdx.x >> 6] = v[k];
-  }
-  __syncthreads();
+  if constexpr (NT > 64) {
+    __shared__ V red[N][NT / 64];
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0)
 #pragma unroll
-  for (int k = 0; k < N; ++k) v[k] = (red[k][0] + red[k][1]) + (red[k][2] + red[k][3]);
-  __syncthreads();
+      for (int k = 0; k < N; ++k) red[k][threadIdx.x >> 6] = v[k];
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      v[k] = red[k][0];
+#pragma unroll
+      for (int j = 1; j < NT / 64; ++j) v[k] += red[k][j];
+    }
+  }
 }
 
+// Rows lo .. hi - 1 dealt to NT threads, four at a time so that their loads are on their way together: f(row) loads, g(row,
+// what f gave) uses it.
+template <int NT, int U = 4, typename F, typename G>
+__device__ __forceinline__ void each_row(Span sp, F f, G g) {
+  for (int t = sp.lo + (int)(threadIdx.x & (NT - 1)); t < sp.hi; t += U * NT) {
+    decltype(f(0)) v[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) v[u] = f(min(t + u * NT, sp.hi - 1));
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (t + u * NT < sp.hi) g(t + u * NT, v[u]);
+  }
+}
+
+// ---------------------------------------------------------------- preferences
 struct PrefArgs {
   int rows, pairs, kind, average;
   double beta, margin, smoothing, weight;
   const float *logp, *ref;
   const int *labels, *start;
-  double* part;
+  double* part;  // nblk x pairs
+  double* loss;
   float *rewards, *dlogp;
   int* bad_flag;
 };
@@ -63,124 +87,291 @@ __device__ __forceinline__ double pair_loss(const PrefArgs& a, double z, double*
   return (1.0 - a.smoothing) * (l + (h < 0.0 ? -h : 0.0)) + keep;
 }
 
-// A workgroup per pair and block.
-__global__ __launch_bounds__(256) void k_preference(PrefArgs a) {
-  const int p = blockIdx.x, b = blockIdx.y;
+// The loss of pair p of block b by NT threads, its rewards and its rows' gradient.
+template <int NT>
+__device__ __forceinline__ double one_pair(const PrefArgs& a, int p, int b) {
   const float* logp = a.logp + (size_t)b * a.rows;
-  double v[4] = {0.0, 0.0, 0.0, 0.0};
+  const bool first = (threadIdx.x & (NT - 1)) == 0;
+  struct Row {
+    float p, q;
+    int y;
+  };
   Span sp[2];
 #pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    sp[k] = span_of(a.start, 2 * p + k, a.rows, threadIdx.x == 0 ? a.bad_flag : nullptr);
-    for (int t = sp[k].lo + threadIdx.x; t < sp[k].hi; t += 256) {
-      if (a.labels && a.labels[t] < 0) continue;
-      v[k] += (double)logp[t] - (a.ref ? (double)a.ref[t] : 0.0);
-      v[2 + k] += 1.0;
-    }
+  for (int k = 0; k < 2; ++k) sp[k] = span_of(a.start, 2 * p + k, a.rows, first ? a.bad_flag : nullptr);
+  // Both sequences' rows together, two of each at a time.
+  double v[2] = {0.0, 0.0};
+  long long counts[1] = {0};  // of the chosen one, and of the other above
+  const int n0 = sp[0].hi - sp[0].lo, n1 = sp[1].hi - sp[1].lo;
+  for (int i = threadIdx.x & (NT - 1); i < max(n0, n1); i += 2 * NT) {
+    Row r[2][2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const int t = min(sp[k].lo + i + u * NT, max(sp[k].hi - 1, 0));
+        r[k][u] = {logp[t], a.ref ? a.ref[t] : 0.f, a.labels ? a.labels[t] : 0};
+      }
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        if (sp[k].lo + i + u * NT >= sp[k].hi || r[k][u].y < 0) continue;
+        v[k] += (double)r[k][u].p - (double)r[k][u].q;
+        counts[0] += 1LL << (32 * k);
+      }
   }
-  group_sum<4>(v);
-  const double w0 = a.average && v[2] > 0.0 ? 1.0 / v[2] : 1.0, w1 = a.average && v[3] > 0.0 ? 1.0 / v[3] : 1.0;
+  group_sum<NT, 2>(v);
+  group_sum<NT, 1>(counts);
+  const double c0 = (double)(int)counts[0], c1 = (double)(int)(counts[0] >> 32);
+  const double w0 = a.average && c0 > 0.0 ? 1.0 / c0 : 1.0, w1 = a.average && c1 > 0.0 ? 1.0 / c1 : 1.0;
   const double r0 = v[0] * w0, r1 = v[1] * w1;
   double slope = 0.0, l = 0.0;
-  if (v[2] > 0.0 && v[3] > 0.0) l = pair_loss(a, r0 - r1 - a.margin, &slope);
-  if (threadIdx.x == 0) {
-    a.part[(size_t)b * a.pairs + p] = l;
-    if (a.rewards) {
-      a.rewards[((size_t)b * a.pairs + p) * 2] = (float)(a.beta * r0);
-      a.rewards[((size_t)b * a.pairs + p) * 2 + 1] = (float)(a.beta * r1);
+  if (c0 > 0.0 && c1 > 0.0) l = pair_loss(a, r0 - r1 - a.margin, &slope);
+  if (first && a.rewards) {
+    a.rewards[((size_t)b * a.pairs + p) * 2] = (float)(a.beta * r0);
+    a.rewards[((size_t)b * a.pairs + p) * 2 + 1] = (float)(a.beta * r1);
+  }
+  if (a.dlogp) {
+    slope *= a.weight / a.pairs;
+    float* d = a.dlogp + (size_t)b * a.rows;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const float up = (float)(k == 0 ? slope * w0 : -slope * w1);
+      each_row<NT>(sp[k], [&](int t) { return a.labels ? a.labels[t] : 0; }, [&](int t, int y) { d[t] = y >= 0 ? up : 0.f; });
     }
   }
-  if (!a.dlogp) return;
-  slope *= a.weight / a.pairs;
-#pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    const float up = (float)(k == 0 ? slope * w0 : -slope * w1);
-    for (int t = sp[k].lo + threadIdx.x; t < sp[k].hi; t += 256)
-      a.dlogp[(size_t)b * a.rows + t] = !a.labels || a.labels[t] >= 0 ? up : 0.f;
-  }
+  return l;
 }
 
-// out[b] = factor sum of part[b]: one workgroup per block.
-__global__ __launch_bounds__(256) void k_preference_total(const double* part, int n, double factor, double* out) {
+// NT threads per pair and block.
+template <int NT>
+__global__ __launch_bounds__(NT < 256 ? 256 : NT) void k_preference(PrefArgs a) {
+  const int p = NT < 256 ? blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x, b = blockIdx.y;
+  if (p >= a.pairs) return;
+  const double l = one_pair<NT>(a, p, b);
+  if ((threadIdx.x & (NT - 1)) == 0) a.part[(size_t)b * a.pairs + p] = l;
+}
+
+__global__ __launch_bounds__(256) void k_preference_total(PrefArgs a) {
   double v[1] = {0.0};
-  for (int i = threadIdx.x; i < n; i += 256) v[0] += part[(size_t)blockIdx.x * n + i];
-  group_sum<1>(v);
-  if (threadIdx.x == 0) out[blockIdx.x] = factor * v[0];
+  for (int i = threadIdx.x; i < a.pairs; i += 256) v[0] += a.part[(size_t)blockIdx.x * a.pairs + i];
+  group_sum<256, 1>(v);
+  if (threadIdx.x == 0) a.loss[blockIdx.x] = a.weight / a.pairs * v[0];
 }
 
+// All pairs of a block by one workgroup, a wave per pair: few rows need no second launch.
+__global__ __launch_bounds__(1024) void k_preference_few(PrefArgs a) {
+  __shared__ double each[16];
+  const int w = threadIdx.x >> 6;
+  double l = 0.0;
+  for (int p = w; p < a.pairs; p += 16) l += one_pair<64>(a, p, blockIdx.x);
+  if ((threadIdx.x & 63) == 0) each[w] = l;
+  __syncthreads();
+  if (threadIdx.x != 0) return;
+  double total = each[0];
+#pragma unroll
+  for (int j = 1; j < 16; ++j) total += each[j];
+  a.loss[blockIdx.x] = a.weight / a.pairs * total;
+}
+
+// ---------------------------------------------------------------- policy
 struct PolicyArgs {
-  int rows, nseq, aggregate, per_token;
+  int nblk, rows, nseq, aggregate, per_token;
   double low, high, kl, weight;
   const float *logp, *old, *ref, *adv;
   const int *labels, *start;
-  int* count;     // rows that count, per sequence
+  int ncount;
+  int* counted;   // rows that count, in ncount parts (token, with a gradient)
+  int* of_seq;    // and of each sequence
   double* part;   // nblk x nseq x 3
+  double *loss, *stats;
   float* dlogp;
   int* bad_flag;
 };
 
+struct PolicyRow {
+  float old, ref, adv;
+  int y;
+};
+__device__ __forceinline__ PolicyRow policy_row(const PolicyArgs& a, int t, int s) {
+  return {a.old[t], a.ref ? a.ref[t] : 0.f, a.adv[a.per_token ? t : s], a.labels ? a.labels[t] : 0};
+}
+
+// Adds a row that counts to (loss, k, clipped) and returns its slope.
+__device__ __forceinline__ double policy_term(const PolicyArgs& a, float logp, const PolicyRow& x, double* v) {
+  const double p = logp, A = x.adv, r = exp(p - (double)x.old);
+  const double c = r < 1.0 - a.low ? 1.0 - a.low : (r > 1.0 + a.high ? 1.0 + a.high : r);
+  const double plain = r * A, kept = c * A;
+  const bool cut = plain > kept;
+  double l = cut ? -kept : -plain, slope = cut ? 0.0 : -plain;
+  if (a.ref) {
+    const double d = (double)x.ref - p, e = exp(d), k = d < __builtin_inf() ? e - d - 1.0 : e;  // infinite at d = inf
+    l += a.kl * k;
+    slope += a.kl * (1.0 - e);
+    v[1] += k;
+  }
+  v[0] += l;
+  v[2] += cut ? 1.0 : 0.0;
+  return slope;
+}
+
+__device__ __forceinline__ double inverse(double n) { return n > 0.0 ? 1.0 / n : 0.0; }
+
+// The rows that count among all: sequences follow one another, so they are rows start[0] .. start[nseq] - 1.
 __global__ __launch_bounds__(256) void k_policy_count(PolicyArgs a) {
-  const Span sp = span_of(a.start, blockIdx.x, a.rows, threadIdx.x == 0 ? a.bad_flag : nullptr);
+  const int lo = min(max(a.start[0], 0), a.rows), hi = min(max(a.start[a.nseq], lo), a.rows);
+  const int each = (hi - lo + a.ncount - 1) / a.ncount;
+  Span sp = {min(lo + (int)blockIdx.x * each, hi), 0};
+  sp.hi = min(sp.lo + each, hi);
   double v[1] = {0.0};
-  for (int t = sp.lo + threadIdx.x; t < sp.hi; t += 256) v[0] += !a.labels || a.labels[t] >= 0 ? 1.0 : 0.0;
-  group_sum<1>(v);
-  if (threadIdx.x == 0) a.count[blockIdx.x] = (int)v[0];
+  each_row<256>(sp, [&](int t) { return a.labels ? a.labels[t] : 0; }, [&](int, int y) { v[0] += y >= 0 ? 1.0 : 0.0; });
+  group_sum<256, 1>(v);
+  if (threadIdx.x == 0) a.counted[blockIdx.x] = (int)v[0];
 }
 
-// A workgroup per sequence and block.
-__global__ __launch_bounds__(256) void k_policy(PolicyArgs a) {
-  const int s = blockIdx.x, b = blockIdx.y;
+// NT threads take a sequence, under NB blocks at once: what the blocks share is loaded once.
+template <int NT, int NB>
+__global__ __launch_bounds__(NT < 256 ? 256 : NT) void k_policy(PolicyArgs a) {
+  const int s = NT < 256 ? blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x, b0 = blockIdx.y * NB;
   double n[1] = {0.0};
-  for (int i = threadIdx.x; i < a.nseq; i += 256) n[0] += a.count[i];
-  group_sum<1>(n);
-  const double mine = a.count[s];
-  const double share = a.weight * (a.aggregate == ZO_AGG_TOKEN ? (n[0] > 0.0 ? 1.0 / n[0] : 0.0)
-                                   : a.aggregate == ZO_AGG_SEQUENCE ? (mine > 0.0 ? 1.0 / mine / a.nseq : 0.0) : 1.0);
-  const Span sp = span_of(a.start, s, a.rows, nullptr);
-  const float* logp = a.logp + (size_t)b * a.rows;
-  double v[3] = {0.0, 0.0, 0.0};
-  for (int t = sp.lo + threadIdx.x; t < sp.hi; t += 256) {
-    float up = 0.f;
-    if (!a.labels || a.labels[t] >= 0) {
-      const double p = logp[t], A = a.adv[a.per_token ? t : s];
-      const double r = exp(p - (double)a.old[t]);
-      const double c = r < 1.0 - a.low ? 1.0 - a.low : (r > 1.0 + a.high ? 1.0 + a.high : r);
-      const double plain = r * A, kept = c * A;
-      const bool cut = plain > kept;
-      double l = cut ? -kept : -plain, slope = cut ? 0.0 : -plain;
-      if (a.ref) {
-        const double d = (double)a.ref[t] - p, e = exp(d), k = d < __builtin_inf() ? e - d - 1.0 : e;  // infinite at d = inf
-        l += a.kl * k;
-        slope += a.kl * (1.0 - e);
-        v[1] += k;
-      }
-      v[0] += l;
-      v[2] += cut ? 1.0 : 0.0;
-      up = (float)(slope * share);
-    }
-    if (a.dlogp) a.dlogp[(size_t)b * a.rows + t] = up;
+  if (a.dlogp && a.aggregate == ZO_AGG_TOKEN) {
+    for (int i = threadIdx.x & (NT - 1); i < a.ncount; i += NT) n[0] += a.counted[i];
+    group_sum<NT, 1>(n);
   }
-  group_sum<3>(v);
-  if (threadIdx.x == 0) {
-    double* to = a.part + ((size_t)b * a.nseq + s) * 3;
-    to[0] = v[0] * share;
-    to[1] = n[0] > 0.0 ? v[1] / n[0] : 0.0;
-    to[2] = n[0] > 0.0 ? v[2] / n[0] : 0.0;
+  if (s >= a.nseq) return;
+  const bool first = (threadIdx.x & (NT - 1)) == 0;
+  const Span sp = span_of(a.start, s, a.rows, first && b0 == 0 ? a.bad_flag : nullptr);
+  if (a.dlogp && a.aggregate == ZO_AGG_SEQUENCE) {
+    each_row<NT>(sp, [&](int t) { return a.labels ? a.labels[t] : 0; }, [&](int, int y) { n[0] += y >= 0 ? 1.0 : 0.0; });
+    group_sum<NT, 1>(n);
+    n[0] *= a.nseq;
+  }
+  const double share = a.weight * (a.aggregate == ZO_AGG_SUM ? 1.0 : inverse(n[0]));  // of the gradient
+  double v[3 * NB + 1];
+#pragma unroll
+  for (int k = 0; k < 3 * NB + 1; ++k) v[k] = 0.0;
+  struct Row {
+    PolicyRow x;
+    float p[NB];
+  };
+  each_row<NT, 1>(
+      sp,
+      [&](int t) {
+        Row r = {policy_row(a, t, s), {}};
+#pragma unroll
+        for (int k = 0; k < NB; ++k) r.p[k] = a.logp[(size_t)min(b0 + k, a.nblk - 1) * a.rows + t];
+        return r;
+      },
+      [&](int t, const Row& r) {
+        const bool on = r.x.y >= 0;
+        v[3 * NB] += on ? 1.0 : 0.0;
+#pragma unroll
+        for (int k = 0; k < NB; ++k) {
+          double slope = 0.0;
+          if (on) slope = policy_term(a, r.p[k], r.x, v + 3 * k);
+          if (a.dlogp && b0 + k < a.nblk) a.dlogp[(size_t)(b0 + k) * a.rows + t] = on ? (float)(slope * share) : 0.f;
+        }
+      });
+  group_sum<NT, 3 * NB + 1>(v);
+  if (!first) return;
+  if (b0 == 0) a.of_seq[s] = (int)v[3 * NB];
+  const double mine = a.aggregate == ZO_AGG_SEQUENCE ? inverse(v[3 * NB] * a.nseq) : 1.0;
+#pragma unroll
+  for (int k = 0; k < NB; ++k) {
+    if (b0 + k >= a.nblk) break;
+    double* to = a.part + ((size_t)(b0 + k) * a.nseq + s) * 3;
+    to[0] = v[3 * k] * mine;
+    to[1] = v[3 * k + 1];
+    to[2] = v[3 * k + 2];
   }
 }
 
-__global__ __launch_bounds__(256) void k_policy_total(const double* part, int n, double* loss, double* stats) {
-  double v[3] = {0.0, 0.0, 0.0};
-  for (int i = threadIdx.x; i < n; i += 256)
+__global__ __launch_bounds__(256) void k_policy_total(PolicyArgs a) {
+  double v[4] = {0.0, 0.0, 0.0, 0.0};
+  const double* part = a.part + (size_t)blockIdx.x * a.nseq * 3;
+  for (int i = threadIdx.x; i < a.nseq; i += 256) {
 #pragma unroll
-    for (int k = 0; k < 3; ++k) v[k] += part[((size_t)blockIdx.x * n + i) * 3 + k];
-  group_sum<3>(v);
-  if (threadIdx.x == 0) {
-    loss[blockIdx.x] = v[0];
-    if (stats) {
-      stats[2 * blockIdx.x] = v[1];
-      stats[2 * blockIdx.x + 1] = v[2];
+    for (int k = 0; k < 3; ++k) v[k] += part[(size_t)i * 3 + k];
+    v[3] += a.of_seq[i];
+  }
+  group_sum<256, 4>(v);
+  if (threadIdx.x != 0) return;
+  a.loss[blockIdx.x] = a.weight * (a.aggregate == ZO_AGG_TOKEN ? v[0] * inverse(v[3]) : v[0]);
+  if (a.stats) {
+    a.stats[2 * blockIdx.x] = v[1] * inverse(v[3]);
+    a.stats[2 * blockIdx.x + 1] = v[2] * inverse(v[3]);
+  }
+}
+
+// All rows of a block by one workgroup, a thread per row: few rows need no other launch.  A row's sequence is the last one
+// that starts at it or before.
+constexpr int FEW_SEQS = 1024, FEW_ROWS = 8;  // sequences, and rows of a thread
+__global__ __launch_bounds__(1024) void k_policy_few(PolicyArgs a) {
+  __shared__ int start[FEW_SEQS + 1], count[FEW_SEQS];
+  const int b = blockIdx.x, t0 = threadIdx.x;
+  for (int s = t0; s <= a.nseq; s += 1024) {
+    const int v = a.start[s];
+    start[s] = min(max(v, 0), a.rows);
+    if (a.bad_flag && (v < 0 || v > a.rows || (s > 0 && a.start[s - 1] > v))) *a.bad_flag = 1;
+    if (s < a.nseq) count[s] = 0;
+  }
+  __syncthreads();
+  const int lo = start[0], hi = max(start[a.nseq], lo);
+  const bool by_seq = a.aggregate == ZO_AGG_SEQUENCE;
+  struct Row {
+    PolicyRow x;
+    float p;
+    int s;
+  } r[FEW_ROWS];
+#pragma unroll
+  for (int k = 0; k < FEW_ROWS; ++k) {
+    if (lo + k * 1024 >= hi) break;
+    const int t = min(lo + k * 1024 + t0, hi - 1);
+    r[k].s = 0;
+    if (by_seq || !a.per_token) {  // start[s] <= t < start[s + 1]
+      int first = 0, behind = a.nseq;
+      while (behind - first > 1) {
+        const int m = (first + behind) >> 1;
+        if (start[m] <= t) first = m;
+        else behind = m;
+      }
+      r[k].s = first;
     }
+    r[k].x = policy_row(a, t, r[k].s);
+    r[k].p = a.logp[(size_t)b * a.rows + t];
+    if (lo + k * 1024 + t0 >= hi) r[k].x.y = -1;
+    if (by_seq && r[k].x.y >= 0) atomicAdd(&count[r[k].s], 1);  // whole numbers: in any order
+  }
+  int n[1] = {0};
+#pragma unroll
+  for (int k = 0; k < FEW_ROWS; ++k)
+    if (lo + k * 1024 < hi) n[0] += r[k].x.y >= 0;
+  group_sum<1024, 1>(n);  // and the counts above are whole
+  const double N = n[0];
+  double v[3] = {0.0, 0.0, 0.0};
+#pragma unroll
+  for (int k = 0; k < FEW_ROWS; ++k) {
+    if (lo + k * 1024 >= hi) break;
+    double up = 0.0;
+    if (r[k].x.y >= 0) {
+      double one[3] = {0.0, 0.0, 0.0};
+      const double slope = policy_term(a, r[k].p, r[k].x, one);
+      const double share = a.aggregate == ZO_AGG_SUM ? 1.0 : inverse(by_seq ? (double)count[r[k].s] * a.nseq : N);
+      v[0] += by_seq ? one[0] * share : one[0];
+      v[1] += one[1];
+      v[2] += one[2];
+      up = slope * share * a.weight;
+    }
+    const int t = lo + k * 1024 + t0;
+    if (a.dlogp && t < hi) a.dlogp[(size_t)b * a.rows + t] = (float)up;
+  }
+  group_sum<1024, 3>(v);
+  if (t0 != 0) return;
+  a.loss[b] = a.weight * (a.aggregate == ZO_AGG_TOKEN ? v[0] * inverse(N) : v[0]);
+  if (a.stats) {
+    a.stats[2 * b] = v[1] * inverse(N);
+    a.stats[2 * b + 1] = v[2] * inverse(N);
   }
 }
 
@@ -190,18 +381,24 @@ int zo_preference_loss_launch(int nblk, int rows, int pairs, int kind, int avera
                               double weight, const float* logp, const float* ref_logp, const int* labels, const int* seq_start,
                               double* loss, float* rewards, float* dlogp, int* bad_flag, void* ws, hipStream_t stream,
                               size_t* ws_needed) {
-  WsCarver w(ws);
-  double* part = (double*)w.take((size_t)nblk * pairs * sizeof(double));
+  const bool few = rows <= 2048 && pairs <= 64;
   if (ws_needed) {
-    *ws_needed = w.off;
+    *ws_needed = few ? 0 : zo_align256((size_t)nblk * pairs * sizeof(double));
     return ZO_OK;
   }
-  const PrefArgs a = {rows, pairs, kind, average, beta, margin, smoothing, weight, logp, ref_logp, labels, seq_start, part,
-                      rewards, dlogp, bad_flag};
-  hipLaunchKernelGGL(k_preference, dim3(pairs, nblk), dim3(256), 0, stream, a);
+  const PrefArgs a = {rows, pairs, kind, average, beta, margin, smoothing, weight, logp, ref_logp, labels, seq_start, (double*)ws,
+                      loss, rewards, dlogp, bad_flag};
+  if (few) {
+    hipLaunchKernelGGL(k_preference_few, dim3(nblk), dim3(1024), 0, stream, a);
+    return zo_hip_status(hipGetLastError(), "k_preference_few");
+  }
+  const int mean = rows / (2 * pairs);
+  if (mean <= 64) hipLaunchKernelGGL(k_preference<64>, dim3((pairs + 3) / 4, nblk), dim3(256), 0, stream, a);
+  else if (mean <= 4096) hipLaunchKernelGGL(k_preference<256>, dim3(pairs, nblk), dim3(256), 0, stream, a);
+  else hipLaunchKernelGGL(k_preference<1024>, dim3(pairs, nblk), dim3(1024), 0, stream, a);
   const int st = zo_hip_status(hipGetLastError(), "k_preference");
   if (st != ZO_OK) return st;
-  hipLaunchKernelGGL(k_preference_total, dim3(nblk), dim3(256), 0, stream, part, pairs, weight / pairs, loss);
+  hipLaunchKernelGGL(k_preference_total, dim3(nblk), dim3(256), 0, stream, a);
   return zo_hip_status(hipGetLastError(), "k_preference_total");
 }
 
@@ -209,20 +406,37 @@ int zo_policy_loss_launch(int nblk, int rows, int nseq, int aggregate, int per_t
                           double kl_coef, double weight, const float* logp, const float* old_logp, const float* ref_logp,
                           const float* advantage, const int* labels, const int* seq_start, double* loss, double* stats,
                           float* dlogp, int* bad_flag, void* ws, hipStream_t stream, size_t* ws_needed) {
+  const bool few = rows <= 1024 * FEW_ROWS && nseq <= FEW_SEQS;
+  const int ncount = rows < 256 * 4096 ? (rows + 4095) / 4096 + (rows == 0) : 256;
   WsCarver w(ws);
-  int* count = (int*)w.take((size_t)nseq * sizeof(int));
+  int* counted = (int*)w.take((size_t)ncount * sizeof(int));
+  int* of_seq = (int*)w.take((size_t)nseq * sizeof(int));
   double* part = (double*)w.take((size_t)nblk * nseq * 3 * sizeof(double));
   if (ws_needed) {
-    *ws_needed = w.off;
+    *ws_needed = few ? 0 : w.off;
     return ZO_OK;
   }
-  const PolicyArgs a = {rows, nseq, aggregate, per_token, clip_low, clip_high, kl_coef, weight, logp, old_logp, ref_logp,
-                        advantage, labels, seq_start, count, part, dlogp, bad_flag};
-  hipLaunchKernelGGL(k_policy_count, dim3(nseq), dim3(256), 0, stream, a);
-  int st = zo_hip_status(hipGetLastError(), "k_policy_count");
+  const PolicyArgs a = {nblk, rows, nseq, aggregate, per_token, clip_low, clip_high, kl_coef, weight, logp, old_logp, ref_logp,
+                        advantage, labels, seq_start, ncount, counted, of_seq, part, loss, stats, dlogp, bad_flag};
+  if (few) {
+    hipLaunchKernelGGL(k_policy_few, dim3(nblk), dim3(1024), 0, stream, a);
+    return zo_hip_status(hipGetLastError(), "k_policy_few");
+  }
+  int st = ZO_OK;
+  if (dlogp && aggregate == ZO_AGG_TOKEN) {
+    hipLaunchKernelGGL(k_policy_count, dim3(ncount), dim3(256), 0, stream, a);
+    if ((st = zo_hip_status(hipGetLastError(), "k_policy_count")) != ZO_OK) return st;
+  }
+  const int mean = rows / nseq, nb = nblk >= 2 && mean <= 4096 ? 2 : 1;
+  auto go = [&](auto wave, auto small, auto large) {
+    const unsigned y = (nblk + nb - 1) / nb;
+    if (mean <= 128) hipLaunchKernelGGL(wave, dim3((nseq + 3) / 4, y), dim3(256), 0, stream, a);
+    else if (mean <= 4096) hipLaunchKernelGGL(small, dim3(nseq, y), dim3(256), 0, stream, a);
+    else hipLaunchKernelGGL(large, dim3(nseq, y), dim3(1024), 0, stream, a);
+    return zo_hip_status(hipGetLastError(), "k_policy");
+  };
+  st = nb == 2 ? go(k_policy<64, 2>, k_policy<256, 2>, k_policy<1024, 1>) : go(k_policy<64, 1>, k_policy<256, 1>, k_policy<1024, 1>);
   if (st != ZO_OK) return st;
-  hipLaunchKernelGGL(k_policy, dim3(nseq, nblk), dim3(256), 0, stream, a);
-  if ((st = zo_hip_status(hipGetLastError(), "k_policy")) != ZO_OK) return st;
-  hipLaunchKernelGGL(k_policy_total, dim3(nblk), dim3(256), 0, stream, part, nseq, loss, stats);
+  hipLaunchKernelGGL(k_policy_total, dim3(nblk), dim3(256), 0, stream, a);
   return zo_hip_status(hipGetLastError(), "k_policy_total");
 }

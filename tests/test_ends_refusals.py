@@ -94,10 +94,11 @@ def test_logits_workspace():
 
 
 BOTH = [(dict(nblk=0), "nblk"), (dict(nblk=65536), "nblk"), (dict(rows=-1), "rows"), (dict(nblk=1 << 15, rows=1 << 16), "rows"),
+        (dict(rows=(1 << 29) + 1), "rows"),
         (dict(logp=None), "NULL"), (dict(start=None), "NULL"), (dict(loss=None), "NULL"), (dict(loss=FAKE + 4), "aligned"),
         (dict(logp=FAKE + 2), "aligned"), (dict(ref=FAKE + 1), "aligned"), (dict(labels=FAKE + 2), "aligned"),
         (dict(start=FAKE + 1), "aligned"), (dict(dlogp=FAKE + 2), "aligned"), (dict(flag=FAKE + 2), "aligned"),
-        (dict(weight=NAN), "weight"), (dict(ws=FAKE + 8), "256-byte")]
+        (dict(weight=NAN), "weight")]
 
 
 @pytest.mark.parametrize("call", [_preference, _policy])
@@ -112,15 +113,15 @@ def test_sequences(call, kw, needle):
     (_preference, dict(beta=INF), 1, "beta"), (_preference, dict(margin=NAN), 1, "margin"),
     (_preference, dict(smoothing=0.6), 1, "smoothing"), (_preference, dict(smoothing=-0.1), 1, "smoothing"),
     (_preference, dict(smoothing=0.1, kind=1), 1, "smoothing"), (_preference, dict(smoothing=NAN), 1, "smoothing"),
-    (_preference, dict(rewards=FAKE + 2), 1, "rewards"), (_preference, dict(n=8), 6, "workspace 8"),
-    (_preference, dict(ws=None), 6, "workspace 0"),
+    (_preference, dict(rewards=FAKE + 2), 1, "rewards"), (_preference, dict(rows=3000, n=8), 6, "workspace 8"),
+    (_preference, dict(rows=3000, ws=None), 6, "workspace 0"), (_preference, dict(rows=3000, ws=FAKE + 8), 1, "256-byte"),
     (_policy, dict(nseq=0), 1, "nseq"), (_policy, dict(nseq=(1 << 23) + 1), 1, "nseq"),
     (_policy, dict(nblk=1000, nseq=1 << 22), 1, "nseq"), (_policy, dict(agg=3), 1, "aggregate"),
     (_policy, dict(low=-0.1), 1, "clip_low"), (_policy, dict(low=1.5), 1, "clip_low"), (_policy, dict(low=NAN), 1, "clip_low"),
     (_policy, dict(high=-1.0), 1, "clip_high"), (_policy, dict(high=INF), 1, "clip_high"), (_policy, dict(kl=-1.0), 1, "kl_coef"),
     (_policy, dict(kl=0.1), 1, "without ref_logp"), (_policy, dict(old=None), 1, "old_logp"), (_policy, dict(adv=None), 1, "advantage"),
-    (_policy, dict(adv=FAKE + 2), 1, "aligned"), (_policy, dict(stats=FAKE + 4), 1, "aligned"), (_policy, dict(n=8), 6, "workspace 8"),
-    (_policy, dict(ws=None), 6, "workspace 0"),
+    (_policy, dict(adv=FAKE + 2), 1, "aligned"), (_policy, dict(stats=FAKE + 4), 1, "aligned"), (_policy, dict(rows=9000, n=8), 6, "workspace 8"),
+    (_policy, dict(rows=9000, ws=None), 6, "workspace 0"), (_policy, dict(rows=9000, ws=FAKE + 8), 1, "256-byte"),
 ])
 def test_losses(call, kw, status, needle):
     assert call(**kw) == status and needle in _detail(), _detail()
@@ -147,6 +148,9 @@ def cpu(monkeypatch):
             return lambda *a: 256 if name.endswith("_workspace") else pytest.fail(name)
 
     monkeypatch.setattr(_lib, "lib", lambda: Library())
+    _lib._ws_bytes.cache_clear()
+    yield
+    _lib._ws_bytes.cache_clear()
 
 
 I, F = (lambda *s: torch.zeros(*s, dtype=torch.int32)), torch.zeros

@@ -23,6 +23,8 @@ LENGTHS = {
     "odd": [63, 64, 65, 255, 256, 257],
     "many": [int(n) for n in np.random.default_rng(0).integers(0, 40, 600)],
     "long": [20000, 9, 1025, 4096],
+    "thousand": [3] * 1024 + [5] * 200,
+    "short": [int(n) for n in np.random.default_rng(3).integers(0, 90, 256)],
     "pairs": [int(n) for n in np.random.default_rng(1).integers(100, 600, 40)],
 }
 
