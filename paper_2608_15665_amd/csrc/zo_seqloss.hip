@@ -18,13 +18,45 @@ __device__ __forceinline__ Span span_of(const int* start, int s, int rows, int* 
   return r;
 }
 
-// Sums over NT threads (a wave, or the workgroup), the same in every thread.
-template <int NT, int N, typename V>
+// A wave's sum in every lane: rows of 16 lanes by shifts, then rows onto the next ones, all in the vector unit (a shuffle goes
+// through LDS, whose pipe the sums of short sequences would fill).
+template <int CTRL, int ROWS, typename V>
+__device__ __forceinline__ V plus_moved(V v) {
+  if constexpr (sizeof(V) == 4) {
+    return v + __builtin_bit_cast(V, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, ROWS, 0xf, false));
+  } else {
+    typedef int i32x2 __attribute__((ext_vector_type(2)));
+    i32x2 w = __builtin_bit_cast(i32x2, v);
+    w.x = __builtin_amdgcn_update_dpp(0, w.x, CTRL, ROWS, 0xf, false);
+    w.y = __builtin_amdgcn_update_dpp(0, w.y, CTRL, ROWS, 0xf, false);
+    return v + __builtin_bit_cast(V, w);
+  }
+}
+template <typename V>
+__device__ __forceinline__ V wave_sum(V v) {
+  v = plus_moved<0x111, 0xf>(v);  // from 1, 2, 4 and 8 lanes before, within 16
+  v = plus_moved<0x112, 0xf>(v);
+  v = plus_moved<0x114, 0xf>(v);
+  v = plus_moved<0x118, 0xf>(v);
+  v = plus_moved<0x142, 0xa>(v);  // lane 15 to the second 16, 47 to the fourth
+  v = plus_moved<0x143, 0xc>(v);  // lane 31 to the last 32
+  if constexpr (sizeof(V) == 4) {
+    return __builtin_bit_cast(V, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 63));
+  } else {
+    typedef int i32x2 __attribute__((ext_vector_type(2)));
+    i32x2 w = __builtin_bit_cast(i32x2, v);
+    w.x = __builtin_amdgcn_readlane(w.x, 63);
+    w.y = __builtin_amdgcn_readlane(w.y, 63);
+    return __builtin_bit_cast(V, w);
+  }
+}
+
+// Sums over NT threads (a wave, or the workgroup), the same in every thread.  Of the N values the last M are a wave's sums
+// already.
+template <int NT, int N, int M = 0, typename V>
 __device__ __forceinline__ void group_sum(V* v) {
 #pragma unroll
-  for (int k = 0; k < N; ++k)
-#pragma unroll
-    for (int off = 32; off > 0; off >>= 1) v[k] += __shfl_xor(v[k], off, 64);
+  for (int k = 0; k < N - M; ++k) v[k] = wave_sum(v[k]);
   if constexpr (NT > 64) {
     __shared__ V red[N][NT / 64];
     __syncthreads();
@@ -41,19 +73,20 @@ __device__ __forceinline__ void group_sum(V* v) {
   }
 }
 
-// Rows lo .. hi - 1 dealt to NT threads, four at a time so that their loads are on their way together: f(row) loads, g(row,
-// what f gave) uses it.
+// Rows lo .. hi - 1 dealt to NT threads, U at a time so that their loads are on their way together: f(row) loads, g(row,
+// whether it is one of them, what f gave) uses it.  All lanes of a wave stay in the loop, so a ballot in g counts the wave's.
 template <int NT, int U = 4, typename F, typename G>
 __device__ __forceinline__ void each_row(Span sp, F f, G g) {
-  for (int t = sp.lo + (int)(threadIdx.x & (NT - 1)); t < sp.hi; t += U * NT) {
+  const int lane = threadIdx.x & 63, hi = __builtin_amdgcn_readfirstlane(sp.hi);
+  for (int t0 = __builtin_amdgcn_readfirstlane(sp.lo + (int)(threadIdx.x & (NT - 64))); t0 < hi; t0 += U * NT) {
     decltype(f(0)) v[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) v[u] = f(min(t + u * NT, sp.hi - 1));
+    for (int u = 0; u < U; ++u) v[u] = f(min(t0 + lane + u * NT, hi - 1));
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (t + u * NT < sp.hi) g(t + u * NT, v[u]);
+    for (int u = 0; u < U; ++u) g(t0 + lane + u * NT, t0 + lane + u * NT < hi, v[u]);
   }
 }
+__device__ __forceinline__ int lanes(bool on) { return __popcll(__ballot(on)); }
 
 // ---------------------------------------------------------------- preferences
 struct PrefArgs {
@@ -138,7 +171,10 @@ __device__ __forceinline__ double one_pair(const PrefArgs& a, int p, int b) {
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
       const float up = (float)(k == 0 ? slope * w0 : -slope * w1);
-      each_row<NT>(sp[k], [&](int t) { return a.labels ? a.labels[t] : 0; }, [&](int t, int y) { d[t] = y >= 0 ? up : 0.f; });
+      each_row<NT>(sp[k], [&](int t) { return a.labels ? a.labels[t] : 0; },
+                   [&](int t, bool in, int y) {
+                     if (in) d[t] = y >= 0 ? up : 0.f;
+                   });
     }
   }
   return l;
@@ -198,8 +234,8 @@ __device__ __forceinline__ PolicyRow policy_row(const PolicyArgs& a, int t, int 
   return {a.old[t], a.ref ? a.ref[t] : 0.f, a.adv[a.per_token ? t : s], a.labels ? a.labels[t] : 0};
 }
 
-// Adds a row that counts to (loss, k, clipped) and returns its slope.
-__device__ __forceinline__ double policy_term(const PolicyArgs& a, float logp, const PolicyRow& x, double* v) {
+// Adds a row that counts to (loss, k), says whether it is clipped and returns its slope.
+__device__ __forceinline__ double policy_term(const PolicyArgs& a, float logp, const PolicyRow& x, double* v, bool* clipped) {
   const double p = logp, A = x.adv, r = exp(p - (double)x.old);
   const double c = r < 1.0 - a.low ? 1.0 - a.low : (r > 1.0 + a.high ? 1.0 + a.high : r);
   const double plain = r * A, kept = c * A;
@@ -212,7 +248,7 @@ __device__ __forceinline__ double policy_term(const PolicyArgs& a, float logp, c
     v[1] += k;
   }
   v[0] += l;
-  v[2] += cut ? 1.0 : 0.0;
+  *clipped = cut;
   return slope;
 }
 
@@ -224,13 +260,15 @@ __global__ __launch_bounds__(256) void k_policy_count(PolicyArgs a) {
   const int each = (hi - lo + a.ncount - 1) / a.ncount;
   Span sp = {min(lo + (int)blockIdx.x * each, hi), 0};
   sp.hi = min(sp.lo + each, hi);
-  double v[1] = {0.0};
-  each_row<256>(sp, [&](int t) { return a.labels ? a.labels[t] : 0; }, [&](int, int y) { v[0] += y >= 0 ? 1.0 : 0.0; });
-  group_sum<256, 1>(v);
-  if (threadIdx.x == 0) a.counted[blockIdx.x] = (int)v[0];
+  int n[1] = {0};
+  each_row<256>(sp, [&](int t) { return a.labels ? a.labels[t] : 0; }, [&](int, bool in, int y) { n[0] += lanes(in && y >= 0); });
+  group_sum<256, 1, 1>(n);
+  if (threadIdx.x == 0) a.counted[blockIdx.x] = n[0];
 }
 
-// NT threads take a sequence, under NB blocks at once: what the blocks share is loaded once.
+// NT threads take a sequence, under NB blocks at once: what the blocks share is loaded once.  Float64 bounds it beside its
+// start: two exponentials of some 30 instructions a row and block; 512 sequences of up to 1024 rows under 16 blocks 21 us (with
+// one block a workgroup 24, four 25), twice the rows 13 more.
 template <int NT, int NB>
 __global__ __launch_bounds__(NT < 256 ? 256 : NT) void k_policy(PolicyArgs a) {
   const int s = NT < 256 ? blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x, b0 = blockIdx.y * NB;
@@ -243,14 +281,16 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void k_policy(PolicyArgs a) {
   const bool first = (threadIdx.x & (NT - 1)) == 0;
   const Span sp = span_of(a.start, s, a.rows, first && b0 == 0 ? a.bad_flag : nullptr);
   if (a.dlogp && a.aggregate == ZO_AGG_SEQUENCE) {
-    each_row<NT>(sp, [&](int t) { return a.labels ? a.labels[t] : 0; }, [&](int, int y) { n[0] += y >= 0 ? 1.0 : 0.0; });
-    group_sum<NT, 1>(n);
-    n[0] *= a.nseq;
+    int c[1] = {0};
+    each_row<NT>(sp, [&](int t) { return a.labels ? a.labels[t] : 0; }, [&](int, bool in, int y) { c[0] += lanes(in && y >= 0); });
+    group_sum<NT, 1, 1>(c);
+    n[0] = (double)c[0] * a.nseq;
   }
   const double share = a.weight * (a.aggregate == ZO_AGG_SUM ? 1.0 : inverse(n[0]));  // of the gradient
-  double v[3 * NB + 1];
+  double v[3 * NB + 1];  // (loss, k) of each block; how many are clipped in each; how many count
 #pragma unroll
-  for (int k = 0; k < 3 * NB + 1; ++k) v[k] = 0.0;
+  for (int k = 0; k < 2 * NB; ++k) v[k] = 0.0;
+  int clipped[NB] = {}, count = 0;
   struct Row {
     PolicyRow x;
     float p[NB];
@@ -263,17 +303,24 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void k_policy(PolicyArgs a) {
         for (int k = 0; k < NB; ++k) r.p[k] = a.logp[(size_t)min(b0 + k, a.nblk - 1) * a.rows + t];
         return r;
       },
-      [&](int t, const Row& r) {
-        const bool on = r.x.y >= 0;
-        v[3 * NB] += on ? 1.0 : 0.0;
+      [&](int t, bool in, const Row& r) {
+        const bool on = in && r.x.y >= 0;
+        bool cut[NB] = {};
+        count += lanes(on);
+        double slope[NB] = {};
+        if (on)
+#pragma unroll
+          for (int k = 0; k < NB; ++k) slope[k] = policy_term(a, r.p[k], r.x, v + 2 * k, cut + k);
 #pragma unroll
         for (int k = 0; k < NB; ++k) {
-          double slope = 0.0;
-          if (on) slope = policy_term(a, r.p[k], r.x, v + 3 * k);
-          if (a.dlogp && b0 + k < a.nblk) a.dlogp[(size_t)(b0 + k) * a.rows + t] = on ? (float)(slope * share) : 0.f;
+          clipped[k] += lanes(cut[k]);
+          if (a.dlogp && in && b0 + k < a.nblk) a.dlogp[(size_t)(b0 + k) * a.rows + t] = on ? (float)(slope[k] * share) : 0.f;
         }
       });
-  group_sum<NT, 3 * NB + 1>(v);
+#pragma unroll
+  for (int k = 0; k < NB; ++k) v[2 * NB + k] = clipped[k];
+  v[3 * NB] = count;
+  group_sum<NT, 3 * NB + 1, NB + 1>(v);
   if (!first) return;
   if (b0 == 0) a.of_seq[s] = (int)v[3 * NB];
   const double mine = a.aggregate == ZO_AGG_SEQUENCE ? inverse(v[3 * NB] * a.nseq) : 1.0;
@@ -281,9 +328,9 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void k_policy(PolicyArgs a) {
   for (int k = 0; k < NB; ++k) {
     if (b0 + k >= a.nblk) break;
     double* to = a.part + ((size_t)(b0 + k) * a.nseq + s) * 3;
-    to[0] = v[3 * k] * mine;
-    to[1] = v[3 * k + 1];
-    to[2] = v[3 * k + 2];
+    to[0] = v[2 * k] * mine;
+    to[1] = v[2 * k + 1];
+    to[2] = v[2 * NB + k];
   }
 }
 
@@ -306,7 +353,7 @@ __global__ __launch_bounds__(256) void k_policy_total(PolicyArgs a) {
 
 // All rows of a block by one workgroup, a thread per row: few rows need no other launch.  A row's sequence is the last one
 // that starts at it or before.
-constexpr int FEW_SEQS = 1024, FEW_ROWS = 8;  // sequences, and rows of a thread
+constexpr int FEW_SEQS = 256, FEW_ROWS = 2;  // sequences, and rows of a thread
 __global__ __launch_bounds__(1024) void k_policy_few(PolicyArgs a) {
   __shared__ int start[FEW_SEQS + 1], count[FEW_SEQS];
   const int b = blockIdx.x, t0 = threadIdx.x;
@@ -343,30 +390,32 @@ __global__ __launch_bounds__(1024) void k_policy_few(PolicyArgs a) {
     if (lo + k * 1024 + t0 >= hi) r[k].x.y = -1;
     if (by_seq && r[k].x.y >= 0) atomicAdd(&count[r[k].s], 1);  // whole numbers: in any order
   }
-  int n[1] = {0};
+  int n[1] = {0}, clipped = 0;
 #pragma unroll
   for (int k = 0; k < FEW_ROWS; ++k)
-    if (lo + k * 1024 < hi) n[0] += r[k].x.y >= 0;
-  group_sum<1024, 1>(n);  // and the counts above are whole
+    if (lo + k * 1024 < hi) n[0] += lanes(r[k].x.y >= 0);
+  group_sum<1024, 1, 1>(n);  // and the counts above are whole
   const double N = n[0];
   double v[3] = {0.0, 0.0, 0.0};
 #pragma unroll
   for (int k = 0; k < FEW_ROWS; ++k) {
     if (lo + k * 1024 >= hi) break;
     double up = 0.0;
+    bool cut = false;
     if (r[k].x.y >= 0) {
-      double one[3] = {0.0, 0.0, 0.0};
-      const double slope = policy_term(a, r[k].p, r[k].x, one);
+      double one[2] = {0.0, 0.0};
+      const double slope = policy_term(a, r[k].p, r[k].x, one, &cut);
       const double share = a.aggregate == ZO_AGG_SUM ? 1.0 : inverse(by_seq ? (double)count[r[k].s] * a.nseq : N);
       v[0] += by_seq ? one[0] * share : one[0];
       v[1] += one[1];
-      v[2] += one[2];
       up = slope * share * a.weight;
     }
+    clipped += lanes(cut);
     const int t = lo + k * 1024 + t0;
     if (a.dlogp && t < hi) a.dlogp[(size_t)b * a.rows + t] = (float)up;
   }
-  group_sum<1024, 3>(v);
+  v[2] = clipped;
+  group_sum<1024, 3, 1>(v);
   if (t0 != 0) return;
   a.loss[b] = a.weight * (a.aggregate == ZO_AGG_TOKEN ? v[0] * inverse(N) : v[0]);
   if (a.stats) {
@@ -381,7 +430,9 @@ int zo_preference_loss_launch(int nblk, int rows, int pairs, int kind, int avera
                               double weight, const float* logp, const float* ref_logp, const int* labels, const int* seq_start,
                               double* loss, float* rewards, float* dlogp, int* bad_flag, void* ws, hipStream_t stream,
                               size_t* ws_needed) {
-  const bool few = rows <= 2048 && pairs <= 64;
+  // us of the kernels (each launch costs the host 3 more): 2 pairs of 200 rows 5.8 in one launch and 7.2 in two, 2 of 1000 9.6
+  // and 7.5, 64 of 30 20.8 and 7.2.
+  const bool few = rows <= 1024 && pairs <= 16;
   if (ws_needed) {
     *ws_needed = few ? 0 : zo_align256((size_t)nblk * pairs * sizeof(double));
     return ZO_OK;
@@ -392,9 +443,11 @@ int zo_preference_loss_launch(int nblk, int rows, int pairs, int kind, int avera
     hipLaunchKernelGGL(k_preference_few, dim3(nblk), dim3(1024), 0, stream, a);
     return zo_hip_status(hipGetLastError(), "k_preference_few");
   }
-  const int mean = rows / (2 * pairs);
-  if (mean <= 64) hipLaunchKernelGGL(k_preference<64>, dim3((pairs + 3) / 4, nblk), dim3(256), 0, stream, a);
-  else if (mean <= 4096) hipLaunchKernelGGL(k_preference<256>, dim3(pairs, nblk), dim3(256), 0, stream, a);
+  // us with a wave, 256 and 1024 threads a pair: 8192 pairs of 2 x 250 rows 19.5, 36.6, -; 2048 of them 9.9, 13.6, -; 512 of 2 x
+  // 500 12.1, 8.8, -; 128 of 2 x 1000 18.3, 8.7, 10.4; 16 of 2 x 3000 -, 15.4, 11.4.
+  const long long mean = rows / (2 * pairs), groups = (long long)nblk * pairs;
+  if (mean <= 64 || groups >= 8 * mean) hipLaunchKernelGGL(k_preference<64>, dim3((pairs + 3) / 4, nblk), dim3(256), 0, stream, a);
+  else if (mean <= 1500) hipLaunchKernelGGL(k_preference<256>, dim3(pairs, nblk), dim3(256), 0, stream, a);
   else hipLaunchKernelGGL(k_preference<1024>, dim3(pairs, nblk), dim3(1024), 0, stream, a);
   const int st = zo_hip_status(hipGetLastError(), "k_preference");
   if (st != ZO_OK) return st;
@@ -406,6 +459,8 @@ int zo_policy_loss_launch(int nblk, int rows, int nseq, int aggregate, int per_t
                           double kl_coef, double weight, const float* logp, const float* old_logp, const float* ref_logp,
                           const float* advantage, const int* labels, const int* seq_start, double* loss, double* stats,
                           float* dlogp, int* bad_flag, void* ws, hipStream_t stream, size_t* ws_needed) {
+  // us of the kernels: 16 sequences of 100 rows 6.8 in one launch and 6.9 in two (each costs the host 3 more), of 500 (8 rows a
+  // thread) 18.0 and 7.0.
   const bool few = rows <= 1024 * FEW_ROWS && nseq <= FEW_SEQS;
   const int ncount = rows < 256 * 4096 ? (rows + 4095) / 4096 + (rows == 0) : 256;
   WsCarver w(ws);
@@ -427,15 +482,19 @@ int zo_policy_loss_launch(int nblk, int rows, int nseq, int aggregate, int per_t
     hipLaunchKernelGGL(k_policy_count, dim3(ncount), dim3(256), 0, stream, a);
     if ((st = zo_hip_status(hipGetLastError(), "k_policy_count")) != ZO_OK) return st;
   }
-  const int mean = rows / nseq, nb = nblk >= 2 && mean <= 4096 ? 2 : 1;
-  auto go = [&](auto wave, auto small, auto large) {
-    const unsigned y = (nblk + nb - 1) / nb;
-    if (mean <= 128) hipLaunchKernelGGL(wave, dim3((nseq + 3) / 4, y), dim3(256), 0, stream, a);
-    else if (mean <= 4096) hipLaunchKernelGGL(small, dim3(nseq, y), dim3(256), 0, stream, a);
-    else hipLaunchKernelGGL(large, dim3(nseq, y), dim3(1024), 0, stream, a);
-    return zo_hip_status(hipGetLastError(), "k_policy");
-  };
-  st = nb == 2 ? go(k_policy<64, 2>, k_policy<256, 2>, k_policy<1024, 1>) : go(k_policy<64, 1>, k_policy<256, 1>, k_policy<1024, 1>);
+  // us with a wave, 256 and 1024 threads a sequence (and two blocks, but with 1024): 4096 sequences of 200 rows 16.6, 19.6, -; 1024
+  // of 200 9.3, 8.8, -; of 600 14.3, 10.4, 18.1; 1024 of 500 under 16 blocks 36.7, 43.1, -; 256 of 4000 -, 22.9, 12.7; 256 of
+  // 600 under 16 blocks 20.3, 17.7, 55.3; 16 of 2000 -, 10.4, 8.6.
+  const long long mean = rows / nseq;
+  const int nb = nblk >= 2 ? 2 : 1, y = (nblk + nb - 1) / nb;
+  auto go = [&](auto k, dim3 grid, int threads) { hipLaunchKernelGGL(k, grid, dim3(threads), 0, stream, a); };
+  if (mean <= 128 || (mean <= 512 && (long long)nseq * y >= 16 * mean))
+    nb == 2 ? go(k_policy<64, 2>, dim3((nseq + 3) / 4, y), 256) : go(k_policy<64, 1>, dim3((nseq + 3) / 4, y), 256);
+  else if (mean <= 1000 || (long long)nseq * nblk > 2048)
+    nb == 2 ? go(k_policy<256, 2>, dim3(nseq, y), 256) : go(k_policy<256, 1>, dim3(nseq, y), 256);
+  else
+    go(k_policy<1024, 1>, dim3(nseq, nblk), 1024);
+  st = zo_hip_status(hipGetLastError(), "k_policy");
   if (st != ZO_OK) return st;
   hipLaunchKernelGGL(k_policy_total, dim3(nblk), dim3(256), 0, stream, a);
   return zo_hip_status(hipGetLastError(), "k_policy_total");
