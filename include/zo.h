@@ -787,8 +787,8 @@ int zo_embedding_backward(long long rows, int vocab, int d, int dtype,
  * is large.  The workspace holds partial sums where few long rows are split over
  * workgroups (0 bytes where none is); calls that may run at the same time need
  * one each.
- * Limits: nblk >= 1, T >= 0, nblk T < 2^31; 1 <= vocab <= ld < 2^31; scale in
- * [2^-60, 2^60]; tensors aligned to their elements. */
+ * Limits: nblk >= 1, T >= 0, nblk T < 2^31; 1 <= vocab <= 2^30, vocab <= ld <
+ * 2^31; scale in [2^-60, 2^60]; tensors aligned to their elements. */
 size_t zo_token_logprob_workspace(int nblk, int T, int vocab, int dtype);
 int zo_token_logprob(int nblk, int T, int vocab, int dtype, const void* X,
                      long long ld, const int* labels, float scale, float* logp,

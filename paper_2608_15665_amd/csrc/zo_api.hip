@@ -1186,7 +1186,8 @@ static int check_logprob(const char* what, int nblk, int T, int vocab, int dtype
                          float scale, const int* bad_flag) {
   ZO_CHECK(nblk >= 1 && T >= 0 && (long long)nblk * T < (1LL << 31),
            "%s: nblk = %d, T = %d (need nblk >= 1, T >= 0, nblk T < 2^31)", what, nblk, T);
-  ZO_CHECK(vocab >= 1 && ld >= vocab && ld < (1LL << 31), "%s: vocab = %d in rows %lld elements apart", what, vocab, ld);
+  ZO_CHECK(vocab >= 1 && vocab <= (1 << 30), "%s: vocab = %d outside [1, 2^30]", what, vocab);
+  ZO_CHECK(ld >= vocab && ld < (1LL << 31), "%s: vocab = %d in rows %lld elements apart", what, vocab, ld);
   ZO_CHECK(dtype == ZO_F32 || dtype == ZO_BF16 || dtype == ZO_F16, "%s: bad dtype %d", what, dtype);
   ZO_CHECK(scale >= 0x1p-60f && scale <= 0x1p60f, "%s: scale = %g outside [2^-60, 2^60]", what, scale);
   ZO_CHECK(T == 0 || (X && labels), "%s: X or labels is NULL", what);

@@ -360,8 +360,7 @@ __global__ __launch_bounds__(256) void k_embed_few(const int* __restrict__ ids, 
 }
 
 // A wave sums 512 columns of CHUNK sorted positions, eight rows on their way at a time (four, and four of the gradient, where
-// it is added to).  HBM bounds it: 131071 rows of 1024 fp32 into 151936 take 181 us, 4.5 TB/s.  16 positions a wave serve up
-// to 4096 tokens better (4096 rows of 4096 bf16 36 us, with 32 positions 38), 32 more of them (65536 rows 233, with 16 245).  Tokens that lie whole in them
+// it is added to).  HBM bounds it: 131071 rows of 1024 fp32 into 151936 take 181 us, 4.5 TB/s.  Tokens that lie whole in them
 // are written; the sums of one that came in from the positions before, or goes on behind, are kept: part[2 chunk] and
 // part[2 chunk + 1].
 template <int DT, int OT, bool ADD, int CHUNK>
@@ -409,30 +408,51 @@ __global__ __launch_bounds__(256) void k_embed_sum(const int* __restrict__ key, 
 }
 
 // Joins the sums of each token that lies in more than one chunk, at the chunk where it begins, which keeps its first sum in
-// part[2 chunk + 1].  A wave looks at a chunk; a token of up to JOIN_ALONE further chunks it adds by itself, in order; longer
-// ones the workgroup takes one after another, each wave a run of chunks, then the waves' sums in order.
+// part[2 chunk + 1].  A wave looks at a chunk, and 256 columns; a token of up to JOIN_ALONE further chunks it adds by itself, in
+// order; longer ones the workgroup takes one after another, each wave a run of chunks, then the waves' sums in order.
 template <int OT, bool ADD, int CHUNK>
 __global__ __launch_bounds__(64 * JOIN_WAVES) void k_embed_join(const int* __restrict__ key, int n, int vocab, int d, float scale,
                                                                 void* dE, const float* __restrict__ part, int nchunk, int nslab) {
-  __shared__ float sums[JOIN_WAVES][512];
+  constexpr int U = 16;
+  __shared__ f32x4 sums[JOIN_WAVES][64];
   __shared__ int reach[JOIN_WAVES];
   const long long block = block_of(), group = block / nslab;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int c = (int)(block - group * nslab) * 512 + lane * 8, first = (int)(group * JOIN_WAVES);
-  auto add_chunks = [&](int j0, int j1, float* s) {
-    for (int j = j0; j < j1; j += 8) {
-      Row8<ZO_F32> v[8];
-#pragma unroll
-      for (int u = 0; u < 8; ++u) v[u].load(row_at<ZO_F32>(part, 2LL * (j + u), d, j + u < j1), c);
-#pragma unroll
-      for (int u = 0; u < 8; ++u) v[u].add_to(s);  // a chunk that is left out adds zeros
-    }
+  const int c = (int)(block - group * nslab) * 256 + lane * 4, first = (int)(group * JOIN_WAVES);
+  auto load = [&](long long row, bool on) {
+    return __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(row_at<ZO_F32>(part, row, d, on), c * 4, 0, 0));
   };
-  auto put = [&](int chunk, const float* s) {
-    const __amdgpu_buffer_rsrc_t at = row_at<OT>(dE, __builtin_amdgcn_readfirstlane(key[chunk * CHUNK + CHUNK - 1]), d);
-    Row8<OT> held;
-    if (ADD) held.load(at, c);
-    put_row<OT, ADD>(at, c, s, scale, held);
+  auto add_chunks = [&](int j0, int j1, f32x4 s) {
+    for (int j = j0; j < j1; j += U) {
+      f32x4 v[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) v[u] = load(2LL * (j + u), j + u < j1);
+#pragma unroll
+      for (int u = 0; u < U; ++u) s += v[u];  // a chunk that is left out adds zeros
+    }
+    return s;
+  };
+  auto put = [&](int chunk, f32x4 s) {
+    if (c >= d) return;
+    const size_t at = (size_t)key[chunk * CHUNK + CHUNK - 1] * d + c;
+    f32x4 v = {0.f, 0.f, 0.f, 0.f};
+    if constexpr (OT == ZO_F32) {
+      f32x4* to = (f32x4*)((float*)dE + at);
+      if (ADD) v = *to;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = ADD ? fmaf(scale, s[e], v[e]) : scale * s[e];
+      *to = v;
+    } else {
+      u32x2* to = (u32x2*)((uint16_t*)dE + at);
+      if (ADD) {
+        const u32x2 h = *to;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = unpk<OT == ZO_F16>(h[e >> 1], e & 1);
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = ADD ? fmaf(scale, s[e], v[e]) : scale * s[e];
+      *to = (u32x2){cvt_pk<OT == ZO_F16>(v[0], v[1]), cvt_pk<OT == ZO_F16>(v[2], v[3])};
+    }
   };
   const int chunk = first + w, i0 = chunk * CHUNK, last = i0 + CHUNK - 1;
   int more = 0;  // chunks behind its own that this wave's token reaches
@@ -454,34 +474,18 @@ __global__ __launch_bounds__(64 * JOIN_WAVES) void k_embed_join(const int* __res
     }
   }
   if (lane == 0) reach[w] = more > JOIN_ALONE ? more : 0;
-  if (more > 0 && more <= JOIN_ALONE) {
-    float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    Row8<ZO_F32> v;
-    v.load(row_at<ZO_F32>(part, 2LL * chunk + 1, d), c);
-    v.add_to(s);
-    add_chunks(chunk + 1, chunk + 1 + more, s);
-    put(chunk, s);
-  }
+  if (more > 0 && more <= JOIN_ALONE) put(chunk, add_chunks(chunk + 1, chunk + 1 + more, load(2LL * chunk + 1, true)));
   __syncthreads();
   for (int q = 0; q < JOIN_WAVES; ++q) {
     const int many = reach[q];
     if (!many) continue;
     const int each = (many + JOIN_WAVES - 1) / JOIN_WAVES, j0 = first + q + 1 + w * each, j1 = min(j0 + each, first + q + 1 + many);
-    float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    if (w == 0) {
-      Row8<ZO_F32> v;
-      v.load(row_at<ZO_F32>(part, 2LL * (first + q) + 1, d), c);
-      v.add_to(s);
-    }
-    add_chunks(j0, j1, s);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) sums[w][e * 64 + lane] = s[e];
+    f32x4 s = add_chunks(j0, j1, load(2LL * (first + q) + 1, w == 0));
+    sums[w][lane] = s;
     __syncthreads();
     if (w == 0) {
 #pragma unroll
-      for (int j = 1; j < JOIN_WAVES; ++j)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) s[e] += sums[j][e * 64 + lane];
+      for (int j = 1; j < JOIN_WAVES; ++j) s += sums[j][lane];
       put(first + q, s);
     }
     __syncthreads();
@@ -538,7 +542,10 @@ int zo_embedding_backward_launch(long long rows, int vocab, int d, int dtype, co
                                  int out_dtype, void* dE, int accumulate, int* bad_flag, void* ws, hipStream_t stream,
                                  size_t* ws_needed) {
   const SortPlan p = sort_plan(rows, vocab);
-  const int n = p.n, chunk = n <= 4096 ? 16 : 32, nchunk = (n + chunk - 1) / chunk, nslab = (d + 511) / 512;
+  const int n = p.n, nslab = (d + 511) / 512;
+  // Positions of a wave, us with 16, 32 and 64: 4096 rows of 4096 bf16 added to fp32 36, 38, 49; 20000 121, 119, 128; 65536, dense,
+  // 245, 240, 230; 100000 rows of 128 50, 46, 51.
+  const int chunk = n <= 4096 ? 16 : n < 65536 || nslab == 1 ? 32 : 64, nchunk = (n + chunk - 1) / chunk;
   const bool few = n <= FEW, one = n <= SORT_ONE && vocab < (1 << 18);
   WsCarver w(ws);
   int* hist = one ? nullptr : (int*)w.take((size_t)p.ntiles * DIGITS * sizeof(int));
@@ -601,15 +608,17 @@ int zo_embedding_backward_launch(long long rows, int vocab, int d, int dtype, co
     constexpr int DT = decltype(dt)::value, OT = decltype(ot)::value;
     constexpr bool ADD = decltype(add)::value;
     const dim3 sums = grid_of(((long long)nchunk * nslab + 3) / 4);
-    const dim3 joins = grid_of((long long)((nchunk + JOIN_WAVES - 1) / JOIN_WAVES) * nslab);
+    const int jslab = (d + 255) / 256;
+    const dim3 joins = grid_of((long long)((nchunk + JOIN_WAVES - 1) / JOIN_WAVES) * jslab);
     auto go = [&](auto sum, auto join) {
       hipLaunchKernelGGL(sum, sums, dim3(256), 0, stream, skey, srow, n, vocab, d, dH, scale, dE, part, nchunk, nslab);
       const int st = zo_hip_status(hipGetLastError(), "k_embed_sum");
       if (st != ZO_OK) return st;
-      hipLaunchKernelGGL(join, joins, dim3(64 * JOIN_WAVES), 0, stream, skey, n, vocab, d, scale, dE, part, nchunk, nslab);
+      hipLaunchKernelGGL(join, joins, dim3(64 * JOIN_WAVES), 0, stream, skey, n, vocab, d, scale, dE, part, nchunk, jslab);
       return zo_hip_status(hipGetLastError(), "k_embed_join");
     };
-    return chunk == 16 ? go(k_embed_sum<DT, OT, ADD, 16>, k_embed_join<OT, ADD, 16>)
-                       : go(k_embed_sum<DT, OT, ADD, 32>, k_embed_join<OT, ADD, 32>);
+    return chunk == 16   ? go(k_embed_sum<DT, OT, ADD, 16>, k_embed_join<OT, ADD, 16>)
+           : chunk == 32 ? go(k_embed_sum<DT, OT, ADD, 32>, k_embed_join<OT, ADD, 32>)
+                         : go(k_embed_sum<DT, OT, ADD, 64>, k_embed_join<OT, ADD, 64>);
   });
 }

@@ -69,7 +69,7 @@ def test_tables_more(call, kw, status, needle):
 @pytest.mark.parametrize("call", [_logprob, _logprob_grad])
 @pytest.mark.parametrize("kw,needle", [
     (dict(nblk=0), "nblk"), (dict(T=-1), "T = -1"), (dict(nblk=1 << 16, T=1 << 15), "nblk T"), (dict(vocab=0), "vocab"),
-    (dict(vocab=17), "16 elements apart"), (dict(ld=1 << 31), "apart"), (dict(dtype=3), "dtype 3"), (dict(scale=0.0), "scale"),
+    (dict(vocab=17), "16 elements apart"), (dict(vocab=(1 << 30) + 1, ld=(1 << 30) + 1), "vocab"), (dict(ld=1 << 31), "apart"), (dict(dtype=3), "dtype 3"), (dict(scale=0.0), "scale"),
     (dict(scale=-1.0), "scale"), (dict(scale=NAN), "scale"), (dict(X=None), "NULL"), (dict(labels=None), "NULL"),
     (dict(X=FAKE + 1), "aligned"), (dict(dtype=0, X=FAKE + 2), "aligned"), (dict(labels=FAKE + 2), "aligned"),
     (dict(lse=FAKE + 2), "4-byte"), (dict(flag=FAKE + 3), "aligned")])

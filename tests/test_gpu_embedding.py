@@ -129,16 +129,18 @@ def test_gradient_keeps_what_is_not_finite_to_its_token():
     assert bad.sum().item() == 2 and dE[3, 1].isnan() and dE[60 % 7, 2] == float("inf")
 
 
-def test_many_rows_of_few_tokens_are_sorted():
-    """131072 rows: 64 sorting tiles, runs over thousands of chunks; whole numbers, so that every sum is exact."""
+@pytest.mark.parametrize("n,vocab,d", [(131071, 70000, 8), (70001, 5000, 520), (66000, 3, 520)])
+def test_many_rows_of_few_tokens_are_sorted(n, vocab, d):
+    """Tens of sorting tiles, runs over thousands of chunks; whole numbers, so that every sum is exact."""
     rng = np.random.default_rng(8)
-    n, vocab, d = 131071, 70000, 8
     ids = _tokens(rng, "text", n, vocab)
-    ids[::3] = 69999
+    ids[::3] = vocab - 1
     g = rng.integers(-8, 9, (n, d))
     dE = zo.embedding_backward(i32(ids), torch.tensor(g, dtype=torch.float32, device="cuda"), vocab)
     want = np.zeros((vocab + 1, d))
-    np.add.at(want, ids, g)  # padding, -1, falls into the last row
+    order = np.argsort(ids, kind="stable")
+    first = np.flatnonzero(np.diff(ids[order], prepend=-2))
+    want[ids[order][first]] = np.add.reduceat(g[order].astype(np.float64), first)  # padding, -1, is the last row
     np.testing.assert_array_equal(host(dE), want[:vocab])
 
 
