@@ -191,7 +191,8 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void k_preference(PrefArgs a) 
 
 __global__ __launch_bounds__(256) void k_preference_total(PrefArgs a) {
   double v[1] = {0.0};
-  for (int i = threadIdx.x; i < a.pairs; i += 256) v[0] += a.part[(size_t)blockIdx.x * a.pairs + i];
+  each_row<256>(Span{0, a.pairs}, [&](int i) { return a.part[(size_t)blockIdx.x * a.pairs + i]; },
+                [&](int, bool in, double l) { v[0] += in ? l : 0.0; });
   group_sum<256, 1>(v);
   if (threadIdx.x == 0) a.loss[blockIdx.x] = a.weight / a.pairs * v[0];
 }
@@ -337,11 +338,18 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void k_policy(PolicyArgs a) {
 __global__ __launch_bounds__(256) void k_policy_total(PolicyArgs a) {
   double v[4] = {0.0, 0.0, 0.0, 0.0};
   const double* part = a.part + (size_t)blockIdx.x * a.nseq * 3;
-  for (int i = threadIdx.x; i < a.nseq; i += 256) {
+  struct Row {
+    double x[3];
+    int n;
+  };
+  each_row<256>(
+      Span{0, a.nseq}, [&](int i) { return Row{{part[(size_t)i * 3], part[(size_t)i * 3 + 1], part[(size_t)i * 3 + 2]}, a.of_seq[i]}; },
+      [&](int, bool in, const Row& r) {
+        if (!in) return;
 #pragma unroll
-    for (int k = 0; k < 3; ++k) v[k] += part[(size_t)i * 3 + k];
-    v[3] += a.of_seq[i];
-  }
+        for (int k = 0; k < 3; ++k) v[k] += r.x[k];
+        v[3] += r.n;
+      });
   group_sum<256, 4>(v);
   if (threadIdx.x != 0) return;
   a.loss[blockIdx.x] = a.weight * (a.aggregate == ZO_AGG_TOKEN ? v[0] * inverse(v[3]) : v[0]);
