@@ -340,9 +340,9 @@ int zo_token_logprob_launch(int nblk, int T, int vocab, int dtype, const void* X
   const unsigned rows = (unsigned)nblk * (unsigned)T;
   const long long bytes = (long long)vocab * (dtype == ZO_F32 ? 4 : 2);
   RowArgs a = {(const char*)X, ld, labels, scale, logp, lse, bad_flag, T, vocab, rows, 1, (float2*)ws};
-  // Few long rows are split: a workgroup's exponentials alone take 7 us for 151936 logits.  us, whole and split: 5 rows of
-  // 151936 bf16 12.2 and 7.1, 61 rows 13.3 and 10.4, 120 rows 13.7 and 12.7; one row of 50272 7.1 and 6.8.
-  if (rows < 128 && bytes > 65536) a.parts = (int)min(min(64LL, (bytes + 16383) / 16384), 512LL / rows);
+  // Few long rows are split: a workgroup's exponentials alone take 8 us for 151936 logits.  us of the kernels, whole and split, bf16:
+  // 5 rows of 151936 10.7 and 7.3, 61 rows 11.5 and 9.7, 120 rows 11.7 and 11.6; one row of 50272 6.3 and 6.9, 60 rows 6.8 and 7.8.
+  if (rows <= 64 && bytes >= 262144) a.parts = (int)min(min(64LL, (bytes + 16383) / 16384), 512LL / rows);
   if (ws_needed) {
     *ws_needed = a.parts > 1 ? zo_align256((size_t)rows * a.parts * sizeof(float2)) : 0;
     return ZO_OK;
@@ -361,9 +361,9 @@ int zo_token_logprob_launch(int nblk, int T, int vocab, int dtype, const void* X
       hipLaunchKernelGGL(join, dim3(rows), dim3(64), 0, stream, a);
       return zo_hip_status(hipGetLastError(), "k_token_logprob_join");
     }
-    // us with a wave, 256 and 1024 threads a row: 32000 rows of 6000 bf16 52, 61, -; of 12000 98, 90, -; 64000 rows of 1500
-    // fp32 50, 74, -; but 240 rows of 7000 fp16 6.5, 5.2, -.  16000 rows of 24000 bf16 -, 93, 127; of 40000 -, 153, 171; 12000
-    // rows of 65000 -, 187, 178; 5600 counted rows of 151851 -, 305, 293.
+    // us with a wave, 256 and 1024 threads a row: 64000 rows of 1500 fp32 51, 83, 284; 32000 of 6000 bf16 52, 59, 159; of 12000
+    // 97, 96, 193; 2400 of 6000 9.0, 8.6, 15.1; 16000 of 40000 159, 152, 166; 12000 of 50272 154, 143, 144; of 65000 198, 186, 183;
+    // of 25000 fp32 148, 142, 136; 5600 of 151851 bf16 290, 299, 279.
     return bytes <= 12288 && rows >= 4096 ? go(wave, 256, 4) : bytes <= 98304 ? go(small, 256, 1) : go(large, 1024, 1);
   };
   auto kernels = [&](auto dt) {

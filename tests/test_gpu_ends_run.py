@@ -162,7 +162,7 @@ class Calls:
         self.table = torch.empty(vocab, d, dtype=dt, device="cuda")
         self.grad = torch.empty(n, d, dtype=dt, device="cuda")
         self.rows = 3 if few else 150
-        self.V = 70001 if few else 5003
+        self.V = 140001 if few else 5003
         self.x = torch.empty(2 * self.rows, self.V, dtype=dt, device="cuda")
         self.labels = torch.empty(self.rows, dtype=torch.int32, device="cuda")
         self.dl = torch.empty(2 * self.rows, device="cuda")

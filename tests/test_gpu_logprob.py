@@ -51,7 +51,7 @@ def _case(seed, dt, rows, vocab, ld, off=0, nblk=1, ignored=0.25):
 
 SHAPES = [(1, 1, 1, 0), (1, 7, 7, 0), (3, 8, 8, 0), (5, 9, 16, 0), (2, 63, 64, 3), (9, 255, 255, 0), (4, 1000, 1000, 0),
           (3, 1023, 1031, 1), (2, 4097, 4100, 5), (7, 5003, 5003, 0), (2, 32000, 32000, 0), (3, 50257, 50304, 0),
-          (2, 50257, 50257, 7), (1, 151851, 152064, 0), (300, 130, 131, 0)]
+          (2, 50257, 50257, 7), (1, 151851, 152064, 0), (64, 140000, 140000, 0), (65, 140000, 140000, 0), (300, 130, 131, 0), (4200, 515, 515, 0)]
 
 
 @pytest.mark.parametrize("dt", ["f32", "bf16", "f16"])
@@ -115,7 +115,7 @@ def test_blocks_share_labels(nblk, rows):
 
 
 @pytest.mark.parametrize("dt", ["f32", "bf16", "f16"])
-@pytest.mark.parametrize("vocab", [9, 1000, 40001])
+@pytest.mark.parametrize("vocab", [9, 1000, 40001, 140001])
 def test_masked_tokens(dt, vocab):
     """-infinity and the type's lowest value in place of masked logits: all but one, the first half, the label's own; a row
     of the lowest value alone is uniform, one of -infinity alone is NaN."""
@@ -147,7 +147,7 @@ def test_masked_tokens(dt, vocab):
 
 
 @pytest.mark.parametrize("dt", ["f32", "bf16", "f16"])
-@pytest.mark.parametrize("vocab,at", [(9, 3), (5000, 0), (5000, 4999), (40001, 20000)])
+@pytest.mark.parametrize("vocab,at", [(9, 3), (5000, 0), (5000, 4999), (40001, 20000), (140001, 140000)])
 def test_what_is_not_finite_stays_in_its_row(dt, vocab, at):
     X, x, labels, _ = _case(6, dt, 5, vocab, vocab, ignored=0.0)
     labels[4] = -1
