@@ -38,7 +38,8 @@
  *     ZO_ERR_UNSUPPORTED / ZO_ERR_WORKSPACE, launches nothing, and
  *     zo_last_error_detail() (thread-local) says what was wrong.  A failed
  *     launch returns ZO_ERR_HIP.
- *   - Results are deterministic: no atomics take part in any reduction.
+ *   - Results are deterministic: no atomics take part in any reduction (some
+ *     calls count whole numbers with them, in whatever order).
  */
 #ifndef ZO_H
 #define ZO_H
