@@ -161,3 +161,16 @@ def test_tables_past_4_gib():
     zo.embedding_backward(i32(ids), torch.ones(5, d, dtype=torch.bfloat16, device="cuda"), vocab, out=E, accumulate=True)
     for v in set(ids):
         assert (E[v] == 1 + ids.count(v)).all()
+
+
+def test_a_result_of_more_workgroups_than_a_row_of_the_grid():
+    """2^31 words and some: 2^22 workgroups and more."""
+    n, d = (1 << 22) + 77, 4096
+    if torch.cuda.mem_get_info()[0] < 48 << 30:
+        pytest.skip("needs 48 GB")
+    E = torch.randn(1000, d, device="cuda").bfloat16()
+    ids = torch.randint(-1, 1000, (n,), device="cuda").int()
+    H = zo.embedding(ids, E)
+    for a in [*range(0, n, 1 << 20), n - 1000]:
+        i = ids[a:a + 5000].long()
+        assert (H[a:a + 5000] == torch.where((i < 0)[:, None], 0.0, E[i.clamp(min=0)].float()).bfloat16()).all()

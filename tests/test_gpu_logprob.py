@@ -159,6 +159,50 @@ def test_what_is_not_finite_stays_in_its_row(dt, vocab, at):
     assert torch.isfinite(out[[0, 3, 4]]).all() and (out[4] == 0).all() and out[1].isnan().all()
 
 
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("left", [0, 3, 8])
+def test_columns_of_a_wider_tensor(dt, left):
+    """Logits and their gradient as column ranges of wider tensors, which stay as they are beside them."""
+    X, x, labels, rng = _case(13, dt, 5, 1003, 1003)
+    wide = torch.full((5, 1003 + left + 9), float("nan"), dtype=DT[dt], device="cuda")
+    wide[:, left:left + 1003] = X
+    view = wide[:, left:left + 1003]
+    logp, lse = zo.token_logprob(view, i32(labels))
+    want, want_lse = ends.token_logprob(x, labels, 1.0)
+    tol, tol_lse = _logp_tol(x, want, want_lse, 1.0)
+    within(host(logp), want, tol)
+    within(host(lse), want_lse, tol_lse)
+    g = torch.from_numpy(rng.standard_normal(5).astype(np.float32)).cuda()
+    out = torch.full_like(wide, 7.0)
+    zo.token_logprob_backward(view, i32(labels), lse, g, out=out[:, left:left + 1003])
+    dx, dtol = _grad_tol(x, labels, host(lse), host(g), 1.0, dt)
+    within(host(out)[:, left:left + 1003], dx, dtol)
+    assert (out[:, :left] == 7.0).all() and (out[:, left + 1003:] == 7.0).all()
+
+
+@pytest.mark.parametrize("rows,vocab", [(70001, 17), (4300001, 8)])
+def test_many_short_rows(rows, vocab):
+    """More rows than a grid's second dimension holds, and more workgroups than a row of the grid."""
+    g = torch.Generator(device="cuda").manual_seed(3)
+    X = (2 * torch.randn(rows, vocab, generator=g, device="cuda")).bfloat16()
+    labels = torch.randint(-3, vocab, (rows,), generator=g, device="cuda").int()
+    up = torch.randn(rows, generator=g, device="cuda")
+    logp, lse = zo.token_logprob(X, labels)
+    dX = zo.token_logprob_backward(X, labels, lse, up)
+    x, on = X.double(), labels >= 0
+    z = torch.logsumexp(x, 1)
+    want = (x.gather(1, labels.long().clamp(min=0)[:, None])[:, 0] - z) * on
+    total = (4 * (np.log(vocab) + 1) + 2 + vocab / 64 + 16) * U32
+    assert ((logp - want).abs() <= (total + U32 * want.abs()) * NEAR).all()
+    assert ((lse - z * on).abs() <= (total + U32 * z.abs()) * NEAR).all()
+    a = x - lse.double()[:, None]
+    hit = torch.arange(vocab, device="cuda") == labels[:, None]
+    grad = up.double()[:, None] * (hit.double() - a.exp()) * on[:, None]
+    tol = ((up.abs()[:, None] * a.exp() * (3 * a.abs() + 3) * U32 + (4 * U32 + U["bf16"]) * grad.abs()) * NEAR + TINY["bf16"]
+           + up.abs()[:, None] * 2.0 ** -125)
+    assert ((dX - grad).abs() <= tol)[on].all() and (dX[~on] == 0).all()
+
+
 def test_large_logits_keep_their_differences():
     """Logits around 10^5: lse is coarse there, logp is not."""
     x = np.array([[1e5, 1e5 + 1, 1e5 - 2, 0.0], [-1e5, -1e5 + 0.5, -3e5, -1e5]])
