@@ -7,7 +7,7 @@ namespace {
 
 constexpr int SORT_WAVES = 8, SORT_TILE = SORT_WAVES * 256;  // of a sorting workgroup, and its tokens
 constexpr int DIGITS = 512;     // 9 bits a pass: two passes sort any vocabulary below 2^18
-constexpr int SORT_ONE = 8192;  // tokens that one workgroup of 16 waves sorts (22 us; in tiles 4 launches, no faster)
+constexpr int SORT_ONE = 8192;  // tokens that one workgroup of 16 waves sorts (20 us; in tiles 4 launches, no faster)
 // Tokens that are compared rather than sorted.  us, compared and sorted, adding rows of 4096 bf16 to fp32: 256 tokens of a
 // text 5.8 and 18.8, 500 8.0 and 19.3, 1000 15.9 and 22.7; 500 times the same token 42 and 15, 1000 times 116 and 15.
 constexpr int FEW = 512;
@@ -76,7 +76,7 @@ __global__ __launch_bounds__(256) void k_embedding(const int* __restrict__ ids, 
 // ---------------------------------------------------------------- sorting
 // Stable radix sort of the pairs (token, row), least digit first.  Tokens that have no row of the table are taken as
 // `vocab` and so come last.  While few workgroups sort, the others of the launch clear their share of a dense gradient:
-// the sorting of 8192 tokens, 22 us, is hidden behind the 80 that clearing 50272 x 5120 bf16 takes (6.4 TB/s).
+// the sorting of 8192 tokens, 20 us, is hidden behind the 80 that clearing 50272 x 5120 bf16 takes (6.4 TB/s).
 struct SortPlan {
   int n, vocab, ntiles, passes, shift[4], mask[4];
 };
@@ -133,8 +133,8 @@ __device__ __forceinline__ int digits_before(int count, int* wsum) {
   return base;
 }
 
-// The whole sort in one workgroup: (token << 13 | row) in LDS from pass to pass.  Its ballots bound it, 6 us for 300 tokens, 22 for
-// 8192.
+// The whole sort in one workgroup: (token << 13 | row) in LDS from pass to pass.  Ballots and LDS round trips in a row bound it, 6 us
+// for 300 tokens, 20 for 8192.
 __global__ __launch_bounds__(1024) void k_sort_one(const int* __restrict__ ids, SortPlan p, int* key_out, int* row_out, Fill f,
                                                    int* bad_flag) {
   __shared__ unsigned item[SORT_ONE];
@@ -173,19 +173,19 @@ __global__ __launch_bounds__(1024) void k_sort_one(const int* __restrict__ ids, 
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
       if (k >= groups || first + k * 64 >= p.n) continue;
-      const int digit = (it[k] >> shift) & mask, to = start[digit] + cnt[w][digit] + rank[k];
-      if (pass + 1 < p.passes) {
-        item[to] = it[k];
-      } else {
-        key_out[to] = (int)(it[k] >> 13);
-        row_out[to] = (int)(it[k] & 8191);
-      }
+      const int digit = (it[k] >> shift) & mask;
+      item[start[digit] + cnt[w][digit] + rank[k]] = it[k];
     }
-    if (pass + 1 == p.passes) break;
     __syncthreads();
 #pragma unroll
     for (int k = 0; k < 8; ++k)
       if (k < groups && first + k * 64 < p.n) it[k] = item[first + k * 64];
+  }
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    if (k >= groups || first + k * 64 >= p.n) continue;
+    key_out[first + k * 64] = (int)(it[k] >> 13);
+    row_out[first + k * 64] = (int)(it[k] & 8191);
   }
 }
 
