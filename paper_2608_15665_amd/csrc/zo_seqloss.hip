@@ -361,7 +361,7 @@ __global__ __launch_bounds__(256) void k_policy_total(PolicyArgs a) {
 
 // All rows of a block by one workgroup, a thread per row: few rows need no other launch (1600 rows 5.0 us).  A row's sequence is
 // the last one that starts at it or before.
-constexpr int FEW_SEQS = 256, FEW_ROWS = 2;  // sequences, and rows of a thread
+constexpr int FEW_SEQS = 256, FEW_ROWS = 4;  // sequences, and rows of a thread
 __global__ __launch_bounds__(1024) void k_policy_few(PolicyArgs a) {
   __shared__ int start[FEW_SEQS + 1], count[FEW_SEQS];
   const int b = blockIdx.x, t0 = threadIdx.x;
@@ -438,9 +438,10 @@ int zo_preference_loss_launch(int nblk, int rows, int pairs, int kind, int avera
                               double weight, const float* logp, const float* ref_logp, const int* labels, const int* seq_start,
                               double* loss, float* rewards, float* dlogp, int* bad_flag, void* ws, hipStream_t stream,
                               size_t* ws_needed) {
-  // us of the kernels (each launch costs the host 3 more): 2 pairs of 200 rows 5.8 in one launch and 7.2 in two, 2 of 1000 9.6
-  // and 7.5, 64 of 30 20.8 and 7.2.
-  const bool few = rows <= 1024 && pairs <= 16;
+  // us a call with one launch and with two, from Python one after another (the host bounds them) and in a graph: 2 pairs of 200
+  // rows 7.6, 11.9 and 5.1, 6.6; 8 of 256 7.7, 12.0 and 5.7, 6.6; 1 of 1024 8.5, 11.9 and 8.8, 6.6; but 32 pairs, two a wave, 10.8,
+  // 11.9 and 11.2, 6.4.
+  const bool few = rows <= 2048 && rows <= 1024LL * pairs && pairs <= 16;
   if (ws_needed) {
     *ws_needed = few ? 0 : zo_align256((size_t)nblk * pairs * sizeof(double));
     return ZO_OK;
@@ -467,8 +468,8 @@ int zo_policy_loss_launch(int nblk, int rows, int nseq, int aggregate, int per_t
                           double kl_coef, double weight, const float* logp, const float* old_logp, const float* ref_logp,
                           const float* advantage, const int* labels, const int* seq_start, double* loss, double* stats,
                           float* dlogp, int* bad_flag, void* ws, hipStream_t stream, size_t* ws_needed) {
-  // us of the kernels: 16 sequences of 100 rows 6.8 in one launch and 6.9 in two (each costs the host 3 more), of 500 (8 rows a
-  // thread) 18.0 and 7.0.
+  // us a call with one launch and with two, from Python one after another (the host bounds them) and in a graph: 16 sequences of
+  // 100 rows 8.4, 12.8 and 6.2, 5.9; of 250 10.0, 12.9 and 10.5, 5.9; 500 rows each, 8 a thread, 18 in a graph.
   const bool few = rows <= 1024 * FEW_ROWS && nseq <= FEW_SEQS;
   const int ncount = rows < 256 * 4096 ? (rows + 4095) / 4096 + (rows == 0) : 256;
   WsCarver w(ws);

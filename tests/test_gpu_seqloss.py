@@ -25,6 +25,8 @@ LENGTHS = {
     "long": [20000, 9, 1025, 4096],
     "thousand": [3] * 1024 + [5] * 200,
     "short": [int(n) for n in np.random.default_rng(3).integers(0, 90, 256)],
+    "several": [480, 3, 0, 511, 700, 290],
+    "full": [16] * 250,
     "pairs": [int(n) for n in np.random.default_rng(1).integers(100, 600, 40)],
 }
 
