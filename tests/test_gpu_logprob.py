@@ -242,6 +242,17 @@ def test_gradient_is_the_slope_of_the_forward():
         within(dX[:, j], g * slope / (2 * h), np.abs(g) * (1.3 ** 3 * h * h / 6 + 2 * 2.0 ** -19 / (2 * h)), f"column {j}")
 
 
+@pytest.mark.parametrize("rows,vocab", [(3, 200), (4, 140001), (5000, 300)])
+def test_without_the_log_sums(rows, vocab):
+    X, _, labels, _ = _case(5, "bf16", rows, vocab, vocab)
+    want, _ = zo.token_logprob(X, i32(labels))
+    logp, lab = torch.full((rows,), 9.0, device="cuda"), i32(labels)
+    ws = torch.empty(1 << 16, dtype=torch.uint8, device="cuda")
+    _lib._check(zo.lib().zo_token_logprob(1, rows, vocab, zo.ZO_BF16, X.data_ptr(), vocab, lab.data_ptr(), 1.0, logp.data_ptr(),
+                                          None, None, ws.data_ptr(), ws.numel(), _lib._stream_handle()))
+    np.testing.assert_array_equal(bits(logp), bits(want))
+
+
 def test_no_rows():
     none = torch.empty(0, dtype=torch.int32, device="cuda")
     logp, lse = zo.token_logprob(torch.empty(0, 50, device="cuda"), none)

@@ -164,6 +164,23 @@ def test_masks_that_leave_nothing():
         assert (loss == 0).all() and (stats == 0).all() and (d[:, :8] == 0).all() and (d[:, 8] == 9).all()
 
 
+@pytest.mark.parametrize("rows,lead", [(12, 0), (5000, 4700)])
+def test_as_many_blocks_as_a_grid_holds(rows, lead):
+    """65535 blocks for the small batch's launch, a few hundred for the others'; every block against the others' formula."""
+    nblk = 65535 if rows == 12 else 400
+    start = np.array([0, 3, 5, 9, 12]) + lead
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x = -torch.rand(nblk, rows, generator=g, device="cuda")
+    seqs = [x[:, a:b].double().sum(1) for a, b in zip(start, start[1:])]
+    got = zo.preference_loss(x, i32(start), 0.5)
+    want = -torch.nn.functional.logsigmoid(0.5 * torch.stack([seqs[0] - seqs[1], seqs[2] - seqs[3]], 1)).mean(1)
+    assert ((got - want).abs() <= 1e-13 * want.abs()).all()
+    old = -torch.rand(rows, generator=g, device="cuda")
+    got = zo.policy_loss(x, old, f32(np.ones(4)), i32(start), clip_low=1.0, clip_high=1e3)
+    r = torch.exp((x.double() - old.double()))[:, start[0]:start[4]]
+    assert ((got + r.mean(1)).abs() <= 1e-13 * r.mean(1)).all()
+
+
 def test_no_rows():
     e = torch.empty(2, 0, device="cuda")
     assert (zo.preference_loss(e, i32([0, 0, 0]), 0.1) == 0).all()
