@@ -755,15 +755,17 @@ int zo_embedding(long long rows, int vocab, int d, int dtype, const int* ids,
  *   dE = round(G) for every v (zeros for a token that does not occur), or with
  *   accumulate != 0: dE[v] = round(dE[v] + G[v]) for the tokens that occur,
  *   other rows untouched.
- * Tokens are sorted (a stable radix sort) and each token's rows summed in fp32
- * in an order fixed by ids alone, so equal calls give equal bits.
+ * Tokens are sorted (a stable radix sort; a few are compared) and each token's
+ * rows summed in fp32 in an order that the ids and sizes fix, so equal calls
+ * give equal bits.
  * accumulate == 0 writes dE twice where it writes zeros first: nothing else may
  * read it while the call runs.  Negative tokens are left out, and so are those
  * >= vocab, which set bad_flag.
  *   dH   device, rows x d of dtype.      dE   device, vocab x d of out_dtype:
  *        dtype or ZO_F32.  It overlaps no other tensor of the call.
  * Limits: 0 <= rows <= 2^24; vocab < 2^30; the rest as for zo_embedding; the
- * workspace is not shared with a call that may run at the same time. */
+ * workspace (0 bytes for few tokens) is not shared with a call that may run at
+ * the same time. */
 size_t zo_embedding_backward_workspace(long long rows, int vocab, int d);
 int zo_embedding_backward(long long rows, int vocab, int d, int dtype,
                           const int* ids, const void* dH, float scale,
@@ -833,7 +835,8 @@ int zo_token_logprob_backward(int nblk, int T, int vocab, int dtype,
  *   rewards   device fp32 [nblk x 2 pairs], nullable: beta R_s (0 for a
  *             sequence without rows that count).
  *   dlogp     device fp32 [nblk x rows], nullable: the gradient of loss[b].
- * float64 arithmetic throughout; sums in a fixed order.
+ * float64 arithmetic throughout; sums in a fixed order.  The workspace (0 bytes
+ * for small batches) is not shared with a call that may run at the same time.
  * Limits: 1 <= nblk <= 65535, 1 <= pairs <= 2^22, 0 <= rows <= 2^29, nblk rows
  * and nblk pairs < 2^31;
  * beta finite and > 0, margin and weight finite, 0 <= smoothing <= 0.5 (0 but for
@@ -863,7 +866,7 @@ int zo_preference_loss(int nblk, int rows, int pairs, int kind, int average,
  *   advantage   device fp32, [rows] with per_token != 0, else [nseq].
  *   stats       device float64 [nblk x 2], nullable: the mean of k and the share
  *               of rows with r A > c A, over the N rows.
- *   logp, loss, dlogp, and the arithmetic as for zo_preference_loss.
+ *   logp, loss, dlogp, the arithmetic and the workspace as for zo_preference_loss.
  * Limits: those of zo_preference_loss with nseq for pairs; clip_low in [0, 1],
  * clip_high finite and >= 0, kl_coef finite and >= 0, weight finite. */
 typedef enum { ZO_AGG_TOKEN = 0, ZO_AGG_SEQUENCE = 1, ZO_AGG_SUM = 2 } zo_aggregate;
