@@ -783,7 +783,8 @@ int zo_embedding_backward(long long rows, int vocab, int d, int dtype,
  *          ZO_F16), ld elements apart (ld >= vocab: a padded head's columns
  *          behind the vocabulary are not read).
  *   logp   device fp32 [nblk T].          lse   the same, nullable.
- * A logit may be -infinity or the type's lowest value (a masked token); a row
+ * A logit may be -infinity or any finite value (a masked token's -1e30, the
+ * type's lowest); a row
  * with a NaN or +infinity, or with nothing but -infinity, gives NaN in logp.
  * Sums are taken in fp32 relative to the row's largest logit, logarithm and
  * differences in fp64, one rounding at the end: logp does not lose where lse

@@ -6,7 +6,7 @@
 namespace {
 
 constexpr float LOG2E = 1.4426950408889634f;
-constexpr float LEAST = -3.402823466e38f;  // the lowest finite fp32 value
+constexpr float LEAST = -16777216.f;  // powers of one pass stay between +-2^24, where their rounding is at most a half
 
 template <int DT>
 struct Elem {
@@ -64,7 +64,9 @@ __device__ __forceinline__ RowWords row_words(const char* x, int vocab) {
 
 // Sum of exp2(c x) relative to 2^R: s = sum of 2^(c x - R).  R only grows; every term is one multiply-add (c x is exact
 // in it) and one exponential.  R is a value of its own, not the rounding of a product that is formed again, so that what
-// it was rounded by cancels: the row's log-sum-exp is (R + log2 s) log 2.
+// it was rounded by cancels: the row's log-sum-exp is (R + log2 s) log 2.  R begins at -2^24 and not at the lowest value: were a
+// masked logit of -1e30 some thread's own R, the rounding of its product would be a power of 2^70, its exponential infinite,
+// and infinity times the 0 that raise() scales it by NaN.  As it is such a logit adds 0.
 struct Sum {
   float R, s;
   __device__ __forceinline__ void raise(float to) {
@@ -176,8 +178,8 @@ __device__ __forceinline__ void finish_row(const char* x, int vocab, int y, floa
   const int tid = threadIdx.x & (NT - 1);
   const float c = scale * LOG2E;
   double ref = (double)sum.R / (double)c;  // the sum is of exp(scale (x - ref))
-  if (!(sum.R > LEAST && sum.R < __builtin_inff())) {
-    // Nothing above the lowest value, or something beyond the largest: once more, with differences from the largest logit.
+  if (!(sum.R > LEAST && sum.R < -LEAST)) {
+    // No power above -2^24, or one beyond 2^24: once more, with differences from the largest logit.
     float m = -__builtin_inff();
     for (int j = tid; j < vocab; j += NT) m = fmaxf(m, EL::load(x + (size_t)j * EL::SIZE));
     m = group_max<NT>(m);

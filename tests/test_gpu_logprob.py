@@ -213,6 +213,37 @@ def test_large_logits_keep_their_differences():
     within(host(logp), want, (4 * 3 + 30) * U32 + 2 * U32 * np.abs(want))
 
 
+@pytest.mark.parametrize("dt,mask", [(dt, m) for dt in ["f32", "bf16", "f16"] for m in [-1e4, -1e7, -1.3e9, -1e10, -1e30, "lowest", "largest"]
+                                     if dt != "f16" or m in (-1e4, "lowest", "largest")])
+@pytest.mark.parametrize("vocab", [9, 1000, 40001, 140001])
+@pytest.mark.parametrize("scale", [1.0, 0.5, 1.0 / 128, 40.0])
+def test_large_finite_masks(dt, vocab, mask, scale):
+    """Masks of any finite size, in all places but one, in the second half, everywhere; the value at the other end, as one
+    logit or as all."""
+    end = float(torch.finfo(DT[dt]).max)
+    value = {"lowest": -end, "largest": end}.get(mask, mask)
+    rng = np.random.default_rng(vocab)
+    a = 3 * rng.standard_normal((4, vocab))
+    a[0, :vocab // 2] = value
+    a[0, vocab // 2 + 1:] = value
+    a[1, vocab // 2:] = value
+    a[2] = value
+    a[3, 5] = -value
+    X, x = put(a, dt)
+    labels = np.array([vocab // 2, 1, 3, 5])
+    logp, lse = zo.token_logprob(X, i32(labels), scale=scale)
+    d = scale * (x - x.max(-1, keepdims=True))
+    ls = np.log(np.exp(d).sum(-1))
+    want, want_lse = np.take_along_axis(d, labels[:, None], 1)[:, 0] - ls, scale * x.max(-1) + ls
+    tol, tol_lse = _logp_tol(x, want, want_lse, scale)
+    over = np.abs(want_lse) > torch.finfo(torch.float32).max
+    lost = np.abs(want) > torch.finfo(torch.float32).max
+    got, got_lse = host(logp), host(lse)
+    assert (got_lse[over] == np.sign(want_lse[over]) * INF).all() and (got[lost] == -INF).all()
+    within(got_lse[~over], want_lse[~over], tol_lse[~over], "lse")
+    within(got[~lost], want[~lost], tol[~lost], "logp")
+
+
 def test_labels_that_the_vocabulary_lacks():
     X, x, _, _ = _case(7, "bf16", 4, 100, 104)
     flag = torch.zeros(1, dtype=torch.int32, device="cuda")
