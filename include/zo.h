@@ -801,16 +801,20 @@ int zo_token_logprob(int nblk, int T, int vocab, int dtype, const void* X,
 
 /* The logits' gradient from the gradient g of logp (device fp32 [nblk T]):
  *   dX[i][j] = round(scale g[i] ([j = y] - exp(scale X[i][j] - lse[i])))
- * with lse as zo_token_logprob gave it (fp32: where |lse| is large, so is its
- * rounding, and exp() is |lse| 2^-24 off).  y < 0: zeros (X and g not read);
- * y >= vocab: NaN and bad_flag.  dX has X's layout and dtype, rows ldo apart;
- * it may be X itself (ldo = ld).  Columns behind the vocabulary stay as they
- * are.  fp32 arithmetic, one rounding.  Limits as for zo_token_logprob. */
+ * with lse as zo_token_logprob gave it.  lse is fp32: where |lse| is large (rows
+ * of large logits, or of the type's lowest value alone), so is its rounding, and
+ * exp() is |lse| 2^-24 off.  With logp (its other result; nullable), rows with
+ * |logp| < |lse| are taken as exp(scale (X[i][j] - X[i][y]) + logp[i]), which is
+ * |logp| 2^-24 off.  y < 0: zeros (X and g not read); y >= vocab: NaN and
+ * bad_flag.  dX has X's layout and dtype, rows ldo apart; it may be X itself
+ * (ldo = ld, logp NULL: another part of a row may have replaced X[i][y]).
+ * Columns behind the vocabulary stay as they are.  fp32 arithmetic, one
+ * rounding.  Limits as for zo_token_logprob. */
 int zo_token_logprob_backward(int nblk, int T, int vocab, int dtype,
                               const void* X, long long ld, const int* labels,
-                              float scale, const float* lse, const float* g,
-                              void* dX, long long ldo, int* bad_flag,
-                              void* stream);
+                              float scale, const float* lse,
+                              const float* logp, const float* g, void* dX,
+                              long long ldo, int* bad_flag, void* stream);
 
 /* Sequences of a loss: row t of sequence s for seq_start[s] <= t <
  * seq_start[s + 1] (device int32 [nseq + 1], not decreasing, within [0, rows]);

@@ -245,7 +245,7 @@ def lib() -> ctypes.CDLL:
             L.zo_token_logprob_workspace.restype = c_sz
             L.zo_token_logprob_workspace.argtypes = [c_int] * 4
             L.zo_token_logprob_backward.restype = c_int
-            L.zo_token_logprob_backward.argtypes = [c_int] * 4 + [c_vp, c_ll, c_vp, c_f, c_vp, c_vp, c_vp, c_ll, c_vp, c_vp]
+            L.zo_token_logprob_backward.argtypes = [c_int] * 4 + [c_vp, c_ll, c_vp, c_f, c_vp, c_vp, c_vp, c_vp, c_ll, c_vp, c_vp]
             L.zo_preference_loss_workspace.restype = c_sz
             L.zo_preference_loss_workspace.argtypes = [c_int] * 3
             L.zo_preference_loss.restype = c_int
@@ -1254,10 +1254,11 @@ def token_logprob(logits: torch.Tensor, labels: torch.Tensor, vocab: Optional[in
 
 def token_logprob_backward(logits: torch.Tensor, labels: torch.Tensor, lse: torch.Tensor, grad: torch.Tensor,
                            vocab: Optional[int] = None, scale: float = 1.0, out: Optional[torch.Tensor] = None,
-                           bad_flag: Optional[torch.Tensor] = None):
+                           bad_flag: Optional[torch.Tensor] = None, logp: Optional[torch.Tensor] = None):
     """The logits' gradient from grad, the gradient of token_logprob's logp, with its lse: in out (the logits' shape and
     type; it may be the logits themselves; columns behind `vocab` are left as they are) or a new tensor, zeros there.
-    See zo_token_logprob_backward."""
+    With its logp too (and out not the logits), rows of large logits are as exact as others.  See
+    zo_token_logprob_backward."""
     here = torch._C._cuda_getDevice()
     nblk, T, vocab, ld, lab = _logits(logits, labels, vocab, here)
     n, cols = logits.shape
@@ -1266,6 +1267,7 @@ def token_logprob_backward(logits: torch.Tensor, labels: torch.Tensor, lse: torc
     ldo = _row_tensor(out, "out", logits.dtype, n, cols, here)
     _check(lib().zo_token_logprob_backward(nblk, T, vocab, _DT[logits.dtype], logits.data_ptr(), ld, lab, scale,
                                            _here(lse, "lse", torch.float32, here, n),
+                                           _optional(logp, "logp", torch.float32, here, n),
                                            _here(grad, "grad", torch.float32, here, n), out.data_ptr(), ldo,
                                            _flag(bad_flag, here), _stream_handle()))
     return out

@@ -1215,16 +1215,19 @@ int zo_token_logprob(int nblk, int T, int vocab, int dtype, const void* X, long 
 }
 
 int zo_token_logprob_backward(int nblk, int T, int vocab, int dtype, const void* X, long long ld, const int* labels, float scale,
-                              const float* lse, const float* g, void* dX, long long ldo, int* bad_flag, void* stream) {
+                              const float* lse, const float* logp, const float* g, void* dX, long long ldo, int* bad_flag,
+                              void* stream) {
   const char* what = "token_logprob_backward";
   const int st = check_logprob(what, nblk, T, vocab, dtype, X, ld, labels, scale, bad_flag);
   if (st != ZO_OK) return st;
   if (T == 0) return ZO_OK;
-  ZO_CHECK(lse && g && aligned(lse, 4) && aligned(g, 4), "%s: lse or g is NULL or not 4-byte aligned", what);
+  ZO_CHECK(lse && g && aligned(lse, 4) && aligned(g, 4) && aligned(logp, 4),
+           "%s: lse or g is NULL, or lse, logp or g not 4-byte aligned", what);
   ZO_CHECK(dX && aligned(dX, dtype == ZO_F32 ? 4 : 2), "%s: dX is NULL or not aligned", what);
   ZO_CHECK(ldo >= vocab && ldo < (1LL << 31), "%s: rows of dX are %lld elements apart (vocab = %d)", what, ldo, vocab);
   ZO_CHECK(dX != X || ldo == ld, "%s: dX is X, with another row distance", what);
-  return zo_token_logprob_backward_launch(nblk, T, vocab, dtype, X, ld, labels, scale, lse, g, dX, ldo, bad_flag,
+  ZO_CHECK(dX != X || !logp, "%s: dX is X, and logp is given", what);
+  return zo_token_logprob_backward_launch(nblk, T, vocab, dtype, X, ld, labels, scale, lse, logp, g, dX, ldo, bad_flag,
                                           (hipStream_t)stream);
 }
 

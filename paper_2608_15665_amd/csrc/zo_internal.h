@@ -240,8 +240,8 @@ int zo_embedding_backward_launch(long long rows, int vocab, int d, int dtype, co
 int zo_token_logprob_launch(int nblk, int T, int vocab, int dtype, const void* X, long long ld, const int* labels, float scale,
                             float* logp, float* lse, int* bad_flag, void* ws, hipStream_t stream, size_t* ws_needed);
 int zo_token_logprob_backward_launch(int nblk, int T, int vocab, int dtype, const void* X, long long ld, const int* labels,
-                                     float scale, const float* lse, const float* g, void* dX, long long ldo, int* bad_flag,
-                                     hipStream_t stream);
+                                     float scale, const float* lse, const float* logp, const float* g, void* dX, long long ldo,
+                                     int* bad_flag, hipStream_t stream);
 // Losses over sequences (zo_seqloss.hip).
 int zo_preference_loss_launch(int nblk, int rows, int pairs, int kind, int average, double beta, double margin, double smoothing,
                               double weight, const float* logp, const float* ref_logp, const int* labels, const int* seq_start,

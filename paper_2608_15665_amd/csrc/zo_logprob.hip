@@ -273,6 +273,7 @@ constexpr int BACK_U = 2;
 template <int DT>
 __global__ __launch_bounds__(256) void k_token_logprob_backward(const char* X, long long ld, const int* __restrict__ labels,
                                                                 float scale, const float* __restrict__ lse,
+                                                                const float* __restrict__ logp,
                                                                 const float* __restrict__ g, char* dX, long long ldo,
                                                                 int* bad_flag, int T, int vocab, unsigned rows) {
   using EL = Elem<DT>;
@@ -281,16 +282,21 @@ __global__ __launch_bounds__(256) void k_token_logprob_backward(const char* X, l
     const int y = labels[row % (unsigned)T];
     const char* x = X + (size_t)row * ld * EL::SIZE;
     char* out = dX + (size_t)row * ldo * EL::SIZE;
-    float up = 0.f, z = 0.f;
+    float up = 0.f, z = 0.f, ref = 0.f;
     if (y >= vocab) {
       up = __builtin_nanf("");
       if (bad_flag && blockIdx.x == 0 && tid == 0) *bad_flag = 1;
     } else if (y >= 0) {
       up = scale * g[row];
       z = lse[row];
+      // The smaller of the two has the smaller rounding: c (x - x_y) + logp is c x - lse.
+      if (logp && fabsf(logp[row]) < fabsf(z)) {
+        z = -logp[row];
+        ref = EL::load(x + (size_t)y * EL::SIZE);
+      }
     }
     auto grad = [&](float v, bool hit) {
-      const float p = __builtin_amdgcn_exp2f(fmaf(v, scale, -z) * LOG2E);
+      const float p = __builtin_amdgcn_exp2f(fmaf(v - ref, scale, -z) * LOG2E);
       return up * ((hit ? 1.f : 0.f) - p);
     };
     if (((uintptr_t)x ^ (uintptr_t)out) & 15) {  // rows that begin elsewhere in a word
@@ -382,13 +388,13 @@ int zo_token_logprob_launch(int nblk, int T, int vocab, int dtype, const void* X
 }
 
 int zo_token_logprob_backward_launch(int nblk, int T, int vocab, int dtype, const void* X, long long ld, const int* labels,
-                                     float scale, const float* lse, const float* g, void* dX, long long ldo, int* bad_flag,
-                                     hipStream_t stream) {
+                                     float scale, const float* lse, const float* logp, const float* g, void* dX, long long ldo,
+                                     int* bad_flag, hipStream_t stream) {
   const unsigned rows = (unsigned)nblk * (unsigned)T;
   const int per = 256 * BACK_U * (dtype == ZO_F32 ? 4 : 8);
   const dim3 grid((unsigned)((vocab + (long long)per - 1) / per), rows < 65535 ? rows : 65535);
   auto go = [&](auto k) {
-    hipLaunchKernelGGL(k, grid, dim3(256), 0, stream, (const char*)X, ld, labels, scale, lse, g, (char*)dX, ldo, bad_flag, T,
+    hipLaunchKernelGGL(k, grid, dim3(256), 0, stream, (const char*)X, ld, labels, scale, lse, logp, g, (char*)dX, ldo, bad_flag, T,
                        vocab, rows);
   };
   if (dtype == ZO_F32) go(k_token_logprob_backward<ZO_F32>);

@@ -27,8 +27,8 @@ def _logprob(nblk=1, T=4, vocab=10, dtype=1, X=FAKE, ld=16, labels=FAKE, scale=1
 
 
 def _logprob_grad(nblk=1, T=4, vocab=10, dtype=1, X=FAKE, ld=16, labels=FAKE, scale=1.0, lse=FAKE, g=FAKE, dX=2 * FAKE, ldo=16,
-                  flag=None):
-    return zo.lib().zo_token_logprob_backward(nblk, T, vocab, dtype, X, ld, labels, scale, lse, g, dX, ldo, flag, None)
+                  flag=None, logp=None):
+    return zo.lib().zo_token_logprob_backward(nblk, T, vocab, dtype, X, ld, labels, scale, lse, logp, g, dX, ldo, flag, None)
 
 
 def _preference(nblk=1, rows=8, pairs=2, kind=0, average=0, beta=0.1, margin=0.0, smoothing=0.0, weight=1.0, logp=FAKE,
@@ -79,6 +79,7 @@ def test_logits(call, kw, needle):
 
 @pytest.mark.parametrize("kw,needle", [(dict(lse=None), "NULL"), (dict(g=None), "NULL"), (dict(dX=None), "dX is NULL"),
                                        (dict(dX=FAKE + 1), "dX"), (dict(ldo=9), "rows of dX"), (dict(dX=FAKE, ldo=24), "dX is X"),
+                                       (dict(dX=FAKE, logp=FAKE), "logp is given"), (dict(logp=FAKE + 2), "4-byte"),
                                        (dict(g=FAKE + 1), "4-byte")])
 def test_logits_gradient(kw, needle):
     assert _logprob_grad(**kw) == 1 and needle in _detail(), _detail()
@@ -178,6 +179,7 @@ I, F = (lambda *s: torch.zeros(*s, dtype=torch.int32)), torch.zeros
     (lambda: zo.token_logprob(F(8, 8), I(8).long()), TypeError, "labels must be"),
     (lambda: zo.token_logprob(F(8, 8), I(8), lse=F(7)), ValueError, "lse must hold 8"),
     (lambda: zo.token_logprob_backward(F(8, 8), I(8), F(8), F(7)), ValueError, "grad must hold 8"),
+    (lambda: zo.token_logprob_backward(F(8, 8), I(8), F(8), F(8), logp=F(7)), ValueError, "logp must hold 8"),
     (lambda: zo.token_logprob_backward(F(8, 8), I(8), F(8), F(8), out=F(8, 9)), ValueError, "out must be 8 x 8"),
     (lambda: zo.token_logprob_backward(F(8, 8), I(8), F(8).double(), F(8)), TypeError, "lse must be"),
     (lambda: zo.preference_loss(F(2, 3, 4), I(5), 0.1), ValueError, "nblk x rows"),

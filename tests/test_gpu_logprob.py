@@ -91,7 +91,7 @@ def test_rows_of_other_distances_and_places(dt, vocab, ldx, ldo, off):
     out = wide[off:off + 6 * ldo].view(6, ldo)
     lab, gd = i32(labels), torch.from_numpy(g).cuda()
     _lib._check(zo.lib().zo_token_logprob_backward(1, 6, vocab, _lib._DT[DT[dt]], X.data_ptr(), ldx, lab.data_ptr(), 1.0,
-                                                   lse.data_ptr(), gd.data_ptr(), out.data_ptr(), ldo, None,
+                                                   lse.data_ptr(), None, gd.data_ptr(), out.data_ptr(), ldo, None,
                                                    _lib._stream_handle()))
     dx, tol = _grad_tol(x, labels, host(lse), g.astype(np.float64), 1.0, dt)
     within(host(out)[:, :vocab], dx, tol, "dX")
@@ -242,6 +242,41 @@ def test_large_finite_masks(dt, vocab, mask, scale):
     assert (got_lse[over] == np.sign(want_lse[over]) * INF).all() and (got[lost] == -INF).all()
     within(got_lse[~over], want_lse[~over], tol_lse[~over], "lse")
     within(got[~lost], want[~lost], tol[~lost], "logp")
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("vocab", [9, 5003])
+def test_gradients_of_large_logits(dt, vocab):
+    """With logp the gradient does not hang on lse's rounding: rows around +-30000, a row of the type's lowest value alone
+    (uniform), one whose label is masked (lse alone serves it), an ordinary one and one that does not count."""
+    rng = np.random.default_rng(vocab)
+    lowest = float(torch.finfo(DT[dt]).min)
+    a = 3 * rng.standard_normal((6, vocab))
+    a[0] = 30000 + 256 * np.round(2 * rng.standard_normal(vocab))  # whole steps of every type there
+    a[1] = -30000 + 256 * np.round(2 * rng.standard_normal(vocab))
+    a[2] = lowest
+    a[3, 4] = -INF
+    X, x = put(a, dt)
+    labels, scale = np.array([1, 2, 3, 4, 5, -1]), 1.0 / 128
+    lab = i32(labels)
+    logp, lse = zo.token_logprob(X, lab, scale=scale)
+    g = rng.standard_normal(6).astype(np.float32)
+    out = host(zo.token_logprob_backward(X, lab, lse, torch.from_numpy(g).cuda(), scale=scale, logp=logp))
+    lp = host(logp)
+    assert lp[3] == -INF and abs(lp[2] + np.log(vocab)) < 1e-5
+    for r in range(5):
+        if r == 3:
+            t, z = scale * x[r], host(lse)[r]
+        else:
+            t = scale * (x[r] - x[r, labels[r]])
+            z = np.log(np.exp(t - t.max()).sum()) + t.max()  # -logp, exact
+        p = np.exp(t - z)
+        want = -scale * g[r] * p
+        want[labels[r]] += scale * g[r]
+        # As for other gradients, and logp's (or, masked, an input's) own rounding and error.
+        off = (4 * (np.log(vocab) + 1) + 18 + vocab / 64 + 2 * abs(z) + 4 * np.abs(np.maximum(t - z, -200)) + 3) * U32
+        within(out[r], want, (np.abs(scale * g[r]) * p * off + (4 * U32 + U[dt]) * np.abs(want)) * NEAR + TINY[dt] + 2.0 ** -125, f"row {r}")
+    assert (out[5] == 0).all()
 
 
 def test_labels_that_the_vocabulary_lacks():
