@@ -1177,7 +1177,7 @@ def embedding(ids: torch.Tensor, table: torch.Tensor, scale: float = 1.0, out: O
     if table.dim() != 2:
         raise ValueError("table must be vocab x d")
     vocab, d = table.shape
-    _fits(vocab, "vocab")
+    _fits(max(vocab, d), "vocab or d")
     rows = ids.numel()
     if out is None:
         out = torch.empty((*ids.shape, d), dtype=table.dtype, device=table.device)
@@ -1198,7 +1198,7 @@ def embedding_backward(ids: torch.Tensor, grad: torch.Tensor, vocab: int, scale:
     if dt not in _DT:
         raise TypeError(f"unsupported dtype {dt}")
     rows, d = ids.numel(), grad.shape[-1]
-    _fits(vocab, "vocab")
+    _fits(max(vocab, d), "vocab or d")
     if out is None:
         if accumulate:
             raise ValueError("accumulate needs out")
@@ -1314,6 +1314,7 @@ def preference_loss(logp: torch.Tensor, seq_start: torch.Tensor, beta: float, re
     pairs = (starts - 1) // 2
     if starts != 2 * pairs + 1 or pairs < 1:
         raise ValueError(f"seq_start must hold 2 pairs + 1 elements (got {starts})")
+    _fits(starts, "elements of seq_start")
     loss = _loss_out(loss, nblk, logp)
     tensors = (_here(logp, "logp", torch.float32, here, nblk * rows), _optional(ref_logp, "ref_logp", torch.float32, here, rows),
                _optional(labels, "labels", torch.int32, here, rows), _here(seq_start, "seq_start", torch.int32, here, starts),
@@ -1345,6 +1346,7 @@ def policy_loss(logp: torch.Tensor, old_logp: torch.Tensor, advantage: torch.Ten
     nseq = seq_start.numel() - 1
     if nseq < 1:
         raise ValueError(f"seq_start must hold nseq + 1 elements, nseq >= 1 (got {seq_start.numel()})")
+    _fits(nseq, "sequences")
     loss = _loss_out(loss, nblk, logp)
     tensors = (_here(logp, "logp", torch.float32, here, nblk * rows), _here(old_logp, "old_logp", torch.float32, here, rows),
                _optional(ref_logp, "ref_logp", torch.float32, here, rows),

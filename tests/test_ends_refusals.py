@@ -208,3 +208,17 @@ def test_binding_refuses_host_tensors(monkeypatch):
                  lambda: zo.preference_loss(F(2, 8), I(5), 0.1), lambda: zo.policy_loss(F(2, 8), F(8), F(4), I(5))):
         with pytest.raises(ValueError, match="current device"):
             call()
+
+
+def test_sizes_that_an_int_would_wrap(cpu):
+    """Columns and sequences beyond 2^32, as views of one element."""
+    wide = torch.zeros(1, 1).expand(1, 2 ** 32 + 8)
+    with pytest.raises(ValueError, match="out of range"):
+        zo.embedding(I(1), wide)
+    with pytest.raises(ValueError, match="out of range"):
+        zo.embedding_backward(I(1), wide, 8)
+    starts = torch.zeros(1, dtype=torch.int32).expand(2 ** 33 + 3)
+    with pytest.raises(ValueError, match="out of range"):
+        zo.preference_loss(F(8), starts, 0.1)
+    with pytest.raises(ValueError, match="out of range"):
+        zo.policy_loss(F(8), F(8), F(8), starts)
