@@ -784,8 +784,8 @@ int zo_embedding_backward(long long rows, int vocab, int d, int dtype,
  *          behind the vocabulary are not read).
  *   logp   device fp32 [nblk T].          lse   the same, nullable.
  * A logit may be -infinity or any finite value (a masked token's -1e30, the
- * type's lowest); a row
- * with a NaN or +infinity, or with nothing but -infinity, gives NaN in logp.
+ * type's lowest); a row with a NaN or +infinity, or with nothing but -infinity,
+ * gives NaN in logp.
  * Sums are taken in fp32 relative to the row's largest logit, logarithm and
  * differences in fp64, one rounding at the end: logp does not lose where lse
  * is large.  The workspace holds partial sums where few long rows are split over
