@@ -64,17 +64,21 @@ __device__ __forceinline__ RowWords row_words(const char* x, int vocab) {
 
 // Sum of exp2(c x) relative to 2^R: s = sum of 2^(c x - R).  R only grows; every term is one multiply-add (c x is exact
 // in it) and one exponential.  R is a value of its own, not the rounding of a product that is formed again, so that what
-// it was rounded by cancels: the row's log-sum-exp is (R + log2 s) log 2.  R begins at -2^24 and not at the lowest value: were a
+// it was rounded by cancels: the row's log-sum-exp is (R + log2 s) log 2.  For that the product that becomes R may not be
+// contracted into the difference that the sum is scaled by: R there would be the product before its rounding, and a carried sum
+// 2^(R's rounding) off, 4 % at logits of 10^6.  R begins at -2^24 and not at the lowest value: were a
 // masked logit of -1e30 some thread's own R, the rounding of its product would be a power of 2^70, its exponential infinite,
 // and infinity times the 0 that raise() scales it by NaN.  As it is such a logit adds 0.
 struct Sum {
   float R, s;
   __device__ __forceinline__ void raise(float to) {
+#pragma clang fp contract(off)
     s *= __builtin_amdgcn_exp2f(R - to);
     R = to;
   }
   template <int N>
   __device__ __forceinline__ void add(const float* x, float c) {
+#pragma clang fp contract(off)
     float m = x[0];
 #pragma unroll
     for (int k = 1; k < N; ++k) m = fmaxf(m, x[k]);
