@@ -867,7 +867,8 @@ int zo_preference_loss(int nblk, int rows, int pairs, int kind, int average,
  *   (a sum over no rows is 0).  The gradient of l is [r A <= c A] (-r A) +
  *   kl_coef (1 - exp(d)).
  *   old_logp    device fp32 [rows].
- *   ref_logp    device fp32 [rows]; NULL: no KL term (kl_coef is then 0).
+ *   ref_logp    device fp32 [rows]; NULL: no KL term (kl_coef is then 0).  With
+ *               kl_coef = 0 k is in stats alone, infinite ones too.
  *   advantage   device fp32, [rows] with per_token != 0, else [nseq].
  *   stats       device float64 [nblk x 2], nullable: the mean of k and the share
  *               of rows with r A > c A, over the N rows.

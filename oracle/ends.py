@@ -120,8 +120,9 @@ def policy_loss(logp, old, adv, labels, start, ref=None, per_token=False, low=0.
             clipped += r * A > c * A
             if ref is not None:
                 d = float(ref[t]) - p
-                l += kl_coef * (np.exp(d) - d - 1)
-                slope += kl_coef * (1 - np.exp(d))
+                if kl_coef != 0:
+                    l += kl_coef * (np.exp(d) - d - 1)
+                    slope += kl_coef * (1 - np.exp(d))
                 kl += np.exp(d) - d - 1
             loss += share * l
             grad[t] = share * slope

@@ -244,8 +244,10 @@ __device__ __forceinline__ double policy_term(const PolicyArgs& a, float logp, c
   double l = cut ? -kept : -plain, slope = cut ? 0.0 : -plain;
   if (a.ref) {
     const double d = (double)x.ref - p, e = exp(d), k = d < __builtin_inf() ? e - d - 1.0 : e;  // infinite at d = inf
-    l += a.kl * k;
-    slope += a.kl * (1.0 - e);
+    if (a.kl != 0.0) {  // else an infinite k is only reported
+      l += a.kl * k;
+      slope += a.kl * (1.0 - e);
+    }
     v[1] += k;
   }
   v[0] += l;
