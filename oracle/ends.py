@@ -1,5 +1,7 @@
 """The two ends of a language model in float64: embedding and its gradient, log-probabilities of labels and the logits'
 gradient, the preference and policy losses with theirs.  Written row by row from their formulas."""
+import math
+
 import numpy as np
 
 
@@ -98,6 +100,16 @@ def preference_loss(logp, ref, labels, start, beta, kind="sigmoid", average=Fals
     return weight / pairs * loss, rewards, grad
 
 
+def _kl(d):
+    """(exp(d) - d - 1, exp(d) - 1), by exp's series where the differences would cancel."""
+    if abs(d) < 0.5:
+        k = sum(d ** n / math.factorial(n) for n in range(20, 1, -1))
+        return k, k + d
+    with np.errstate(over="ignore"):
+        m = np.expm1(d)
+    return (m - d if d < np.inf else m), m
+
+
 def policy_loss(logp, old, adv, labels, start, ref=None, per_token=False, low=0.2, high=0.2, kl_coef=0.0, aggregate="token",
                 weight=1.0):
     """(loss, [mean k, share of clipped rows], gradient) of one block; rows of the gradient in no sequence are NaN."""
@@ -120,10 +132,11 @@ def policy_loss(logp, old, adv, labels, start, ref=None, per_token=False, low=0.
             clipped += r * A > c * A
             if ref is not None:
                 d = float(ref[t]) - p
+                k, m = _kl(d)
                 if kl_coef != 0:
-                    l += kl_coef * (np.exp(d) - d - 1)
-                    slope += kl_coef * (1 - np.exp(d))
-                kl += np.exp(d) - d - 1
+                    l += kl_coef * k
+                    slope -= kl_coef * m
+                kl += k
             loss += share * l
             grad[t] = share * slope
     return loss, np.array([kl, clipped]) / max(N, 1), grad

@@ -235,24 +235,57 @@ __device__ __forceinline__ PolicyRow policy_row(const PolicyArgs& a, int t, int 
   return {a.old[t], a.ref ? a.ref[t] : 0.f, a.adv[a.per_token ? t : s], a.labels ? a.labels[t] : 0};
 }
 
+// exp(d) = 2^n (1 + r + q): d = n log 2 + r with |r| <= log(2) / 2, and q = exp(r) - r - 1 by its series, r^2 (1/2! + r/3! + ... +
+// r^11/13!), 2^-52 of it left out.  Below -800 exp is 0; n stops at 1154, where it is infinite whatever r is; NaN stays in r.
+struct Exponential {
+  double r, q;
+  int n;
+  __device__ __forceinline__ explicit Exponential(double d) {
+    constexpr double over[12] = {1.0 / 6227020800.0, 1.0 / 479001600.0, 1.0 / 39916800.0, 1.0 / 3628800.0, 1.0 / 362880.0, 1.0 / 40320.0,
+                                 1.0 / 5040.0,       1.0 / 720.0,       1.0 / 120.0,      1.0 / 24.0,      1.0 / 6.0,      0.5};
+    const double x = d < -800.0 ? -800.0 : d;
+    const double e = fmin(rint(x * 1.4426950408889634), 1154.0);
+    r = fma(-e, 2.3190468138462996e-17, fma(-e, 0.6931471805599453, x));  // log 2 in two parts
+    double p = over[0];
+#pragma unroll
+    for (int i = 1; i < 12; ++i) p = fma(p, r, over[i]);
+    q = r * r * p;
+    n = (int)e;
+  }
+  __device__ __forceinline__ double value() const { return ldexp(1.0 + (r + q), n); }
+};
+
+// k = exp(d) - d - 1 and m = exp(d) - 1, without the differences that would cancel where the models nearly agree (at d = 1e-6 k would
+// keep four digits): with t = 2^n, k = t q + (t - 1 + (t r - d)), which is q at n = 0; elsewhere k is at least 0.047 exp(d).
+__device__ __forceinline__ double kl_term(double d, double* m) {
+  const Exponential e(d);
+  const double t = ldexp(1.0, e.n), t1 = t - 1.0;
+  const bool huge = e.n > 1023;  // t is infinite, or d is NaN
+  *m = huge ? t * d : fma(t, e.r + e.q, t1);
+  return huge ? t * d : fma(t, e.q, t1 + fma(t, e.r, -d));
+}
+
 // Adds a row that counts to (loss, k), says whether it is clipped and returns its slope.
+template <bool GRAD>
 __device__ __forceinline__ double policy_term(const PolicyArgs& a, float logp, const PolicyRow& x, double* v, bool* clipped) {
-  const double p = logp, A = x.adv, r = exp(p - (double)x.old);
-  const double c = r < 1.0 - a.low ? 1.0 - a.low : (r > 1.0 + a.high ? 1.0 + a.high : r);
-  const double plain = r * A, kept = c * A;
+  const double p = logp, A = x.adv, r = Exponential(p - (double)x.old).value();
+  const double c = fmin(fmax(r, 1.0 - a.low), 1.0 + a.high);
+  const double plain = r * A, kept = c * A;  // where r is NaN, plain is
   const bool cut = plain > kept;
-  double l = cut ? -kept : -plain, slope = cut ? 0.0 : -plain;
+  double gain = cut ? kept : plain, rise = 0.0;
+  if constexpr (GRAD) rise = cut ? 0.0 : plain;
   if (a.ref) {
-    const double d = (double)x.ref - p, e = exp(d), k = d < __builtin_inf() ? e - d - 1.0 : e;  // infinite at d = inf
+    double m;
+    const double k = kl_term((double)x.ref - p, &m);
     if (a.kl != 0.0) {  // else an infinite k is only reported
-      l += a.kl * k;
-      slope += a.kl * (1.0 - e);
+      gain -= a.kl * k;
+      if constexpr (GRAD) rise += a.kl * m;
     }
     v[1] += k;
   }
-  v[0] += l;
+  v[0] -= gain;
   *clipped = cut;
-  return slope;
+  return -rise;
 }
 
 __device__ __forceinline__ double inverse(double n) { return n > 0.0 ? 1.0 / n : 0.0; }
@@ -272,18 +305,18 @@ __global__ __launch_bounds__(256) void k_policy_count(PolicyArgs a) {
 // NT threads take a sequence, under NB blocks at once: what the blocks share is loaded once.  Float64 bounds it beside its
 // start: two exponentials of some 30 instructions a row and block; 512 sequences of up to 1024 rows under 16 blocks 21 us (with
 // one block a workgroup 24, four 25), twice the rows 13 more.
-template <int NT, int NB>
+template <int NT, int NB, bool GRAD>
 __global__ __launch_bounds__(NT < 256 ? 256 : NT) void k_policy(PolicyArgs a) {
   const int s = NT < 256 ? blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x, b0 = blockIdx.y * NB;
   double n[1] = {0.0};
-  if (a.dlogp && a.aggregate == ZO_AGG_TOKEN) {
+  if (GRAD && a.aggregate == ZO_AGG_TOKEN) {
     for (int i = threadIdx.x & (NT - 1); i < a.ncount; i += NT) n[0] += a.counted[i];
     group_sum<NT, 1>(n);
   }
   if (s >= a.nseq) return;
   const bool first = (threadIdx.x & (NT - 1)) == 0;
   const Span sp = span_of(a.start, s, a.rows, first && b0 == 0 ? a.bad_flag : nullptr);
-  if (a.dlogp && a.aggregate == ZO_AGG_SEQUENCE) {
+  if (GRAD && a.aggregate == ZO_AGG_SEQUENCE) {
     int c[1] = {0};
     each_row<NT>(sp, [&](int t) { return a.labels ? a.labels[t] : 0; }, [&](int, bool in, int y) { c[0] += lanes(in && y >= 0); });
     group_sum<NT, 1, 1>(c);
@@ -313,11 +346,11 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void k_policy(PolicyArgs a) {
         double slope[NB] = {};
         if (on)
 #pragma unroll
-          for (int k = 0; k < NB; ++k) slope[k] = policy_term(a, r.p[k], r.x, v + 2 * k, cut + k);
+          for (int k = 0; k < NB; ++k) slope[k] = policy_term<GRAD>(a, r.p[k], r.x, v + 2 * k, cut + k);
 #pragma unroll
         for (int k = 0; k < NB; ++k) {
           clipped[k] += lanes(cut[k]);
-          if (a.dlogp && in && b0 + k < a.nblk) a.dlogp[(size_t)(b0 + k) * a.rows + t] = on ? (float)(slope[k] * share) : 0.f;
+          if (GRAD && in && b0 + k < a.nblk) a.dlogp[(size_t)(b0 + k) * a.rows + t] = on ? (float)(slope[k] * share) : 0.f;
         }
       });
 #pragma unroll
@@ -414,7 +447,7 @@ __global__ __launch_bounds__(1024) void k_policy_few(PolicyArgs a) {
     bool cut = false;
     if (r[k].x.y >= 0) {
       double one[2] = {0.0, 0.0};
-      const double slope = policy_term(a, r[k].p, r[k].x, one, &cut);
+      const double slope = policy_term<true>(a, r[k].p, r[k].x, one, &cut);
       const double share = a.aggregate == ZO_AGG_SUM ? 1.0 : inverse(by_seq ? (double)count[r[k].s] * a.nseq : N);
       v[0] += by_seq ? one[0] * share : one[0];
       v[1] += one[1];
@@ -498,13 +531,19 @@ int zo_policy_loss_launch(int nblk, int rows, int nseq, int aggregate, int per_t
   // 600 under 16 blocks 20.3, 17.7, 55.3; 16 of 2000 -, 10.4, 8.6.
   const long long mean = rows / nseq;
   const int nb = nblk >= 2 ? 2 : 1, y = (nblk + nb - 1) / nb;
-  auto go = [&](auto k, dim3 grid, int threads) { hipLaunchKernelGGL(k, grid, dim3(threads), 0, stream, a); };
-  if (mean <= 128 || (mean <= 512 && (long long)nseq * y >= 16 * mean))
-    nb == 2 ? go(k_policy<64, 2>, dim3((nseq + 3) / 4, y), 256) : go(k_policy<64, 1>, dim3((nseq + 3) / 4, y), 256);
-  else if (mean <= 1000 || (long long)nseq * nblk > 2048)
-    nb == 2 ? go(k_policy<256, 2>, dim3(nseq, y), 256) : go(k_policy<256, 1>, dim3(nseq, y), 256);
-  else
-    go(k_policy<1024, 1>, dim3(nseq, nblk), 1024);
+  auto go = [&](auto grad, auto none, dim3 grid, int threads) {
+    hipLaunchKernelGGL(dlogp ? grad : none, grid, dim3(threads), 0, stream, a);
+  };
+  if (mean <= 128 || (mean <= 512 && (long long)nseq * y >= 16 * mean)) {
+    const dim3 grid((nseq + 3) / 4, y);
+    nb == 2 ? go(k_policy<64, 2, true>, k_policy<64, 2, false>, grid, 256) : go(k_policy<64, 1, true>, k_policy<64, 1, false>, grid, 256);
+  } else if (mean <= 1000 || (long long)nseq * nblk > 2048) {
+    const dim3 grid(nseq, y);
+    nb == 2 ? go(k_policy<256, 2, true>, k_policy<256, 2, false>, grid, 256)
+            : go(k_policy<256, 1, true>, k_policy<256, 1, false>, grid, 256);
+  } else {
+    go(k_policy<1024, 1, true>, k_policy<1024, 1, false>, dim3(nseq, nblk), 1024);
+  }
   st = zo_hip_status(hipGetLastError(), "k_policy");
   if (st != ZO_OK) return st;
   hipLaunchKernelGGL(k_policy_total, dim3(nblk), dim3(256), 0, stream, a);
