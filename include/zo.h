@@ -822,7 +822,8 @@ int zo_token_logprob_backward(int nblk, int T, int vocab, int dtype,
  * labels is NULL or labels[t] >= 0 (device int32 [rows]); what does not count
  * may hold anything, NaN included, and gets a gradient of 0.  A seq_start that
  * breaks the rule sets bad_flag (device int, nullable, never cleared here) and
- * is taken as clamped to it.  Tensors of a block are `rows` apart; what is not
+ * is taken as clamped to it: into [0, rows], and up to the largest one before.
+ * (In a large batch that costs a second pass by one workgroup a block.)  Tensors of a block are `rows` apart; what is not
  * per block is shared by all blocks.
  *
  * Preference loss: sequence 2p is the chosen, 2p + 1 the rejected one of pair

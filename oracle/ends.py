@@ -59,8 +59,9 @@ def token_logprob_backward(X, labels, lse, g, scale):
 
 
 def _span(start, s, rows):
-    lo = min(max(int(start[s]), 0), rows)
-    return lo, min(max(int(start[s + 1]), lo), rows)
+    """A sequence's rows: starts clamped into the rows, and up to the largest one before."""
+    start = np.clip(np.asarray(start[:s + 2], np.int64), 0, rows)
+    return int(start[:s + 1].max()), int(start.max())
 
 
 def _log_sigma(h):

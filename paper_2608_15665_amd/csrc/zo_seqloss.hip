@@ -8,15 +8,31 @@ namespace {
 struct Span {
   int lo, hi;
 };
-// A sequence's rows, clamped into the tensors.
-__device__ __forceinline__ Span span_of(const int* start, int s, int rows, int* bad_flag) {
+// Starts that break their rule are clamped: into the rows, and up to the largest start before them.  A sequence of a large batch
+// sees its own two starts and the first: in a broken batch it may take rows that are another's, never ones outside all sequences,
+// and at least one sequence sees the break.  Its mark in the workspace makes the last launch, which sums what the sequences
+// left there, do its block again, one sequence after another (a sequence that is not marked costs nothing more).
+__device__ __forceinline__ int clamped(int start, int rows) { return min(max(start, 0), rows); }
+__device__ __forceinline__ Span span_of(const int* start, int s, int rows, bool* broken, int* bad_flag) {
   const int a = start[s], b = start[s + 1];
   Span r;
-  r.lo = min(max(a, 0), rows);
-  r.hi = min(max(b, r.lo), rows);
-  if (bad_flag && (r.lo != a || r.hi != b)) *bad_flag = 1;
+  r.lo = max(clamped(a, rows), clamped(start[0], rows));
+  r.hi = max(clamped(b, rows), r.lo);
+  *broken = r.lo != a || r.hi != b;
+  if (bad_flag && *broken) *bad_flag = 1;
   return r;
 }
+// Takes the sequences in order: the next one's rows.
+struct InOrder {
+  const int* start;
+  int rows, hi;
+  __device__ __forceinline__ InOrder(const int* start, int rows) : start(start), rows(rows), hi(clamped(start[0], rows)) {}
+  __device__ __forceinline__ Span next(int s) {
+    const int lo = hi;
+    hi = max(hi, clamped(start[s + 1], rows));
+    return {lo, hi};
+  }
+};
 
 // A wave's sum in every lane: rows of 16 lanes by shifts, then rows onto the next ones, all in the vector unit (a shuffle goes
 // through LDS, whose pipe the sums of short sequences would fill).
@@ -120,18 +136,15 @@ __device__ __forceinline__ double pair_loss(const PrefArgs& a, double z, double*
   return (1.0 - a.smoothing) * (l + (h < 0.0 ? -h : 0.0)) + keep;
 }
 
-// The loss of pair p of block b by NT threads, its rewards and its rows' gradient.
+// The loss of pair p of block b, sequences sp, by NT threads, its rewards and its rows' gradient.
 template <int NT>
-__device__ __forceinline__ double one_pair(const PrefArgs& a, int p, int b) {
+__device__ __forceinline__ double one_pair(const PrefArgs& a, int p, int b, const Span* sp) {
   const float* logp = a.logp + (size_t)b * a.rows;
   const bool first = (threadIdx.x & (NT - 1)) == 0;
   struct Row {
     float p, q;
     int y;
   };
-  Span sp[2];
-#pragma unroll
-  for (int k = 0; k < 2; ++k) sp[k] = span_of(a.start, 2 * p + k, a.rows, first ? a.bad_flag : nullptr);
   // Both sequences' rows together, two of each at a time.
   double v[2] = {0.0, 0.0};
   long long counts[1] = {0};  // of the chosen one, and of the other above
@@ -185,8 +198,13 @@ template <int NT>
 __global__ __launch_bounds__(NT < 256 ? 256 : NT) void k_preference(PrefArgs a) {
   const int p = NT < 256 ? blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x, b = blockIdx.y;
   if (p >= a.pairs) return;
-  const double l = one_pair<NT>(a, p, b);
-  if ((threadIdx.x & (NT - 1)) == 0) a.part[(size_t)b * a.pairs + p] = l;
+  const bool first = (threadIdx.x & (NT - 1)) == 0;
+  Span sp[2];
+  bool broken[2];
+#pragma unroll
+  for (int k = 0; k < 2; ++k) sp[k] = span_of(a.start, 2 * p + k, a.rows, broken + k, first ? a.bad_flag : nullptr);
+  const double l = one_pair<NT>(a, p, b, sp);
+  if (first) a.part[(size_t)b * a.pairs + p] = broken[0] || broken[1] ? __builtin_nan("") : l;  // the mark
 }
 
 __global__ __launch_bounds__(256) void k_preference_total(PrefArgs a) {
@@ -194,15 +212,42 @@ __global__ __launch_bounds__(256) void k_preference_total(PrefArgs a) {
   each_row<256>(Span{0, a.pairs}, [&](int i) { return a.part[(size_t)blockIdx.x * a.pairs + i]; },
                 [&](int, bool in, double l) { v[0] += in ? l : 0.0; });
   group_sum<256, 1>(v);
+  if (v[0] != v[0]) {  // by a mark, or by the inputs
+    int broken = 0;
+    for (int s = threadIdx.x; s <= 2 * a.pairs; s += 256)
+      broken |= clamped(a.start[s], a.rows) != a.start[s] || (s > 0 && a.start[s - 1] > a.start[s]);
+    if (__syncthreads_or(broken)) {
+      InOrder seqs(a.start, a.rows);
+      v[0] = 0.0;
+      for (int p = 0; p < a.pairs; ++p) {
+        const Span sp[2] = {seqs.next(2 * p), seqs.next(2 * p + 1)};
+        v[0] += one_pair<256>(a, p, blockIdx.x, sp);
+      }
+    }
+  }
   if (threadIdx.x == 0) a.loss[blockIdx.x] = a.weight / a.pairs * v[0];
 }
 
 // All pairs of a block by one workgroup, a wave per pair: few rows need no second launch.
 __global__ __launch_bounds__(1024) void k_preference_few(PrefArgs a) {
   __shared__ double each[16];
-  const int w = threadIdx.x >> 6;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  // Lane s has the clamped start of sequence s: at most 33.
+  const int given = a.start[min(lane, 2 * a.pairs)];
+  int start = clamped(given, a.rows);
+  const int before = __shfl_up(start, 1, 64);
+  if (__ballot(start != given || (lane > 0 && before > start))) {
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) start = max(start, __shfl_up(start, off, 64));  // a lane without one takes its own
+    if (a.bad_flag && threadIdx.x == 0) *a.bad_flag = 1;
+  }
   double l = 0.0;
-  for (int p = w; p < a.pairs; p += 16) l += one_pair<64>(a, p, blockIdx.x);
+  for (int p = w; p < a.pairs; p += 16) {
+    const int s[3] = {__builtin_amdgcn_readlane(start, 2 * p), __builtin_amdgcn_readlane(start, 2 * p + 1),
+                      __builtin_amdgcn_readlane(start, 2 * p + 2)};
+    const Span sp[2] = {{s[0], s[1]}, {s[1], s[2]}};
+    l += one_pair<64>(a, p, blockIdx.x, sp);
+  }
   if ((threadIdx.x & 63) == 0) each[w] = l;
   __syncthreads();
   if (threadIdx.x != 0) return;
@@ -315,7 +360,8 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void k_policy(PolicyArgs a) {
   }
   if (s >= a.nseq) return;
   const bool first = (threadIdx.x & (NT - 1)) == 0;
-  const Span sp = span_of(a.start, s, a.rows, first && b0 == 0 ? a.bad_flag : nullptr);
+  bool broken;
+  const Span sp = span_of(a.start, s, a.rows, &broken, first && b0 == 0 ? a.bad_flag : nullptr);
   if (GRAD && a.aggregate == ZO_AGG_SEQUENCE) {
     int c[1] = {0};
     each_row<NT>(sp, [&](int t) { return a.labels ? a.labels[t] : 0; }, [&](int, bool in, int y) { c[0] += lanes(in && y >= 0); });
@@ -358,7 +404,7 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void k_policy(PolicyArgs a) {
   v[3 * NB] = count;
   group_sum<NT, 3 * NB + 1, NB + 1>(v);
   if (!first) return;
-  if (b0 == 0) a.of_seq[s] = (int)v[3 * NB];
+  if (b0 == 0) a.of_seq[s] = broken ? -1 : (int)v[3 * NB];  // the mark
   const double mine = a.aggregate == ZO_AGG_SEQUENCE ? inverse(v[3 * NB] * a.nseq) : 1.0;
 #pragma unroll
   for (int k = 0; k < NB; ++k) {
@@ -368,6 +414,41 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void k_policy(PolicyArgs a) {
     to[1] = v[2 * k + 1];
     to[2] = v[2 * NB + k];
   }
+}
+
+// All sequences of a block whose starts are broken, one after another by 256 threads: v gets the sums of the loss, of k and of
+// the clipped rows, and the rows that count.
+__device__ __forceinline__ void in_order(const PolicyArgs& a, double* v) {
+  auto label = [&](int t) { return a.labels ? a.labels[t] : 0; };
+  int n[1] = {0};
+  InOrder all(a.start, a.rows);
+  for (int s = 0; s < a.nseq; ++s) each_row<256>(all.next(s), label, [&](int, bool in, int y) { n[0] += lanes(in && y >= 0); });
+  group_sum<256, 1, 1>(n);
+  v[0] = v[1] = v[2] = 0.0;
+  v[3] = n[0];
+  const size_t block = (size_t)blockIdx.x * a.rows;
+  InOrder seqs(a.start, a.rows);
+  for (int s = 0; s < a.nseq; ++s) {
+    const Span sp = seqs.next(s);
+    double share = a.aggregate == ZO_AGG_TOKEN ? inverse(v[3]) : 1.0;
+    if (a.aggregate == ZO_AGG_SEQUENCE) {
+      int c[1] = {0};
+      each_row<256>(sp, label, [&](int, bool in, int y) { c[0] += lanes(in && y >= 0); });
+      group_sum<256, 1, 1>(c);
+      share = inverse((double)c[0] * a.nseq);
+    }
+    for (int t = sp.lo + (int)threadIdx.x; t < sp.hi; t += 256) {
+      double one[2] = {0.0, 0.0}, slope = 0.0;
+      bool cut = false;
+      const PolicyRow x = policy_row(a, t, s);
+      if (x.y >= 0) slope = policy_term<true>(a, a.logp[block + t], x, one, &cut);
+      v[0] += a.aggregate == ZO_AGG_SEQUENCE ? one[0] * share : one[0];
+      v[1] += one[1];
+      v[2] += cut ? 1.0 : 0.0;
+      if (a.dlogp) a.dlogp[block + t] = (float)(slope * share * a.weight);
+    }
+  }
+  group_sum<256, 3>(v);
 }
 
 __global__ __launch_bounds__(256) void k_policy_total(PolicyArgs a) {
@@ -383,9 +464,10 @@ __global__ __launch_bounds__(256) void k_policy_total(PolicyArgs a) {
         if (!in) return;
 #pragma unroll
         for (int k = 0; k < 3; ++k) v[k] += r.x[k];
-        v[3] += r.n;
+        v[3] += r.n < 0 ? __builtin_nan("") : (double)r.n;
       });
   group_sum<256, 4>(v);
+  if (v[3] != v[3]) in_order(a, v);
   if (threadIdx.x != 0) return;
   a.loss[blockIdx.x] = a.weight * (a.aggregate == ZO_AGG_TOKEN ? v[0] * inverse(v[3]) : v[0]);
   if (a.stats) {
@@ -398,16 +480,29 @@ __global__ __launch_bounds__(256) void k_policy_total(PolicyArgs a) {
 // the last one that starts at it or before.
 constexpr int FEW_SEQS = 256, FEW_ROWS = 4;  // sequences, and rows of a thread
 __global__ __launch_bounds__(1024) void k_policy_few(PolicyArgs a) {
-  __shared__ int start[FEW_SEQS + 1], count[FEW_SEQS];
+  constexpr int WAVES = FEW_SEQS / 64 + 1;  // that have starts
+  __shared__ int start[FEW_SEQS + 1], count[FEW_SEQS], broken[WAVES];
   const int b = blockIdx.x, t0 = threadIdx.x;
-  for (int s = t0; s <= a.nseq; s += 1024) {
-    const int v = a.start[s];
-    start[s] = min(max(v, 0), a.rows);
-    if (a.bad_flag && (v < 0 || v > a.rows || (s > 0 && a.start[s - 1] > v))) *a.bad_flag = 1;
-    if (s < a.nseq) count[s] = 0;
+  if (t0 < 64 * WAVES) {
+    const int s = min(t0, a.nseq), given = a.start[s], before = a.start[max(s - 1, 0)];
+    start[s] = clamped(given, a.rows);
+    if (t0 < a.nseq) count[t0] = 0;
+    const unsigned long long bad = __ballot(clamped(given, a.rows) != given || (s > 0 && before > given));
+    if ((t0 & 63) == 0) broken[t0 >> 6] = bad != 0;
   }
   __syncthreads();
-  const int lo = start[0], hi = max(start[a.nseq], lo);
+  const int lo = start[0];
+  int hi = start[a.nseq], bad = 0;
+#pragma unroll
+  for (int w = 0; w < WAVES; ++w) bad |= broken[w];
+  if (bad) {
+    if (t0 == 0) {
+      for (int s = 1; s <= a.nseq; ++s) start[s] = max(start[s], start[s - 1]);
+      if (a.bad_flag) *a.bad_flag = 1;
+    }
+    __syncthreads();
+    hi = start[a.nseq];
+  }
   const bool by_seq = a.aggregate == ZO_AGG_SEQUENCE;
   struct Row {
     PolicyRow x;
