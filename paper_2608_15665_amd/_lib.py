@@ -1221,6 +1221,7 @@ def _logits(X: torch.Tensor, labels: torch.Tensor, vocab: Optional[int], here: i
         raise ValueError("logits must be rows x columns")
     n, cols = X.shape
     vocab = cols if vocab is None else int(vocab)
+    _fits(vocab, "vocab")
     T = labels.numel()
     if vocab > cols:
         raise ValueError(f"logits of {cols} columns for a vocabulary of {vocab}")
