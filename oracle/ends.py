@@ -129,7 +129,7 @@ def policy_loss(logp, old, adv, labels, start, ref=None, per_token=False, low=0.
             A, p = float(adv[t] if per_token else adv[s]), float(logp[t])
             r = np.exp(p - float(old[t]))
             c = min(max(r, 1 - low), 1 + high)
-            l, slope = -min(r * A, c * A), (-r * A if r * A <= c * A else 0.0)
+            l, slope = -min(r * A, c * A), (0.0 if r * A > c * A else -r * A)
             clipped += r * A > c * A
             if ref is not None:
                 d = float(ref[t]) - p
