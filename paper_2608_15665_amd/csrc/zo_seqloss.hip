@@ -281,7 +281,8 @@ __device__ __forceinline__ PolicyRow policy_row(const PolicyArgs& a, int t, int 
 }
 
 // exp(d) = 2^n (1 + r + q): d = n log 2 + r with |r| <= log(2) / 2, and q = exp(r) - r - 1 by its series, r^2 (1/2! + r/3! + ... +
-// r^11/13!), 2^-52 of it left out.  Below -800 exp is 0; n stops at 1154, where it is infinite whatever r is; NaN stays in r.
+// r^11/13!), 2^-52 of it left out.  Below -800 exp is 0.  n stops at 1023, where r grows instead and 2^n (1 + r + q) beyond all numbers
+// with it; infinity and NaN stay in r.
 struct Exponential {
   double r, q;
   int n;
@@ -289,7 +290,7 @@ struct Exponential {
     constexpr double over[12] = {1.0 / 6227020800.0, 1.0 / 479001600.0, 1.0 / 39916800.0, 1.0 / 3628800.0, 1.0 / 362880.0, 1.0 / 40320.0,
                                  1.0 / 5040.0,       1.0 / 720.0,       1.0 / 120.0,      1.0 / 24.0,      1.0 / 6.0,      0.5};
     const double x = d < -800.0 ? -800.0 : d;
-    const double e = fmin(rint(x * 1.4426950408889634), 1154.0);
+    const double e = fmin(rint(x * 1.4426950408889634), 1023.0);
     r = fma(-e, 2.3190468138462996e-17, fma(-e, 0.6931471805599453, x));  // log 2 in two parts
     double p = over[0];
 #pragma unroll
@@ -305,9 +306,8 @@ struct Exponential {
 __device__ __forceinline__ double kl_term(double d, double* m) {
   const Exponential e(d);
   const double t = ldexp(1.0, e.n), t1 = t - 1.0;
-  const bool huge = e.n > 1023;  // t is infinite, or d is NaN
-  *m = huge ? t * d : fma(t, e.r + e.q, t1);
-  return huge ? t * d : fma(t, e.q, t1 + fma(t, e.r, -d));
+  *m = fma(t, e.r + e.q, t1);
+  return fma(t, e.q, t1 + fma(t, e.r, -fmin(d, 1e300)));  // at d = infinity r alone is infinite
 }
 
 // Adds a row that counts to (loss, k), says whether it is clipped and returns its slope.
