@@ -744,8 +744,8 @@ int zo_paged_attention(const zo_kv_cache* cache, const zo_kv_batch* batch,
  *   bad_flag  device int, nullable: set to 1 (never cleared here) when a token
  *             is >= vocab; its row of H is NaN.
  * The product is taken in fp32 and rounded once.  rows = 0 launches nothing.
- * Limits: 0 <= rows <= 2^30; vocab >= 1; d % 8 == 0, d <= 2^20; 16-byte
- * aligned E and H; scale finite. */
+ * Limits: 0 <= rows <= 2^30; 1 <= vocab < 2^30; d % 8 == 0, 8 <= d <= 2^20;
+ * rows d < 2^40; 16-byte aligned E and H; scale finite. */
 int zo_embedding(long long rows, int vocab, int d, int dtype, const int* ids,
                  const void* E, float scale, void* H, int* bad_flag,
                  void* stream);
@@ -763,9 +763,11 @@ int zo_embedding(long long rows, int vocab, int d, int dtype, const int* ids,
  * >= vocab, which set bad_flag.
  *   dH   device, rows x d of dtype.      dE   device, vocab x d of out_dtype:
  *        dtype or ZO_F32.  It overlaps no other tensor of the call.
- * Limits: 0 <= rows <= 2^24; vocab < 2^30; the rest as for zo_embedding; the
- * workspace (0 bytes for few tokens) is not shared with a call that may run at
- * the same time. */
+ * The sort's reads grow with the square of the rows from some 2^20 on: 1 ms at
+ * 2^22, 11 ms at 2^24 (the sums read rows d elements beside it).
+ * Limits: 0 <= rows <= 2^24; the rest as for zo_embedding; the workspace (0
+ * bytes for few tokens) is not shared with a call that may run at the same
+ * time. */
 size_t zo_embedding_backward_workspace(long long rows, int vocab, int d);
 int zo_embedding_backward(long long rows, int vocab, int d, int dtype,
                           const int* ids, const void* dH, float scale,
@@ -807,7 +809,9 @@ int zo_token_logprob(int nblk, int T, int vocab, int dtype, const void* X,
  * |logp| < |lse| are taken as exp(scale (X[i][j] - X[i][y]) + logp[i]), which is
  * |logp| 2^-24 off.  y < 0: zeros (X and g not read); y >= vocab: NaN and
  * bad_flag.  dX has X's layout and dtype, rows ldo apart; it may be X itself
- * (ldo = ld, logp NULL: another part of a row may have replaced X[i][y]).
+ * (ldo = ld, logp NULL: another part of a row may have replaced X[i][y]).  A call
+ * whose rows of dX begin elsewhere in a 16-byte word than X's takes about twice
+ * as long.
  * Columns behind the vocabulary stay as they are.  fp32 arithmetic, one
  * rounding.  Limits as for zo_token_logprob. */
 int zo_token_logprob_backward(int nblk, int T, int vocab, int dtype,
@@ -874,8 +878,8 @@ int zo_preference_loss(int nblk, int rows, int pairs, int kind, int average,
  *   stats       device float64 [nblk x 2], nullable: the mean of k and the share
  *               of rows with r A > c A, over the N rows.
  *   logp, loss, dlogp, the arithmetic and the workspace as for zo_preference_loss.
- * Limits: those of zo_preference_loss with nseq for pairs; clip_low in [0, 1],
- * clip_high finite and >= 0, kl_coef finite and >= 0, weight finite. */
+ * Limits: those of zo_preference_loss with nseq for pairs, and nseq <= 2^23;
+ * clip_low in [0, 1], clip_high and kl_coef finite and >= 0, weight finite. */
 typedef enum { ZO_AGG_TOKEN = 0, ZO_AGG_SEQUENCE = 1, ZO_AGG_SUM = 2 } zo_aggregate;
 size_t zo_policy_loss_workspace(int nblk, int rows, int nseq);
 int zo_policy_loss(int nblk, int rows, int nseq, int aggregate, int per_token,

@@ -37,16 +37,20 @@ of include/zo.h); this package only binds it.  Entry points:
     sq_loss, combine_central, combine_forward   loss and estimate helpers (central
                            difference, or forward difference against a baseline block)
 """
-from ._lib import (ZO_BF16, ZO_E4M3, ZO_EPI_NONE, ZO_EPI_RELU, ZO_EPI_RESIDUAL, ZO_EPI_SILU_MUL, ZO_F16, ZO_F32, ZO_MAX_BLOCKS,
-                   ZO_MAX_QR_RANK, ZO_MAX_RANK, ZO_NOALLOC_SCRATCH_BYTES, ABI_SYMBOLS, LIB_PATH, DecoderLayer, LlamaLayer,
-                   LlamaLoraLayer, LoraPerturbedLinear, PerturbedLinear, Workspace, ZoError, abi_version, causal_attention, combine_central,
-                   combine_forward, embedding, embedding_backward, kv_append, layernorm, lib, lora_perturbed_linear,
-                   paged_attention, perturbed_linear, policy_loss, preference_loss, prepare_group, rmsnorm, rope, sq_loss, subspace_adam_update, subspace_refresh, subspace_refresh_noalloc,
+from ._lib import (ZO_BF16, ZO_E4M3, ZO_EPI_NONE, ZO_EPI_RELU, ZO_EPI_RESIDUAL, ZO_EPI_SILU_MUL, ZO_F16,
+                   ZO_F32, ZO_MAX_BLOCKS, ZO_MAX_QR_RANK, ZO_MAX_RANK, ZO_NOALLOC_SCRATCH_BYTES, ABI_SYMBOLS,
+                   LIB_PATH, DecoderLayer, LlamaLayer, LlamaLoraLayer, LoraPerturbedLinear, PerturbedLinear,
+                   Workspace, ZoError, abi_version, causal_attention, combine_central, combine_forward,
+                   embedding, embedding_backward, kv_append, layernorm, lib, lora_perturbed_linear,
+                   paged_attention, perturbed_linear, policy_loss, preference_loss, prepare_group, rmsnorm,
+                   rope, sq_loss, subspace_adam_update, subspace_refresh, subspace_refresh_noalloc,
                    subspace_sgd_update, token_logprob, token_logprob_backward)
 
-__all__ = ["ZO_BF16", "ZO_E4M3", "ZO_EPI_NONE", "ZO_EPI_RELU", "ZO_EPI_RESIDUAL", "ZO_EPI_SILU_MUL", "ZO_F16", "ZO_F32", "ZO_MAX_BLOCKS",
-           "ZO_MAX_QR_RANK", "ZO_MAX_RANK", "ZO_NOALLOC_SCRATCH_BYTES", "ABI_SYMBOLS", "LIB_PATH", "DecoderLayer", "LlamaLayer", "LlamaLoraLayer", "LoraPerturbedLinear",
+__all__ = ["ZO_BF16", "ZO_E4M3", "ZO_EPI_NONE", "ZO_EPI_RELU", "ZO_EPI_RESIDUAL", "ZO_EPI_SILU_MUL", "ZO_F16",
+           "ZO_F32", "ZO_MAX_BLOCKS", "ZO_MAX_QR_RANK", "ZO_MAX_RANK", "ZO_NOALLOC_SCRATCH_BYTES",
+           "ABI_SYMBOLS", "LIB_PATH", "DecoderLayer", "LlamaLayer", "LlamaLoraLayer", "LoraPerturbedLinear",
            "PerturbedLinear", "Workspace", "ZoError", "abi_version", "causal_attention", "combine_central",
-           "combine_forward", "embedding", "embedding_backward", "kv_append", "layernorm", "lib", "lora_perturbed_linear", "paged_attention", "perturbed_linear",
-           "policy_loss", "preference_loss", "prepare_group", "rmsnorm", "rope", "sq_loss",
-           "subspace_adam_update", "subspace_refresh", "subspace_refresh_noalloc", "subspace_sgd_update", "token_logprob", "token_logprob_backward"]
+           "combine_forward", "embedding", "embedding_backward", "kv_append", "layernorm", "lib",
+           "lora_perturbed_linear", "paged_attention", "perturbed_linear", "policy_loss", "preference_loss",
+           "prepare_group", "rmsnorm", "rope", "sq_loss", "subspace_adam_update", "subspace_refresh",
+           "subspace_refresh_noalloc", "subspace_sgd_update", "token_logprob", "token_logprob_backward"]

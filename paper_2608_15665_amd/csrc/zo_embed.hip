@@ -208,7 +208,8 @@ __global__ __launch_bounds__(64 * SORT_WAVES) void k_sort_count(const int* __res
   if (t < DIGITS) hist[(size_t)blockIdx.x * DIGITS + t] = cnt[t];
 }
 
-// A tile's items to their places among all.
+// A tile's items to their places among all.  Each tile reads all tiles' counts, 2 KB x tiles^2 a pass: nothing at 64 tiles, but what a
+// call of 2^22 and of 2^24 rows of 8 columns takes (1.2 and 11 ms; 2^20 0.24).
 __global__ __launch_bounds__(64 * SORT_WAVES) void k_sort_scatter(const int* __restrict__ ids, SortPlan p, int pass,
                                                                   const int* __restrict__ hist, const int* key_in,
                                                                   const int* row_in, int* key_out, int* row_out, Fill f) {

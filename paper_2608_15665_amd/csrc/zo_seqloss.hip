@@ -347,9 +347,9 @@ __global__ __launch_bounds__(256) void k_policy_count(PolicyArgs a) {
   if (threadIdx.x == 0) a.counted[blockIdx.x] = n[0];
 }
 
-// NT threads take a sequence, under NB blocks at once: what the blocks share is loaded once.  Float64 bounds it beside its
-// start: two exponentials of some 30 instructions a row and block; 512 sequences of up to 1024 rows under 16 blocks 21 us (with
-// one block a workgroup 24, four 25), twice the rows 13 more.
+// NT threads take a sequence, under NB blocks at once: what the blocks share is loaded once.  Float64 bounds it beside its start:
+// 112 vector instructions a row and block, two exponentials and k about half of them.  512 sequences of up to 1024 rows under 16
+// blocks, a call in a graph: 21.3 us (with one block a workgroup 24.0, four 21.8), twice the rows 12.6 more.
 template <int NT, int NB, bool GRAD>
 __global__ __launch_bounds__(NT < 256 ? 256 : NT) void k_policy(PolicyArgs a) {
   const int s = NT < 256 ? blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x, b0 = blockIdx.y * NB;
@@ -598,8 +598,9 @@ int zo_policy_loss_launch(int nblk, int rows, int nseq, int aggregate, int per_t
                           double kl_coef, double weight, const float* logp, const float* old_logp, const float* ref_logp,
                           const float* advantage, const int* labels, const int* seq_start, double* loss, double* stats,
                           float* dlogp, int* bad_flag, void* ws, hipStream_t stream, size_t* ws_needed) {
-  // us a call with one launch and with two, from Python one after another (the host bounds them) and in a graph: 16 sequences of
-  // 100 rows 8.4, 12.8 and 6.2, 5.9; of 250 10.0, 12.9 and 10.5, 5.9; 500 rows each, 8 a thread, 18 in a graph.
+  // us a call with a KL term and gradients in one launch and in two (three for ZO_AGG_TOKEN), from Python one after another (the host
+  // bounds the latter) and in a graph.  Sequence means, 16 sequences of 100 rows: 8.4, 12.3 and 6.2, 6.3; of 250: 10.3, 12.1 and 10.8,
+  // 6.2.  Token means: 8.3, 14.6 and 5.7, 8.7; 8.8, 15.3 and 9.3, 9.8.  16 of 500 rows, 8 a thread, 18 in a graph.
   const bool few = rows <= 1024 * FEW_ROWS && nseq <= FEW_SEQS;
   const int ncount = rows < 256 * 4096 ? (rows + 4095) / 4096 + (rows == 0) : 256;
   WsCarver w(ws);
@@ -621,9 +622,9 @@ int zo_policy_loss_launch(int nblk, int rows, int nseq, int aggregate, int per_t
     hipLaunchKernelGGL(k_policy_count, dim3(ncount), dim3(256), 0, stream, a);
     if ((st = zo_hip_status(hipGetLastError(), "k_policy_count")) != ZO_OK) return st;
   }
-  // us with a wave, 256 and 1024 threads a sequence (and two blocks, but with 1024): 4096 sequences of 200 rows 16.6, 19.6, -; 1024
-  // of 200 9.3, 8.8, -; of 600 14.3, 10.4, 18.1; 1024 of 500 under 16 blocks 36.7, 43.1, -; 256 of 4000 -, 22.9, 12.7; 256 of
-  // 600 under 16 blocks 20.3, 17.7, 55.3; 16 of 2000 -, 10.4, 8.6.
+  // us in a graph with a wave, 256 and 1024 threads a sequence (and two blocks, but with 1024), with a KL term and, for one block, its
+  // gradient: 4096 sequences of 200 rows 18.0, 19.4, 51.0; 1024 of 200 12.6, 11.5, 19.1; of 600 16.1, 13.1, 20.5; 1024 of 500 under 16
+  // blocks 30.1, 30.8, 135; 256 of 4000 67.9, 25.2, 17.0; 256 of 600 under 16 blocks 14.2, 13.6, 37.1; 16 of 2000 26.3, 13.4, 12.0.
   const long long mean = rows / nseq;
   const int nb = nblk >= 2 ? 2 : 1, y = (nblk + nb - 1) / nb;
   auto go = [&](auto grad, auto none, dim3 grid, int threads) {
